@@ -1,0 +1,318 @@
+"""The 8-bit operators of the link-step library as timed cases, with their plain forms.
+
+The projections of the recomputed rows can run on 8-bit operands: e4m3 values with one
+power-of-two scale (e8m0) for each 128 consecutive values of a row of activations, or for
+each 128 x 128 block of weights.  Three operators make such a layer:
+
+    quant  rows or weights in bf16 -> e4m3 and scales             epic_quant_fp8
+    norm   residual stream + partial products -> RMSNorm -> e4m3  epic_rmsnorm_fp8
+    gemm   e4m3 x e4m3 product with its epilogues                 epic_gemm_fp8
+
+    own                 False: plain torch; True: the library's kernels
+    listed()            the named cases
+    draw(rng)           one more case of the same ranges
+    prepare(case, seed) inputs and buffers in device memory
+    run(state)          one pass; returns its outputs
+    work(case)          bytes and operations the pass cannot do without
+    exact(case, seed)   the same outputs from the definition in float64
+
+Scales are bytes of e8m0 (2 ** (byte - 127)).  Scales of m rows are laid out
+[k / 128][m rounded up to 4]: a group of all rows is contiguous.
+"""
+import math
+
+import torch
+
+own = False
+
+GROUP = 128
+TOP = 448.0                      # largest e4m3 value
+EPS = 1e-5
+# (n, k) of the projections of the 32-layer model configuration: q|k|v, output, gate|up, down
+QKV, OUT, GATE_UP, DOWN = (6144, 4096), (4096, 4096), (28672, 4096), (4096, 14336)
+ROWS_LINK, ROWS_COMPILE = 736, 20560      # recomputed rows of a link step; tokens of a compile step
+MOST = ROWS_COMPILE * GATE_UP[0] * GATE_UP[1]
+
+
+def _quant(name, m, k, block_rows=1):
+    return {"name": name, "what": "quant", "m": m, "k": k, "block_rows": block_rows}
+
+
+def _norm(name, m, k, adds):
+    return {"name": name, "what": "norm", "m": m, "k": k, "adds": adds}
+
+
+def _gemm(name, epilogue, m, shape):
+    return {"name": name, "what": "gemm", "epilogue": epilogue, "m": m, "n": shape[0], "k": shape[1]}
+
+
+def listed():
+    return [
+        # attention output of a decode step of 32 requests, before the output projection
+        _quant("quant_decode32", 32, 4096),
+        # attention output of a compile step
+        _quant("quant_compile", ROWS_COMPILE, 4096),
+        # gate|up weights of a layer, laid out once when the model is loaded
+        _quant("quant_weights_gate_up", *GATE_UP, block_rows=128),
+        # one request decoding: the stream plus one partial product
+        _norm("norm_decode1", 1, 4096, 1),
+        # a link step, its output projection left in two parts of k
+        _norm("norm_link736_two", ROWS_LINK, 4096, 2),
+        # a compile step of a wide model
+        _norm("norm_compile8192", ROWS_COMPILE, 8192, 1),
+        # one request decoding: q|k|v
+        _gemm("gemm_decode1_qkv", "store", 1, QKV),
+        # a batch of 32 decoding: down projection onto the stream
+        _gemm("gemm_decode32_down", "residual", 32, DOWN),
+        # a batch of 100: gate|up to bf16
+        _gemm("gemm_batch100_gate_up", "swiglu", 100, GATE_UP),
+        # a ragged row count between decode and link
+        _gemm("gemm_rows501_out", "store", 501, OUT),
+        # a link step: gate|up, its result quantised for the down projection
+        _gemm("gemm_link736_gate_up", "swiglu_fp8", ROWS_LINK, GATE_UP),
+        # a compile step: gate|up, the largest product
+        _gemm("gemm_compile_gate_up", "swiglu_fp8", ROWS_COMPILE, GATE_UP),
+    ]
+
+
+def _log(rng, lo, hi, step=1):
+    return max(lo, min(hi, step * round(math.exp(rng.uniform(math.log(lo), math.log(hi))) / step)))
+
+
+def draw(rng):
+    what = rng.choice(["quant", "norm", "gemm", "gemm"])
+    m = _log(rng, 1, ROWS_COMPILE)
+    if what == "quant":
+        k = _log(rng, 128, 14336, 128)
+        return {"what": what, "m": m, "k": k, "block_rows": rng.choice([1, 1, 128])}
+    if what == "norm":
+        return {"what": what, "m": m, "k": _log(rng, 256, 8192, 128), "adds": rng.randrange(4)}
+    n, k = _log(rng, 512, 28672, 256), _log(rng, 256, 14336, 128)
+    m = max(1, min(m, MOST // (n * k)))
+    return {"what": what, "epilogue": rng.choice(["store", "residual", "swiglu", "swiglu_fp8"]), "m": m, "n": n, "k": k}
+
+
+def work(case):
+    m, k = case["m"], case["k"]
+    groups = m * (k // GROUP)
+    if case["what"] == "quant":
+        scales = -(-m // case["block_rows"]) * (k // GROUP)
+        return {"bytes": 3 * m * k + scales, "flops": 3.0 * m * k}
+    if case["what"] == "norm":
+        stream = 8 if case["adds"] else 4                     # the stream is written back where it changes
+        return {"bytes": m * k * (stream + 4 * case["adds"] + 1) + groups + 2 * k, "flops": (6.0 + case["adds"]) * m * k}
+    n = case["n"]
+    out = {"store": 4 * m * n, "residual": 8 * m * n, "swiglu": m * n, "swiglu_fp8": m * (n // 2) + m * (n // 2 // GROUP)}
+    blocks = (n // GROUP) * (k // GROUP)
+    return {"bytes": m * k + groups + n * k + blocks + out[case["epilogue"]], "flops": 2.0 * m * n * k}
+
+
+# ---------------------------------------------------------------- the definition
+
+def _exponent(top):
+    """Smallest t with top <= 448 * 2 ** t (0 where top is 0), in the range of an e8m0 byte."""
+    f, x = torch.frexp(top)                                   # top = f 2^x, 0.5 <= f < 1; 448 = 0.875 * 2^9
+    t = torch.where(f > TOP / 512.0, x - 8, x - 9)
+    return torch.where(top > 0, t, torch.zeros_like(t)).clamp(-127, 127)
+
+
+def _groups(y, block_rows):
+    """y [m, k] -> exponents of its blocks [ceil(m / block_rows), k / 128], from its finite values."""
+    m, k = y.shape
+    top = torch.where(torch.isfinite(y), y.abs(), torch.zeros_like(y)).view(m, k // GROUP, GROUP).amax(-1)
+    if block_rows > 1:
+        top = torch.nn.functional.pad(top, (0, 0, 0, -m % block_rows)).view(-1, block_rows, k // GROUP).amax(1)
+    return _exponent(top)
+
+
+def _scaled(y, t, block_rows):
+    """y / 2 ** t, blockwise."""
+    m, k = y.shape
+    t = t.repeat_interleave(block_rows, 0)[:m] if block_rows > 1 else t
+    return torch.ldexp(y.view(m, k // GROUP, GROUP), -t[..., None]).view(m, k)
+
+
+def _bytes(t):
+    return (t + 127).to(torch.uint8)
+
+
+def _to_fp8(y, block_rows=1):
+    """(values in e4m3, scale bytes with one row per row block)."""
+    t = _groups(y, block_rows)
+    return _scaled(y, t, block_rows).to(torch.float8_e4m3fn), _bytes(t)
+
+
+def _wide(q, scale, block_rows, dtype):
+    """What e4m3 values and scale bytes (one row per row block) stand for."""
+    m, k = q.shape
+    s = torch.ldexp(torch.ones((), dtype=dtype, device=q.device), scale.to(torch.int32) - 127)
+    s = s.repeat_interleave(block_rows, 0)[:m] if block_rows > 1 else s
+    return (q.to(dtype).view(m, k // GROUP, GROUP) * s[..., None]).view(m, k)
+
+
+def _normed(x, weight):
+    return x * torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS) * weight.to(x.dtype)
+
+
+def _swiglu(y):
+    gate, up = y.chunk(2, -1)
+    return gate * torch.sigmoid(gate) * up
+
+
+# ---------------------------------------------------------------- inputs
+
+def _activations(gen, m, k):
+    """Rows as a decoder has them: channels of unlike size, one in 64 much larger."""
+    size = torch.exp(0.5 * torch.empty(k, device="cuda").normal_(generator=gen))
+    loud = torch.rand(k, device="cuda", generator=gen) < 1.0 / 64
+    return torch.empty(m, k, device="cuda").normal_(generator=gen) * torch.where(loud, 12.0 * size, size)
+
+
+def _padded(scale):
+    """Scale bytes [m, k / 128] of rows in the library's layout [k / 128][m rounded up to 4]."""
+    m, g = scale.shape
+    out = torch.zeros((g, -(-m // 4) * 4), dtype=torch.uint8, device=scale.device)
+    out[:, :m] = scale.t()
+    return out
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    m, k = case["m"], case["k"]
+
+    def empty(*shape, dtype=torch.uint8):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+    st = {"case": case}
+    if case["what"] == "quant":
+        rows = case["block_rows"]
+        if rows == 1:
+            st["x"] = _activations(gen, m, k).to(torch.bfloat16)
+            st["scale"] = empty(k // GROUP, -(-m // 4) * 4)
+        else:
+            st["x"] = (torch.empty(m, k, device="cuda").normal_(generator=gen) * (0.5 / math.sqrt(k))).to(torch.bfloat16)
+            st["scale"] = empty(-(-m // rows), k // GROUP)
+        st["q"] = empty(m, k)
+        return st
+    if case["what"] == "norm":
+        st["x"] = _activations(gen, m, k)
+        st["add"] = torch.empty(case["adds"], m, k, device="cuda").normal_(generator=gen) if case["adds"] else None
+        st["weight"] = (1.0 + 0.1 * torch.empty(k, device="cuda").normal_(generator=gen)).to(torch.bfloat16)
+        st["sum"] = empty(m, k, dtype=torch.float32) if case["adds"] else None
+        st["q"], st["scale"] = empty(m, k), empty(k // GROUP, -(-m // 4) * 4)
+        return st
+    n = case["n"]
+    a, sa = _to_fp8(_activations(gen, m, k))
+    w, st["w_scale"] = _to_fp8(torch.empty(n, k, device="cuda").normal_(generator=gen) * (0.5 / math.sqrt(k)), 128)
+    st["a"], st["w"], st["a_scale"] = a, w, _padded(sa)
+    e = case["epilogue"]
+    if e == "store":
+        st["c"] = empty(m, n, dtype=torch.float32)
+    elif e == "residual":
+        st["c"] = torch.empty(m, n, device="cuda").normal_(generator=gen)
+    elif e == "swiglu":
+        st["act"] = empty(m, n // 2, dtype=torch.bfloat16)
+    else:
+        st["act"], st["act_scale"] = empty(m, n // 2), empty(n // 2 // GROUP, -(-m // 4) * 4)
+    # 64 MB of partial sums and what else the library's products need
+    st["workspace"] = empty(72 << 20)
+    return st
+
+
+# ---------------------------------------------------------------- one pass
+
+def _e4m3(q):
+    return q.view(torch.float8_e4m3fn)
+
+
+def _row_scales(scale, m):
+    return scale[:, :m].view(torch.float8_e8m0fnu)
+
+
+def _run_own(st):
+    from paper_2410_15332_amd import epic_link as el
+
+    case = st["case"]
+    m = case["m"]
+    if case["what"] == "quant":
+        el.epic_quant_fp8(st["x"], st["q"], st["scale"], block_rows=case["block_rows"])
+        if case["block_rows"] == 1:
+            return {"q": _e4m3(st["q"]), "scale": _row_scales(st["scale"], m)}
+        return {"q": _e4m3(st["q"]), "scale": st["scale"].view(torch.float8_e8m0fnu)}
+    if case["what"] == "norm":
+        el.epic_rmsnorm_fp8(st["x"], st["weight"], EPS, st["q"], st["scale"], add=st["add"], x_out=st["sum"])
+        out = {"q": _e4m3(st["q"]), "scale": _row_scales(st["scale"], m)}
+        return {**out, "x": st["sum"]} if case["adds"] else out
+    e, ab = case["epilogue"], (st["a"], st["a_scale"], st["w"], st["w_scale"])
+    if e == "store":
+        el.epic_gemm_fp8(el.GEMM_STORE, *ab, c=st["c"], workspace=st["workspace"])
+        return st["c"]
+    if e == "residual":
+        el.epic_gemm_fp8(el.GEMM_RESIDUAL, *ab, c=st["c"], workspace=st["workspace"])
+        return st["c"]
+    if e == "swiglu":
+        el.epic_gemm_fp8(el.GEMM_SWIGLU, *ab, act=st["act"], workspace=st["workspace"])
+        return st["act"]
+    el.epic_gemm_fp8(el.GEMM_SWIGLU_FP8, *ab, act=st["act"], act_scale=st["act_scale"], workspace=st["workspace"])
+    return {"q": _e4m3(st["act"]), "scale": _row_scales(st["act_scale"], m)}
+
+
+def _row_outputs(q, scale):
+    return {"q": q, "scale": scale.t().contiguous().view(torch.float8_e8m0fnu)}
+
+
+def run(st):
+    if own:
+        return _run_own(st)
+    case = st["case"]
+    if case["what"] == "quant":
+        q, scale = _to_fp8(st["x"].float(), case["block_rows"])
+        return _row_outputs(q, scale) if case["block_rows"] == 1 else {"q": q, "scale": scale.view(torch.float8_e8m0fnu)}
+    if case["what"] == "norm":
+        x = st["x"]
+        if case["adds"]:
+            total = st["add"][0] if case["adds"] == 1 else st["add"].sum(0)
+            x = x + total
+        out = _row_outputs(*_to_fp8(_normed(x, st["weight"])))
+        return {**out, "x": x} if case["adds"] else out
+    a = _wide(st["a"], st["a_scale"][:, :case["m"]].t(), 1, torch.float32)
+    y = a @ _wide(st["w"], st["w_scale"], 128, torch.float32).t()
+    e = case["epilogue"]
+    if e == "store":
+        return y
+    if e == "residual":
+        st["c"] += y
+        return st["c"]
+    act = _swiglu(y)
+    return act.to(torch.bfloat16) if e == "swiglu" else _row_outputs(*_to_fp8(act))
+
+
+# ---------------------------------------------------------------- the same in float64
+
+def _ideal(y, block_rows=1):
+    """The quantised form of y without its last rounding: values over the scale, and the scale."""
+    t = _groups(y, block_rows)
+    scale = torch.exp2(t.to(torch.float64))
+    return {"q": _scaled(y, t, block_rows), "scale": scale.t().contiguous() if block_rows == 1 else scale}
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    if case["what"] == "quant":
+        return _ideal(st["x"].double(), case["block_rows"])
+    if case["what"] == "norm":
+        x = st["x"].double()
+        if case["adds"]:
+            x = x + st["add"].double().sum(0)
+        out = _ideal(_normed(x, st["weight"]))
+        return {**out, "x": x} if case["adds"] else out
+    a = _wide(st["a"], st["a_scale"][:, :case["m"]].t(), 1, torch.float64)
+    y = a @ _wide(st["w"], st["w_scale"], 128, torch.float64).t()
+    e = case["epilogue"]
+    if e == "store":
+        return y
+    if e == "residual":
+        return st["c"].double() + y
+    act = _swiglu(y)
+    return act if e == "swiglu" else _ideal(act)
