@@ -5,8 +5,9 @@ power-of-two scale (e8m0) for each 128 consecutive values of a row of activation
 each 128 x 128 block of weights.  Three operators make such a layer:
 
     quant  rows or weights in bf16 -> e4m3 and scales             epic_quant_fp8
-    norm   residual stream + partial products -> RMSNorm -> e4m3  epic_rmsnorm_fp8
-    gemm   e4m3 x e4m3 product with its epilogues                 epic_gemm_fp8
+    norm   residual stream + a product -> RMSNorm -> e4m3         epic_rmsnorm_fp8
+    gemm   e4m3 x e4m3 product, to bf16, through SwiGLU, or that  epic_gemm_fp8
+           rounded to e4m3 again
 
     own                 False: plain torch; True: the library's kernels
     listed()            the named cases
@@ -16,7 +17,9 @@ each 128 x 128 block of weights.  Three operators make such a layer:
     work(case)          bytes and operations the pass cannot do without
     exact(case, seed)   the same outputs from the definition in float64
 
-Scales are bytes of e8m0 (2 ** (byte - 127)).  Scales of m rows are laid out
+Products leave in bf16 or e4m3: their sums are kept in 32 bits, but the matrix cores' 8-bit
+dot products of eight carry about 13 bits below the largest of the eight.  Scales are
+bytes of e8m0 (2 ** (byte - 127)).  Scales of m rows are laid out
 [k / 128][m rounded up to 4]: a group of all rows is contiguous.
 """
 import math
@@ -38,8 +41,8 @@ def _quant(name, m, k, block_rows=1):
     return {"name": name, "what": "quant", "m": m, "k": k, "block_rows": block_rows}
 
 
-def _norm(name, m, k, adds):
-    return {"name": name, "what": "norm", "m": m, "k": k, "adds": adds}
+def _norm(name, m, k, delta=True):
+    return {"name": name, "what": "norm", "m": m, "k": k, "delta": delta}
 
 
 def _gemm(name, epilogue, m, shape):
@@ -54,20 +57,20 @@ def listed():
         _quant("quant_compile", ROWS_COMPILE, 4096),
         # gate|up weights of a layer, laid out once when the model is loaded
         _quant("quant_weights_gate_up", *GATE_UP, block_rows=128),
-        # one request decoding: the stream plus one partial product
-        _norm("norm_decode1", 1, 4096, 1),
-        # a link step, its output projection left in two parts of k
-        _norm("norm_link736_two", ROWS_LINK, 4096, 2),
+        # one request decoding: the stream plus the output projection's result
+        _norm("norm_decode1", 1, 4096),
+        # a link step: the first norm of a call, whose stream is complete
+        _norm("norm_link736_first", ROWS_LINK, 4096, delta=False),
         # a compile step of a wide model
-        _norm("norm_compile8192", ROWS_COMPILE, 8192, 1),
+        _norm("norm_compile8192", ROWS_COMPILE, 8192),
         # one request decoding: q|k|v
-        _gemm("gemm_decode1_qkv", "store", 1, QKV),
-        # a batch of 32 decoding: down projection onto the stream
-        _gemm("gemm_decode32_down", "residual", 32, DOWN),
+        _gemm("gemm_decode1_qkv", "bf16", 1, QKV),
+        # a batch of 32 decoding: down projection
+        _gemm("gemm_decode32_down", "bf16", 32, DOWN),
         # a batch of 100: gate|up to bf16
         _gemm("gemm_batch100_gate_up", "swiglu", 100, GATE_UP),
         # a ragged row count between decode and link
-        _gemm("gemm_rows501_out", "store", 501, OUT),
+        _gemm("gemm_rows501_out", "bf16", 501, OUT),
         # a link step: gate|up, its result quantised for the down projection
         _gemm("gemm_link736_gate_up", "swiglu_fp8", ROWS_LINK, GATE_UP),
         # a compile step: gate|up, the largest product
@@ -86,10 +89,10 @@ def draw(rng):
         k = _log(rng, 128, 14336, 128)
         return {"what": what, "m": m, "k": k, "block_rows": rng.choice([1, 1, 128])}
     if what == "norm":
-        return {"what": what, "m": m, "k": _log(rng, 256, 8192, 128), "adds": rng.randrange(4)}
+        return {"what": what, "m": m, "k": _log(rng, 256, 8192, 128), "delta": rng.random() < 0.7}
     n, k = _log(rng, 512, 28672, 256), _log(rng, 256, 14336, 128)
     m = max(1, min(m, MOST // (n * k)))
-    return {"what": what, "epilogue": rng.choice(["store", "residual", "swiglu", "swiglu_fp8"]), "m": m, "n": n, "k": k}
+    return {"what": what, "epilogue": rng.choice(["bf16", "bf16", "swiglu", "swiglu_fp8"]), "m": m, "n": n, "k": k}
 
 
 def work(case):
@@ -99,10 +102,10 @@ def work(case):
         scales = -(-m // case["block_rows"]) * (k // GROUP)
         return {"bytes": 3 * m * k + scales, "flops": 3.0 * m * k}
     if case["what"] == "norm":
-        stream = 8 if case["adds"] else 4                     # the stream is written back where it changes
-        return {"bytes": m * k * (stream + 4 * case["adds"] + 1) + groups + 2 * k, "flops": (6.0 + case["adds"]) * m * k}
+        stream = 4 + 2 + 4 if case["delta"] else 4            # the stream is written back where it changes
+        return {"bytes": m * k * (stream + 1) + groups + 2 * k, "flops": (7.0 if case["delta"] else 6.0) * m * k}
     n = case["n"]
-    out = {"store": 4 * m * n, "residual": 8 * m * n, "swiglu": m * n, "swiglu_fp8": m * (n // 2) + m * (n // 2 // GROUP)}
+    out = {"bf16": 2 * m * n, "swiglu": m * n, "swiglu_fp8": m * (n // 2) + m * (n // 2 // GROUP)}
     blocks = (n // GROUP) * (k // GROUP)
     return {"bytes": m * k + groups + n * k + blocks + out[case["epilogue"]], "flops": 2.0 * m * n * k}
 
@@ -197,9 +200,10 @@ def prepare(case, seed):
         return st
     if case["what"] == "norm":
         st["x"] = _activations(gen, m, k)
-        st["add"] = torch.empty(case["adds"], m, k, device="cuda").normal_(generator=gen) if case["adds"] else None
+        delta = torch.empty(m, k, device="cuda").normal_(generator=gen).to(torch.bfloat16)
+        st["delta"] = delta if case["delta"] else None
         st["weight"] = (1.0 + 0.1 * torch.empty(k, device="cuda").normal_(generator=gen)).to(torch.bfloat16)
-        st["sum"] = empty(m, k, dtype=torch.float32) if case["adds"] else None
+        st["sum"] = empty(m, k, dtype=torch.float32) if case["delta"] else None
         st["q"], st["scale"] = empty(m, k), empty(k // GROUP, -(-m // 4) * 4)
         return st
     n = case["n"]
@@ -207,14 +211,13 @@ def prepare(case, seed):
     w, st["w_scale"] = _to_fp8(torch.empty(n, k, device="cuda").normal_(generator=gen) * (0.5 / math.sqrt(k)), 128)
     st["a"], st["w"], st["a_scale"] = a, w, _padded(sa)
     e = case["epilogue"]
-    if e == "store":
-        st["c"] = empty(m, n, dtype=torch.float32)
-    elif e == "residual":
-        st["c"] = torch.empty(m, n, device="cuda").normal_(generator=gen)
+    st["out_scale"] = None
+    if e == "bf16":
+        st["out"] = empty(m, n, dtype=torch.bfloat16)
     elif e == "swiglu":
-        st["act"] = empty(m, n // 2, dtype=torch.bfloat16)
+        st["out"] = empty(m, n // 2, dtype=torch.bfloat16)
     else:
-        st["act"], st["act_scale"] = empty(m, n // 2), empty(n // 2 // GROUP, -(-m // 4) * 4)
+        st["out"], st["out_scale"] = empty(m, n // 2), empty(n // 2 // GROUP, -(-m // 4) * 4)
     # 64 MB of partial sums and what else the library's products need
     st["workspace"] = empty(72 << 20)
     return st
@@ -241,21 +244,15 @@ def _run_own(st):
             return {"q": _e4m3(st["q"]), "scale": _row_scales(st["scale"], m)}
         return {"q": _e4m3(st["q"]), "scale": st["scale"].view(torch.float8_e8m0fnu)}
     if case["what"] == "norm":
-        el.epic_rmsnorm_fp8(st["x"], st["weight"], EPS, st["q"], st["scale"], add=st["add"], x_out=st["sum"])
+        el.epic_rmsnorm_fp8(st["x"], st["weight"], EPS, st["q"], st["scale"], delta=st["delta"], x_out=st["sum"])
         out = {"q": _e4m3(st["q"]), "scale": _row_scales(st["scale"], m)}
-        return {**out, "x": st["sum"]} if case["adds"] else out
-    e, ab = case["epilogue"], (st["a"], st["a_scale"], st["w"], st["w_scale"])
-    if e == "store":
-        el.epic_gemm_fp8(el.GEMM_STORE, *ab, c=st["c"], workspace=st["workspace"])
-        return st["c"]
-    if e == "residual":
-        el.epic_gemm_fp8(el.GEMM_RESIDUAL, *ab, c=st["c"], workspace=st["workspace"])
-        return st["c"]
-    if e == "swiglu":
-        el.epic_gemm_fp8(el.GEMM_SWIGLU, *ab, act=st["act"], workspace=st["workspace"])
-        return st["act"]
-    el.epic_gemm_fp8(el.GEMM_SWIGLU_FP8, *ab, act=st["act"], act_scale=st["act_scale"], workspace=st["workspace"])
-    return {"q": _e4m3(st["act"]), "scale": _row_scales(st["act_scale"], m)}
+        return {**out, "x": st["sum"]} if case["delta"] else out
+    epilogue = {"bf16": el.FP8_BF16, "swiglu": el.FP8_SWIGLU, "swiglu_fp8": el.FP8_SWIGLU_FP8}[case["epilogue"]]
+    el.epic_gemm_fp8(epilogue, st["a"], st["a_scale"], st["w"], st["w_scale"], st["out"], out_scale=st["out_scale"],
+                     workspace=st["workspace"])
+    if st["out_scale"] is None:
+        return st["out"]
+    return {"q": _e4m3(st["out"]), "scale": _row_scales(st["out_scale"], m)}
 
 
 def _row_outputs(q, scale):
@@ -270,20 +267,14 @@ def run(st):
         q, scale = _to_fp8(st["x"].float(), case["block_rows"])
         return _row_outputs(q, scale) if case["block_rows"] == 1 else {"q": q, "scale": scale.view(torch.float8_e8m0fnu)}
     if case["what"] == "norm":
-        x = st["x"]
-        if case["adds"]:
-            total = st["add"][0] if case["adds"] == 1 else st["add"].sum(0)
-            x = x + total
+        x = st["x"] + st["delta"].float() if case["delta"] else st["x"]
         out = _row_outputs(*_to_fp8(_normed(x, st["weight"])))
-        return {**out, "x": x} if case["adds"] else out
+        return {**out, "x": x} if case["delta"] else out
     a = _wide(st["a"], st["a_scale"][:, :case["m"]].t(), 1, torch.float32)
     y = a @ _wide(st["w"], st["w_scale"], 128, torch.float32).t()
     e = case["epilogue"]
-    if e == "store":
-        return y
-    if e == "residual":
-        st["c"] += y
-        return st["c"]
+    if e == "bf16":
+        return y.to(torch.bfloat16)
     act = _swiglu(y)
     return act.to(torch.bfloat16) if e == "swiglu" else _row_outputs(*_to_fp8(act))
 
@@ -303,16 +294,14 @@ def exact(case, seed):
         return _ideal(st["x"].double(), case["block_rows"])
     if case["what"] == "norm":
         x = st["x"].double()
-        if case["adds"]:
-            x = x + st["add"].double().sum(0)
+        if case["delta"]:
+            x = x + st["delta"].double()
         out = _ideal(_normed(x, st["weight"]))
-        return {**out, "x": x} if case["adds"] else out
+        return {**out, "x": x} if case["delta"] else out
     a = _wide(st["a"], st["a_scale"][:, :case["m"]].t(), 1, torch.float64)
     y = a @ _wide(st["w"], st["w_scale"], 128, torch.float64).t()
     e = case["epilogue"]
-    if e == "store":
+    if e == "bf16":
         return y
-    if e == "residual":
-        return st["c"].double() + y
     act = _swiglu(y)
     return act if e == "swiglu" else _ideal(act)
