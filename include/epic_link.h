@@ -379,6 +379,55 @@ size_t epic_gemm_workspace_bytes(void);
 epic_status epic_gemm(int32_t epilogue, const uint16_t* a, const uint16_t* w, int32_t m, int32_t n, int32_t k,
                       float* c, uint16_t* act, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------- 8-bit projections */
+
+/* The decoder layer's projections on 8-bit operands: e4m3 values (1-4-3 bits, largest 448,
+ * no infinities) with one power-of-two scale per 128 values, an e8m0 byte (2^(byte - 127)),
+ * which the matrix instruction applies.  For a group of values y, t is the smallest
+ * integer in [-127, 127] with max |y| <= 448 * 2^t, over the finite y (t = 0 if all of them
+ * are 0); the scale's byte is t + 127 and the values are y / 2^t rounded once, to nearest
+ * even.  Infinities and NaN become NaN.
+ *  - Rows: values [m][k], a scale per 128 consecutive values of a row, laid out
+ *    [k / 128][m rounded up to 4] (a group's scales of all rows are contiguous; the padding
+ *    is never used and may be written).  epic_fp8_scale_bytes(m, k) bytes (0 if m < 0 or
+ *    k is not a positive multiple of 128).
+ *  - Weights: values [n][k] ([out][in]), a scale per 128 x 128 block, [ceil(n / 128)][k / 128].
+ * All of it contiguous device memory, k % 128 == 0; values 16-byte, row scales 4-byte
+ * aligned.  Every call is deterministic: sums have a fixed order for given sizes. */
+size_t epic_fp8_scale_bytes(int32_t m, int32_t k);
+
+/* Round x (bf16 [m][k]) to q and scale: as rows (block_rows == 1), or as weights
+ * (block_rows == 128; the last block may have fewer rows). */
+epic_status epic_quant_fp8(const uint16_t* x, int32_t m, int32_t k, int32_t block_rows, uint8_t* q, uint8_t* scale,
+                           void* stream);
+
+/* The residual stream's addition, RMSNorm and rounding in one pass:
+ *   s = x + delta;   y = s / sqrt(mean(s^2) + eps) * weight;   y -> q, scale (rows)
+ * x, x_out: fp32 [m][hidden]; delta: bf16 [m][hidden] (a product of epic_gemm_fp8, say), or
+ * NULL for none; weight: bf16 [hidden].  x_out receives s unless it is NULL; it may be x,
+ * and else overlaps nothing.  Sums and statistics are fp32.  hidden % 128 == 0, at most
+ * 32768. */
+epic_status epic_rmsnorm_fp8(const float* x, const uint16_t* delta, const uint16_t* weight, int32_t m, int32_t hidden,
+                             float eps, float* x_out, uint8_t* q, uint8_t* scale, void* stream);
+
+/* The projection GEMM on 8-bit rows a and weights w:
+ *   C[i][j] = sum over blocks b of 2^(a_scale[i][b] + w_scale[j / 128][b]) sum over t in b of a[i][t] w[j][t]
+ * epilogue EPIC_FP8_BF16:       out bf16 [m][n] = C
+ *          EPIC_FP8_SWIGLU:     out bf16 [m][n/2] = silu(C[i][j]) C[i][j + n/2]
+ *          EPIC_FP8_SWIGLU_FP8: the same as rows, out e4m3 [m][n/2] and out_scale (else unused)
+ * Sums are fp32, but the matrix cores drop what lies more than 13 bits below the largest
+ * product of eight neighbouring t (all with t / 8 alike): 1.5e-5 to 4e-5 of a result, below
+ * what its rounding to bf16 or e4m3 costs.
+ * Shapes: m >= 0, k % 128 == 0, n % 128 == 0 (SwiGLU: n % 256 == 0), and with m rounded up
+ * to a multiple of 256 every operand and a bf16 [m][n] below 2^31 bytes; else
+ * EPIC_ERR_UNSUPPORTED.  workspace: epic_gemm_fp8_workspace_bytes() bytes, 256-byte
+ * aligned, for partial sums; calls in flight at the same time need separate ones. */
+typedef enum { EPIC_FP8_BF16 = 0, EPIC_FP8_SWIGLU = 1, EPIC_FP8_SWIGLU_FP8 = 2 } epic_fp8_epilogue;
+size_t epic_gemm_fp8_workspace_bytes(void);
+epic_status epic_gemm_fp8(int32_t epilogue, const uint8_t* a, const uint8_t* a_scale, const uint8_t* w,
+                          const uint8_t* w_scale, int32_t m, int32_t n, int32_t k, void* out, uint8_t* out_scale,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,418 @@
+// 8-bit GEMMs of more rows: C[M x N] = A[M x K] . W[N x K]^T on tiles of 256 or 128 rows x
+// 256 columns, one workgroup of four wavefronts per CU, epilogues fused.
+//
+// A stage is 128 of K, which are 128 bytes of a row, as 64 of K are in the bf16 kernel
+// (gemm_wide.hip), and the matrix cores take it in the same time with twice the products.
+// So the schedule is that kernel's: a wavefront owns TM/2 x 128 outputs in AGPRs, the
+// fragments of the next half stage are read and the loads of later stages issued between
+// the MFMAs of this one, and LDS is a ring of five half stages (one operand, 128 of K,
+// 32 KB each), of which a stage frees two: they take the W half of the stage after next
+// and the A half of the one after that.
+//
+// Scales: one per row and stage, applied by the matrix instruction.  A wavefront's rows
+// are dealt to its I row tiles in turn (tile i has rows I r + i), so the I scales of a
+// lane are neighbouring bytes of one load, and the instruction picks byte i.  The scale of
+// the columns' weight block is one byte per wavefront and stage (SwiGLU: of the gate's
+// and of the up block).  They are loaded into registers two stages ahead.
+//
+// With few tiles the same kernel runs equal parts of K of every tile, one workgroup each,
+// into fp32 planes that the consumer adds (stream_sum.h).
+//
+// Half-stage layout: rows of 128 bytes in groups of 8 (1 KB, one load instruction); the
+// eight 16-byte chunks of row r are XOR-swizzled by (r / 2) % 8, so the 16 lanes of each
+// ds_read_b128 group touch distinct banks.  For SwiGLU the W rows of a tile are gate and
+// up in turn, 32 rows each.  Rows past M and columns past N are read clamped and never
+// stored.
+#include <algorithm>
+#include <utility>
+
+#include "gemm8.h"
+#include "gemm8_device.h"
+#include "quant.h"
+#include "quant_device.h"
+
+namespace epic {
+
+namespace {
+
+constexpr int kBK = 128, kTN = 256;
+constexpr int kMaxWorkers = 256;
+constexpr int kPlanesOut = 3;  // epilogue: fp32 partial sums into planes
+
+struct WidePlan8 {
+  int m_tiles, n_tiles, tiles;
+  int ks;                      // K stages per tile
+  int gm;                      // row tiles per ordering group
+  int G;                       // workgroups, a multiple of 8
+  int parts;                   // kPlanesOut: equal parts of K per tile, a workgroup each
+};
+
+__device__ __forceinline__ float silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(-x * kLog2e)); }
+
+template <class F, int... M>
+__device__ __forceinline__ void for_each_index(const F& f, std::integer_sequence<int, M...>) {
+  (f(std::integral_constant<int, M>{}), ...);
+}
+
+template <int EPI, int TM>
+__global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePlan8 p) {
+  constexpr int I = TM / 64, J = 4;                     // 32 x 32 MFMA tiles per wavefront
+  constexpr int NLA = TM / 32, NLB = kTN / 32;          // 1 KB row groups per wavefront and stage
+  constexpr int SLOTS = 5, SLOT = kTN * 128;            // half stages (one operand, 128 of K)
+  constexpr bool SPLIT = EPI == kPlanesOut;
+  constexpr bool GLU = EPI == kGluOut || EPI == kGluQuantOut;
+  __shared__ __attribute__((aligned(1024))) char lds[SLOTS][SLOT];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wv >> 1, wn = wv & 1;
+  const int w = blockIdx.x;
+  const int wr = (w % 8) * (p.G / 8) + w / 8;           // XCD-contiguous worker index (G % 8 == 0)
+  // This worker's K stages: whole tiles wr, wr + G, ..; with planes part wr / tiles of
+  // tile wr % tiles, so that the workgroups of an XCD are at the same K.
+  if (wr >= (SPLIT ? p.parts * p.tiles : p.tiles)) return;
+  const int part = SPLIT ? wr / p.tiles : 0;
+  const int tile0 = SPLIT ? wr - part * p.tiles : wr;
+  const int kt0 = SPLIT ? part * p.ks / p.parts : 0;
+  const int n_units = SPLIT ? (part + 1) * p.ks / p.parts - kt0 : (p.tiles - wr + p.G - 1) / p.G * p.ks;
+
+  auto tile_mn = [&](int t, int& mt, int& nt) __attribute__((always_inline)) {
+    if constexpr (SPLIT) {
+      nt = t / p.m_tiles;
+      mt = t - nt * p.m_tiles;
+      return;
+    }
+    const int per_group = p.gm * p.n_tiles;
+    const int grp = t / per_group;
+    const int first = grp * p.gm;
+    const int gsz = min(p.m_tiles - first, p.gm);
+    const int r = t - grp * per_group;
+    mt = first + r % gsz;
+    nt = r / gsz;
+  };
+
+  // ---- loads: this wavefront stages A row groups NLA wv .., W row groups NLB wv ..
+  const int lrow = lane >> 3;
+  const int ffn = g.N / 2, ld = (g.M + 3) & ~3;
+  const __amdgpu_buffer_rsrc_t rsa =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.A), 0, g.M * g.K, kBufWord3);
+  const __amdgpu_buffer_rsrc_t rsb =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.W), 0, g.N * g.K, kBufWord3);
+  const __amdgpu_buffer_rsrc_t rsc =                    // scales; past the end (rows past M only) they read as 0
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.sa), 0, p.ks * ld, kBufWord3);
+  const __amdgpu_buffer_rsrc_t rsd =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.sw), 0, (g.N >> 7) * p.ks, kBufWord3);
+  int va[NLA], vb[NLB], vsa, vsw, vsu;
+  struct Cursor {
+    int tile, kt, slot, left;
+  };
+  // next half stages (ca, cb) and scales (cs) to load
+  Cursor ca{tile0, kt0, 0, n_units}, cb{tile0, kt0, 1, n_units}, cs{tile0, kt0, 0, n_units};
+  auto setup_a = [&]() __attribute__((always_inline)) {
+    int mt, nt;
+    tile_mn(ca.tile, mt, nt);
+#pragma unroll
+    for (int i = 0; i < NLA; ++i) {
+      const int row = (NLA * wv + i) * 8 + lrow;        // in LDS: row tile after row tile of a wavefront's
+      const int in = row % (TM / 2), gr = row - in + in % 32 * I + in / 32;
+      va[i] = min(mt * TM + gr, g.M - 1) * g.K + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    }
+  };
+  auto setup_b = [&]() __attribute__((always_inline)) {
+    int mt, nt;
+    tile_mn(cb.tile, mt, nt);
+#pragma unroll
+    for (int i = 0; i < NLB; ++i) {
+      const int row = (NLB * wv + i) * 8 + lrow;
+      const int gr = GLU ? ((row >> 5) & 1) * ffn + nt * (kTN / 2) + (row >> 6) * 32 + (row & 31)
+                         : min(nt * kTN + row, g.N - 1);
+      vb[i] = gr * g.K + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    }
+  };
+  auto setup_s = [&]() __attribute__((always_inline)) {
+    int mt, nt;
+    tile_mn(cs.tile, mt, nt);
+    vsa = mt * TM + wm * (TM / 2) + (lane & 31) * I;
+    const int nb = GLU ? nt : min(nt * 2 + wn, (g.N >> 7) - 1);
+    vsw = nb * p.ks;
+    vsu = (nb + (ffn >> 7)) * p.ks;
+  };
+  setup_a();
+  setup_b();
+  setup_s();
+  auto bump = [&](int slot) __attribute__((always_inline)) { return slot >= SLOTS - 2 ? slot + 2 - SLOTS : slot + 2; };
+  // to the next half stage; past the last, that one again.  True: another tile
+  auto advance = [&](Cursor& c) __attribute__((always_inline)) {
+    c.slot = bump(c.slot);
+    if (--c.left <= 0) return false;
+    if (++c.kt < p.ks) return false;
+    c.tile += p.G;
+    c.kt = 0;
+    return true;
+  };
+  auto dma_a = [&](int i) __attribute__((always_inline)) {
+    dma16(rsa, lds[ca.slot] + (NLA * wv + i) * 1024, va[i], ca.kt * kBK);
+    if (i == NLA - 1 && advance(ca)) setup_a();
+  };
+  auto dma_b = [&](int i) __attribute__((always_inline)) {
+    dma16(rsb, lds[cb.slot] + (NLB * wv + i) * 1024, vb[i], cb.kt * kBK);
+    if (i == NLB - 1 && advance(cb)) setup_b();
+  };
+  struct Scales {
+    int a, w, u;                                        // I rows of a lane; the columns' block (gate, up)
+  } sc0, sc1, sc2;                                      // of this stage, the next, and the last ones loaded
+  auto load_scales = [&](Scales& s) __attribute__((always_inline)) {
+    if constexpr (I == 4) s.a = int(__builtin_amdgcn_raw_buffer_load_b32(rsc, vsa, cs.kt * ld, 0));
+    else s.a = int(__builtin_amdgcn_raw_buffer_load_b16(rsc, vsa, cs.kt * ld, 0));
+    s.w = int(__builtin_amdgcn_raw_buffer_load_b8(rsd, vsw, cs.kt, 0));
+    if constexpr (GLU) s.u = int(__builtin_amdgcn_raw_buffer_load_b8(rsd, vsu, cs.kt, 0));
+    if (advance(cs)) setup_s();
+  };
+
+  // ---- fragments
+  const int half = lane >> 5, lsw = (lane >> 1) & 7;
+  const int la = wm * (TM / 2) * 128 + (lane & 31) * 128;
+  const int lb = wn * 128 * 128 + (lane & 31) * 128;
+  int sw[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) sw[s] = ((4 * s + 2 * half) ^ lsw) * 16;
+  struct Frags {
+    i32x8 a[I], b[J];
+  } f0, f1;
+  auto read1 = [&](Frags& f, const char* sa, const char* sb, int s, int i) __attribute__((always_inline)) {   // a0 b0 .. b3 a1 ..
+    if (i == 0) f.a[0] = read32(sa + la, sw[s], sw[s] ^ 16);
+    else if (i <= J) f.b[i <= J && i > 0 ? i - 1 : 0] = read32(sb + lb + (i - 1) * 4096, sw[s], sw[s] ^ 16);
+    else f.a[i > J ? i - J : 0] = read32(sa + la + (i - J) * 4096, sw[s], sw[s] ^ 16);
+  };
+
+  f32x16 acc[I][J];
+  constexpr int NM = I * J;
+  auto mma = [&](const Frags& f, const Scales& s, auto m) __attribute__((always_inline)) {
+    constexpr int i = decltype(m)::value / J, j = decltype(m)::value % J;
+    const int b = GLU && j % 2 ? s.u : s.w;
+    acc[i][j] = mfma8<0, i>(f.b[j], f.a[i], acc[i][j], b, s.a);
+    __asm__ volatile("" : "+a"(acc[i][j]));             // here: the compiler sinks MFMAs past the branches that follow
+  };
+  // half a stage: its MFMAs on f; the fragments of the next half (half s of the stage at
+  // sa, sb) read into fn beside the first of them, and one operand's loads (W: 0, A: 1)
+  auto slice = [&](const Frags& f, Frags& fn, const char* sa, const char* sb, int s, auto load) __attribute__((always_inline)) {
+    constexpr int L = decltype(load)::value;
+    constexpr int NL = L == 0 ? NLB : NLA;
+    auto step = [&](auto mi) __attribute__((always_inline)) {
+      constexpr int m = decltype(mi)::value;
+      mma(f, sc0, mi);
+      if constexpr (m < I + J) read1(fn, sa, sb, s, m);
+      // few row tiles: the rest of the fragments beside the last MFMA
+      if constexpr (m == NM - 1) {
+#pragma unroll
+        for (int r = NM; r < I + J; ++r) read1(fn, sa, sb, s, r);
+      }
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (m == i * NM / NL) {
+          if constexpr (L == 0) dma_b(i);
+          else dma_a(i);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    for_each_index(step, std::make_integer_sequence<int, NM>{});
+  };
+  // the next stage's loads landed, everyone's (the A loads past it stay in flight), and
+  // this stage is read
+  auto sync = [&]() __attribute__((always_inline)) {
+    wait_vmem<NLA>();
+    barrier_lds();
+  };
+
+  load_scales(sc0);
+#pragma unroll
+  for (int i = 0; i < NLA; ++i) dma_a(i);
+#pragma unroll
+  for (int i = 0; i < NLB; ++i) dma_b(i);
+  load_scales(sc2);
+#pragma unroll
+  for (int i = 0; i < NLA; ++i) dma_a(i);
+#pragma unroll
+  for (int i = 0; i < NLB; ++i) dma_b(i);
+  wait_vmem<NLA + NLB + (GLU ? 3 : 2)>();               // stage 0
+  __asm__ volatile("s_barrier" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < I + J; ++i) read1(f0, lds[0], lds[1], 0, i);
+
+  int sa = 0, sb = 1;
+  for (int tile = tile0, left = n_units; left > 0;) {
+    const int n = SPLIT ? n_units : p.ks;
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j) acc[i][j] = f32x16{};
+    for (int kt = 0; kt < n; ++kt) {
+      slice(f0, f1, lds[sa], lds[sb], 1, std::integral_constant<int, 1>{});
+      sync();
+      sa = bump(sa);
+      sb = bump(sb);
+      sc1 = sc2;
+      load_scales(sc2);
+      slice(f1, f0, lds[sa], lds[sb], 0, std::integral_constant<int, 0>{});
+      sc0 = sc1;
+    }
+    // ---- epilogue: lane l has row I (l % 32) + i of the wavefront's in row tile i, and of
+    // column tile j the columns 8 q + 4 (l / 32) + 0 .. 3 in registers 4 q .. 4 q + 3.  Results go
+    // through LDS, so that a store instruction writes runs of 256 bytes (rows past M fall
+    // outside the descriptors): through the half stage that the next A loads will take,
+    // which held this stage's W and has been read by everyone.
+    int mt, nt;
+    tile_mn(tile, mt, nt);
+    const int mw = mt * TM + wm * (TM / 2);             // the wavefront's first row
+    char* room = lds[ca.slot];
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    if constexpr (GLU) {
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+#pragma unroll
+        for (int j = 0; j < J; j += 2) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = silu(acc[i][j][r]) * acc[i][j + 1][r];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    if constexpr (EPI == kGluQuantOut) {
+      // a row's other columns are in lane l ^ 32 and in the wavefront with the other wn: the
+      // room takes first the maxima, then the tile
+      uint32_t top[I];
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        top[i] = 0;
+#pragma unroll
+        for (int j = 0; j < J; j += 2)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) top[i] = max(top[i], finite_abs(acc[i][j][r]));
+        top[i] = max(top[i], uint32_t(__shfl_xor(int(top[i]), 32)));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      uint32_t* tops = reinterpret_cast<uint32_t*>(room);   // [wm][wn][i][32]
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+        if (half == 0) tops[(wv * I + i) * 32 + (lane & 31)] = top[i];
+      barrier_lds();
+      int byte[I];
+#pragma unroll
+      for (int i = 0; i < I; ++i) byte[i] = scale_byte(max(top[i], tops[((wv ^ 1) * I + i) * 32 + (lane & 31)]));
+      barrier_lds();                                    // the maxima are read
+      const int row0 = wm * (TM / 2) + (lane & 31) * I;  // of the tile
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+#pragma unroll
+        for (int j = 0; j < J; j += 2)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int row = row0 + i, c = wn * 64 + j * 16 + q * 8 + half * 4;
+            *reinterpret_cast<uint32_t*>(room + row * 128 + ((c >> 4) ^ ((row / I) & 7)) * 16 + (c & 15)) =
+                pack_e4m3x4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3], byte[i]);
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const int first = mw + (lane & 31) * I;
+      if (wn == 0 && half == 0 && first < g.M) {        // I neighbouring rows; those past M are padding
+        uint8_t* to = g.out_scale + size_t(nt) * ld + first;
+        if constexpr (I == 4) *reinterpret_cast<uint32_t*>(to) = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
+        else *reinterpret_cast<uint16_t*>(to) = uint16_t(byte[0] | byte[1] << 8);
+      }
+      barrier_lds();
+      const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(g.out, 0, g.M * ffn, kBufWord3);
+#pragma unroll
+      for (int x = 0; x < TM / 32; ++x) {               // eight lanes a row
+        const int row = x * 32 + (tid >> 3), c = tid & 7;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(room + row * 128 + (c ^ ((row / I) & 7)) * 16);
+        __builtin_amdgcn_raw_buffer_store_b128(v, ro, (mt * TM + row) * ffn + nt * (kTN / 2) + c * 16, 0, 0);
+      }
+    } else {
+      // a wavefront's own 8 KB of the room: 32 rows of 256 bytes at a time (bf16: all the
+      // columns of a row tile, after SwiGLU half as many; fp32: half of them)
+      char* mine = room + wv * 8192;
+      constexpr int OUT = SPLIT ? 4 : 2;                // bytes of a result
+      constexpr int JS = SPLIT ? 2 : 4;                 // column tiles per pass
+      constexpr int W = GLU ? 128 : 256;                // bytes of a row per pass
+      const int cols = GLU ? ffn : g.N;
+      const int n0 = GLU ? nt * (kTN / 2) + wn * 64 : nt * kTN + wn * 128;
+      char* out = reinterpret_cast<char*>(SPLIT ? static_cast<void*>(g.partial + size_t(part) * g.M * g.N) : g.out);
+      // N % 128 == 0: all of the wavefront's columns, or none
+      const __amdgpu_buffer_rsrc_t ro =
+          __builtin_amdgcn_make_buffer_rsrc(out, 0, n0 < cols ? g.M * cols * OUT : 0, kBufWord3);
+      const int row = lane & 31;
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j0 = 0; j0 < J; j0 += JS) {
+#pragma unroll
+          for (int j = 0; j < JS; j += GLU ? 2 : 1)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const f32x16& v = acc[i][j0 + j];
+              const int c = ((GLU ? j / 2 : j) * 32 + q * 8 + half * 4) * OUT;   // byte of the row
+              char* to = mine + row * W + ((c >> 4) ^ (row & (W / 16 - 1))) * 16 + (c & 15);
+              if constexpr (SPLIT)
+                *reinterpret_cast<float4*>(to) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+              else
+                *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(v[4 * q], v[4 * q + 1]),
+                                                           pack_bf16x2(v[4 * q + 2], v[4 * q + 3]));
+            }
+          constexpr int LR = W / 16;                    // lanes a row
+#pragma unroll
+          for (int x = 0; x < 32 * LR / 64; ++x) {
+            const int r = x * (64 / LR) + lane / LR, c = lane % LR;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * W + (c ^ (r & (LR - 1))) * 16);
+            __builtin_amdgcn_raw_buffer_store_b128(v, ro, ((mw + r * I + i) * cols + n0 + j0 * 32) * OUT + c * 16, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    barrier_lds();                                      // the room is read: the next A loads may land
+    left -= n;
+    tile += p.G;
+  }
+  wait_vmem<0>();                                       // no load may land in LDS after the workgroup ends
+}
+
+int cdiv(int a, int b) { return (a + b - 1) / b; }
+
+WidePlan8 plan_of(const Gemm8Args& g, int tm) {
+  WidePlan8 p{};
+  p.m_tiles = cdiv(g.M, tm);
+  p.n_tiles = cdiv(g.N, kTN);
+  p.tiles = p.m_tiles * p.n_tiles;
+  p.ks = g.K / kBK;
+  p.gm = std::min(p.m_tiles, 8);
+  p.parts = 1;
+  p.G = cdiv(cdiv(p.tiles, cdiv(p.tiles, kMaxWorkers)), 8) * 8;
+  return p;
+}
+
+template <int TM>
+void launch_wide_tm(const Gemm8Args& g, int epi, hipStream_t stream) {
+  const WidePlan8 p = plan_of(g, TM);
+  if (epi == kBf16Out) gemm8_wide_kernel<kBf16Out, TM><<<p.G, 256, 0, stream>>>(g, p);
+  else if (epi == kGluOut) gemm8_wide_kernel<kGluOut, TM><<<p.G, 256, 0, stream>>>(g, p);
+  else gemm8_wide_kernel<kGluQuantOut, TM><<<p.G, 256, 0, stream>>>(g, p);
+}
+
+}  // namespace
+
+void launch_gemm8_wide(const Gemm8Args& g, int epi, int tm, hipStream_t stream) {
+  if (tm == 256) launch_wide_tm<256>(g, epi, stream);
+  else launch_wide_tm<128>(g, epi, stream);
+}
+
+StreamSum launch_gemm8_split(const Gemm8Args& g, int tm, int parts, hipStream_t stream) {
+  WidePlan8 p = plan_of(g, tm);
+  p.parts = parts;
+  p.G = cdiv(p.tiles * parts, 8) * 8;
+  StreamSum s{};
+  s.partial = g.partial;
+  s.M = g.M, s.N = g.N, s.fixed = parts;
+  if (tm == 256) gemm8_wide_kernel<kPlanesOut, 256><<<p.G, 256, 0, stream>>>(g, p);
+  else gemm8_wide_kernel<kPlanesOut, 128><<<p.G, 256, 0, stream>>>(g, p);
+  return s;
+}
+
+}  // namespace epic

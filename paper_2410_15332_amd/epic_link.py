@@ -136,15 +136,29 @@ _gemm = _proto("epic_gemm", C.c_int,
                [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                 C.c_void_p, C.c_size_t, C.c_void_p])
 
+_fp8_scale_bytes = _proto("epic_fp8_scale_bytes", C.c_size_t, [C.c_int32, C.c_int32])
+_quant_fp8 = _proto("epic_quant_fp8", C.c_int,
+                    [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p])
+_rmsnorm_fp8 = _proto("epic_rmsnorm_fp8", C.c_int,
+                      [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_void_p,
+                       C.c_void_p, C.c_void_p])
+_gemm_fp8_ws = _proto("epic_gemm_fp8_workspace_bytes", C.c_size_t, [])
+_gemm_fp8 = _proto("epic_gemm_fp8", C.c_int,
+                   [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p])
+
 EXPORTED = ["epic_status_string", "epic_last_error", "epic_version", "epic_plan_sizes_get", "epic_plan_layout",
             "epic_plan_link", "epic_link_workspace_bytes", "epic_link_attention", "epic_set_profile_events",
             "epic_model_workspace_bytes", "epic_link_layer", "epic_link_model", "epic_gemm_workspace_bytes",
             "epic_gemm", "epic_plan_decode_sizes", "epic_plan_decode", "epic_plan_compile_sizes",
-            "epic_plan_compile", "epic_link_attention_noalloc"]
+            "epic_plan_compile", "epic_link_attention_noalloc", "epic_fp8_scale_bytes", "epic_quant_fp8",
+            "epic_rmsnorm_fp8", "epic_gemm_fp8_workspace_bytes", "epic_gemm_fp8"]
 
 NOALLOC_SCRATCH_BYTES = 96 << 20      # EPIC_NOALLOC_SCRATCH_BYTES
 
 GEMM_STORE, GEMM_RESIDUAL, GEMM_SWIGLU = 0, 1, 2
+FP8_BF16, FP8_SWIGLU, FP8_SWIGLU_FP8 = 0, 1, 2      # epilogues of epic_gemm_fp8
+FP8_GROUP = 128                       # values that share a scale
 
 
 def _check(st: int, where: str):
@@ -378,6 +392,99 @@ def epic_gemm(epilogue: int, a, w, c=None, act=None, workspace=None, stream=None
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_gemm(epilogue, _ptr(a), _ptr(w), m, n, k, _ptr(c), _ptr(act), _ptr(workspace), ws_bytes,
                  _stream(stream)), "epic_gemm")
+
+
+# ---------------------------------------------------------------- 8-bit projections
+
+def fp8_row_scale_shape(m: int, k: int):
+    """Shape of the scale bytes of m rows of k values."""
+    return k // FP8_GROUP, -(-m // 4) * 4
+
+
+def fp8_block_scale_shape(n: int, k: int):
+    """Shape of the scale bytes of n x k weights."""
+    return -(-n // FP8_GROUP), k // FP8_GROUP
+
+
+def _expect(name: str, t, shape, *dtypes):
+    """The 8-bit operators take packed tensors of the current device: others are refused."""
+    import torch
+
+    if t is None:
+        raise ValueError(f"{name} is missing")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {tuple(shape)} expected, got {tuple(t.shape)} with strides {t.stride()}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: {' or '.join(map(str, dtypes))} expected, got {t.dtype}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: a tensor of the current device expected, got {t.device}")
+
+
+def _bytes_of(kind: str):
+    import torch
+
+    return torch.uint8, getattr(torch, kind)
+
+
+def epic_fp8_scale_bytes(m: int, k: int) -> int:
+    return int(_fp8_scale_bytes(m, k))
+
+
+def epic_quant_fp8(x, q, scale, block_rows: int = 1, stream=None):
+    """Enqueue x bf16 [m, k] -> e4m3 values q [m, k] and e8m0 scales (see include/epic_link.h):
+    rows (block_rows 1, scale fp8_row_scale_shape(m, k)) or weights (128,
+    fp8_block_scale_shape(m, k)).  q and scale: uint8 or torch's 8-bit float types."""
+    import torch
+
+    m, k = x.shape
+    _expect("x", x, (m, k), torch.bfloat16)
+    _expect("q", q, (m, k), *_bytes_of("float8_e4m3fn"))
+    _expect("scale", scale, fp8_row_scale_shape(m, k) if block_rows == 1 else fp8_block_scale_shape(m, k),
+            *_bytes_of("float8_e8m0fnu"))
+    _check(_quant_fp8(_ptr(x), m, k, block_rows, _ptr(q), _ptr(scale), _stream(stream)), "epic_quant_fp8")
+
+
+def epic_rmsnorm_fp8(x, weight, eps: float, q, scale, delta=None, x_out=None, stream=None):
+    """Enqueue s = x + delta, x_out = s (x itself or None are fine) and RMSNorm(s) weight -> q, scale
+    as rows (see include/epic_link.h); x, x_out fp32, delta bf16 or None."""
+    import torch
+
+    m, hidden = x.shape
+    _expect("x", x, (m, hidden), torch.float32)
+    _expect("weight", weight, (hidden,), torch.bfloat16)
+    _expect("q", q, (m, hidden), *_bytes_of("float8_e4m3fn"))
+    _expect("scale", scale, fp8_row_scale_shape(m, hidden), *_bytes_of("float8_e8m0fnu"))
+    if delta is not None:
+        _expect("delta", delta, (m, hidden), torch.bfloat16)
+    if x_out is not None:
+        _expect("x_out", x_out, (m, hidden), torch.float32)
+    _check(_rmsnorm_fp8(_ptr(x), _ptr(delta), _ptr(weight), m, hidden, eps, _ptr(x_out), _ptr(q), _ptr(scale),
+                        _stream(stream)), "epic_rmsnorm_fp8")
+
+
+def epic_gemm_fp8_workspace_bytes() -> int:
+    return int(_gemm_fp8_ws())
+
+
+def epic_gemm_fp8(epilogue: int, a, a_scale, w, w_scale, out, out_scale=None, workspace=None, stream=None):
+    """Enqueue the 8-bit projection GEMM (see include/epic_link.h): a [m, k] with row scales, w
+    [n, k] with block scales; out bf16 [m, n] (FP8_BF16) or [m, n/2] (FP8_SWIGLU), or e4m3
+    [m, n/2] with out_scale (FP8_SWIGLU_FP8)."""
+    import torch
+
+    (m, k), n = a.shape, w.shape[0]
+    e4m3, e8m0 = _bytes_of("float8_e4m3fn"), _bytes_of("float8_e8m0fnu")
+    _expect("a", a, (m, k), *e4m3)
+    _expect("w", w, (n, k), *e4m3)
+    _expect("a_scale", a_scale, fp8_row_scale_shape(m, k), *e8m0)
+    _expect("w_scale", w_scale, fp8_block_scale_shape(n, k), *e8m0)
+    _expect("out", out, (m, n if epilogue == FP8_BF16 else n // 2),
+            *(e4m3 if epilogue == FP8_SWIGLU_FP8 else (torch.bfloat16,)))
+    if epilogue == FP8_SWIGLU_FP8:
+        _expect("out_scale", out_scale, fp8_row_scale_shape(m, n // 2), *e8m0)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_gemm_fp8(epilogue, _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), m, n, k, _ptr(out), _ptr(out_scale),
+                     _ptr(workspace), ws_bytes, _stream(stream)), "epic_gemm_fp8")
 
 
 # ---------------------------------------------------------------- cache layout helpers

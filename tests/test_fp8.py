@@ -1,0 +1,142 @@
+"""The 8-bit operators without a GPU: the oracle's e4m3 and scales against another definition,
+and everything that the entry points refuse (no call here reaches a launch)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import fp8  # noqa: E402
+from paper_2410_15332_amd import epic_link as el  # noqa: E402
+
+INVALID, UNSUPPORTED, WORKSPACE = 1, 2, 4
+
+
+# ---------------------------------------------------------------- the oracle
+
+def test_e4m3_values_are_torchs():
+    codes = np.arange(256, dtype=np.uint8)
+    ref = torch.from_numpy(codes).view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(fp8.e4m3_decode(codes), ref, equal_nan=True)
+
+
+def test_e4m3_rounding_is_torchs():
+    rng = np.random.default_rng(3)
+    y = np.concatenate([rng.uniform(-448, 448, 20000), rng.normal(0, 0.02, 20000), fp8.POSITIVE[:127],
+                        (fp8.POSITIVE[:126] + fp8.POSITIVE[1:127]) / 2, [0.0, -0.0, 2.0 ** -10, -2.0 ** -10]])
+    y = y.astype(np.float32)
+    ref = torch.from_numpy(y).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    assert np.array_equal(fp8.e4m3_encode(y), ref)
+    assert list(fp8.e4m3_encode(np.array([np.nan, np.inf, -np.inf]))) == [0x7F] * 3
+
+
+@pytest.mark.parametrize("top,t", [(448.0, 0), (448.0 * (1 + 2.0 ** -20), 1), (224.0, -1), (1.75, -8), (1.7500001, -7),
+                                   (1.0, -8), (0.0, 0), (2.0 ** -149, -127), (3.0e38, 120)])
+def test_scale_exponent(top, t):
+    assert fp8.scale_exponent(top) == t
+    if 0 < t < 127 or -127 < t < 0:
+        assert top <= 448 * 2.0 ** t and top > 448 * 2.0 ** (t - 1)
+
+
+def test_quantise_keeps_half_a_step():
+    rng = np.random.default_rng(4)
+    y = rng.normal(size=(5, 256)) * np.exp(rng.normal(size=(5, 256)))
+    q, t = fp8.quantise(y)
+    s = np.ldexp(1.0, fp8.spread(t, 5, 256))
+    assert np.all(np.abs(fp8.dequantise(q, t) - y) <= np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * s))
+
+
+# ---------------------------------------------------------------- refusals of the C entry points
+
+P = 1 << 20                                              # an aligned address that is never followed
+
+
+def _quant(x=P, m=4, k=128, rows=1, q=P, scale=P):
+    return el._quant_fp8(x, m, k, rows, q, scale, None)
+
+
+def _norm(x=P, delta=P, w=P, m=4, k=128, eps=1e-5, out=P, q=P, scale=P):
+    return el._rmsnorm_fp8(x, delta, w, m, k, eps, out, q, scale, None)
+
+
+def _gemm(epi=0, a=P, sa=P, w=P, sw=P, m=4, n=256, k=128, out=P, ss=P, ws=P, size=64 << 20):
+    return el._gemm_fp8(epi, a, sa, w, sw, m, n, k, out, ss, ws, size, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(m=-1), INVALID), (dict(k=0), INVALID), (dict(rows=2), INVALID), (dict(rows=0), INVALID),
+    (dict(x=None), INVALID), (dict(q=None), INVALID), (dict(scale=None), INVALID), (dict(x=P + 8), INVALID),
+    (dict(q=P + 4), INVALID), (dict(k=64), UNSUPPORTED), (dict(k=192), UNSUPPORTED),
+    (dict(m=(1 << 31) - 1, k=128), UNSUPPORTED), (dict(m=1 << 30, k=1024), UNSUPPORTED),
+    (dict(m=65536 * 128, rows=128), UNSUPPORTED)])
+def test_quant_refuses(kw, status):
+    assert _quant(**kw) == status
+    assert el._last_error()
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(m=-1), INVALID), (dict(k=0), INVALID), (dict(eps=0.0), INVALID),
+    (dict(eps=float("nan")), INVALID), (dict(x=None), INVALID), (dict(w=None), INVALID),
+    (dict(q=None), INVALID), (dict(scale=None), INVALID), (dict(out=P + 4), INVALID), (dict(delta=P + 8), INVALID),
+    (dict(k=130), UNSUPPORTED), (dict(k=32768 + 128), UNSUPPORTED), (dict(m=(1 << 31) - 1), UNSUPPORTED)])
+def test_norm_refuses(kw, status):
+    assert _norm(**kw) == status
+    assert el._last_error()
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(epi=3), INVALID), (dict(epi=-1), INVALID), (dict(m=-1), INVALID), (dict(n=0), INVALID), (dict(k=-128), INVALID),
+    (dict(a=None), INVALID), (dict(sa=None), INVALID), (dict(w=None), INVALID), (dict(sw=None), INVALID),
+    (dict(out=None), INVALID), (dict(epi=2, ss=None), INVALID), (dict(sa=P + 2), INVALID), (dict(a=P + 8), INVALID),
+    (dict(w=P + 8), INVALID), (dict(out=P + 4), INVALID), (dict(epi=2, ss=P + 1), INVALID), (dict(ws=P + 128), INVALID),
+    (dict(k=64), UNSUPPORTED), (dict(k=200), UNSUPPORTED), (dict(n=200), UNSUPPORTED), (dict(epi=1, n=384), UNSUPPORTED),
+    (dict(epi=2, n=128), UNSUPPORTED), (dict(m=1 << 24, k=128), UNSUPPORTED), (dict(n=1 << 24, k=128), UNSUPPORTED),
+    (dict(m=1 << 20, n=1024), UNSUPPORTED), (dict(ws=None), WORKSPACE), (dict(size=(64 << 20) - 1), WORKSPACE)])
+def test_gemm_refuses(kw, status):
+    assert _gemm(**kw) == status
+    assert el._last_error()
+
+
+def test_no_rows_is_no_work():
+    assert _quant(m=0, x=None, q=None, scale=None) == 0
+    assert _norm(m=0, x=None, w=None, q=None, scale=None) == 0
+    assert _gemm(m=0, a=None, sa=None, out=None, ws=None) == 0
+
+
+def test_scale_bytes():
+    assert el.epic_fp8_scale_bytes(5, 256) == 2 * 8 == int(np.prod(el.fp8_row_scale_shape(5, 256)))
+    assert el.epic_fp8_scale_bytes(0, 256) == 0
+    assert el.epic_fp8_scale_bytes(5, 100) == 0 and el.epic_fp8_scale_bytes(-1, 128) == 0
+    assert el.fp8_block_scale_shape(300, 256) == (3, 2)
+
+
+# ---------------------------------------------------------------- refusals of the binding
+
+def test_binding_refuses_what_the_kernels_cannot_read():
+    x = torch.zeros(4, 256, dtype=torch.bfloat16)
+    q, s = torch.zeros(4, 256, dtype=torch.uint8), torch.zeros(2, 4, dtype=torch.uint8)
+    for bad in (dict(x=x.float()), dict(x=x.t().contiguous().t()), dict(q=q[:, :128]), dict(q=q.to(torch.int8)),
+                dict(scale=s[:, :3]), dict(scale=None), dict()):                      # the last: not on a GPU
+        with pytest.raises(ValueError):
+            el.epic_quant_fp8(**{**dict(x=x, q=q, scale=s), **bad})
+    with pytest.raises(ValueError):
+        el.epic_rmsnorm_fp8(torch.zeros(4, 256), torch.zeros(128, dtype=torch.bfloat16), 1e-5, q, s)
+    with pytest.raises(ValueError):
+        el.epic_gemm_fp8(el.FP8_BF16, q, s, torch.zeros(128, 128, dtype=torch.uint8), torch.zeros(1, 2, dtype=torch.uint8),
+                         torch.zeros(4, 128, dtype=torch.bfloat16))
+
+
+# ---------------------------------------------------------------- the kernel chosen by sizes
+
+def route(epi, m, n, k):
+    f = el._lib.epic_gemm_fp8_route_name
+    f.restype = C.c_char_p
+    return f(epi, m, n, k).decode()
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 128, 128), (4, 6144, 4096), (100, 28672, 4096), (128, 4096, 14336),
+                                   (501, 4096, 4096), (736, 28672, 4096), (20560, 4096, 14336), (129, 256, 128)])
+def test_every_size_has_a_kernel(m, n, k):
+    for epi in range(3):
+        assert route(epi, m, n, k) != ""
