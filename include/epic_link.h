@@ -428,6 +428,38 @@ epic_status epic_gemm_fp8(int32_t epilogue, const uint8_t* a, const uint8_t* a_s
                           const uint8_t* w_scale, int32_t m, int32_t n, int32_t k, void* out, uint8_t* out_scale,
                           void* workspace, size_t workspace_bytes, void* stream);
 
+/* One layer's weights for the 8-bit projections: norms bf16, the matrices of
+ * epic_layer_weights as e4m3 with block scales (epic_quant_fp8, block_rows 128). */
+typedef struct {
+  const uint16_t* attn_norm;
+  const uint8_t* wqkv;
+  const uint8_t* wqkv_scale;
+  const uint8_t* wo;
+  const uint8_t* wo_scale;
+  const uint16_t* mlp_norm;
+  const uint8_t* w_gate_up;
+  const uint8_t* w_gate_up_scale;
+  const uint8_t* w_down;
+  const uint8_t* w_down_scale;
+} epic_layer_weights_fp8;
+
+/* epic_link_layer and epic_link_model with their projections on 8-bit operands: the same
+ * plans, caches (bf16), residual stream and outputs (fp32).  The norms' outputs, the
+ * attention's and the SwiGLU's are rounded to e4m3 per 128 values before the product that
+ * reads them; W_O's and W_down's products of many rows are added to the stream in bf16.
+ * Hq * head_dim % 128 == 0 and hidden <= 32768 are required besides what epic_model_cfg asks. */
+size_t epic_model_fp8_workspace_bytes(const epic_model_cfg* cfg, const epic_plan_sizes* sizes);
+epic_status epic_link_layer_fp8(const epic_model_cfg* cfg, const epic_layer_weights_fp8* w,
+                                const epic_plan_sizes* sizes, const epic_plan* plan_dev,
+                                float* hidden_s, uint16_t* k_cache, uint16_t* v_cache,
+                                void* workspace, size_t workspace_bytes, void* stream);
+epic_status epic_link_model_fp8(const epic_model_cfg* cfg, const epic_layer_weights_fp8* layers,
+                                const uint16_t* final_norm,
+                                const epic_plan_sizes* sizes, const epic_plan* plan_dev,
+                                float* hidden_s, uint16_t* const* k_caches, uint16_t* const* v_caches,
+                                float* out_hidden, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
 #ifdef __cplusplus
 }
 #endif

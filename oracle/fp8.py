@@ -73,3 +73,41 @@ def dequantise(codes, t, block_rows=1):
     """What bytes and exponents stand for."""
     m, k = codes.shape
     return np.ldexp(e4m3_decode(codes), spread(t, m, k, block_rows))
+
+
+# ---------------------------------------------------------------- the decoder layer on 8-bit projections
+
+def rows(y):
+    """What the rows y stand for after rounding to e4m3 with their scales."""
+    return dequantise(*quantise(y))
+
+
+def weights(w):
+    """A layer's bf16 matrices (bit patterns) rounded to e4m3 in 128 x 128 blocks; norms as they are."""
+    from .model import _bf16_to_f64
+
+    out = {}
+    for name, bits in w.items():
+        v = _bf16_to_f64(bits)
+        out[name] = v if v.ndim == 1 else dequantise(*quantise(v, GROUP), GROUP)
+    return out
+
+
+def decoder_layer(h, s_pos, w, cached_k, cached_v, n_total, ffn, hq, hkv, d, theta, eps):
+    """model.decoder_layer with every product's input rows rounded to e4m3 (w: weights()'s);
+    q, k, v and the attention output are bf16 before that, the residual stream is not rounded.
+    Returns (h, k, v, and what the layer's two branches added to h)."""
+    from .link import _round_bf16, expand_kv, masked_attention, rope
+    from .model import _silu, rmsnorm
+
+    n, h = len(s_pos), np.asarray(h, np.float64)
+    qkv = rows(rmsnorm(h, w["attn_norm"], eps)) @ w["wqkv"].T
+    q = _round_bf16(rope(qkv[:, :hq * d].reshape(n, hq, d), s_pos, theta))
+    k = _round_bf16(rope(qkv[:, hq * d:(hq + hkv) * d].reshape(n, hkv, d), s_pos, theta))
+    v = _round_bf16(qkv[:, (hq + hkv) * d:].reshape(n, hkv, d))
+    K, V = expand_kv(cached_k, cached_v, s_pos, k, v, n_total)
+    o = _round_bf16(masked_attention(q, K, V, s_pos)[0].reshape(n, hq * d))
+    attn = rows(o) @ w["wo"].T
+    gu = rows(rmsnorm(h + attn, w["mlp_norm"], eps)) @ w["w_gate_up"].T
+    mlp = rows(_silu(gu[:, :ffn]) * gu[:, ffn:]) @ w["w_down"].T
+    return h + attn + mlp, k, v, (attn, mlp)

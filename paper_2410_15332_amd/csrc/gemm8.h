@@ -17,7 +17,7 @@
 
 namespace epic {
 
-enum Gemm8Epilogue { kBf16Out = 0, kGluOut = 1, kGluQuantOut = 2 };
+enum Gemm8Epilogue { kBf16Out = 0, kGluOut = 1, kGluQuantOut = 2, kRopeOut = 3 };
 
 struct Gemm8Args {
   const uint8_t* A;     // [M][K] e4m3
@@ -28,6 +28,12 @@ struct Gemm8Args {
   uint8_t* out_scale;   // [N / 256][scale_ld(M)] e8m0 (kGluQuantOut)
   float* partial;       // planes of partial sums, kPartial8Bytes
   int M, N, K;
+  // kRopeOut (the fused Q|K|V projection): columns are heads of head_dim, hq query heads, then
+  // hkv key heads, then hkv value heads; q and k heads are rotated by the rotary table cs
+  // [M][head_dim / 2] (cos, sin) of each row; bf16 q [M][hq][D], k / v [M][hkv][D].
+  uint16_t *q, *k, *v;
+  const float2* cs;
+  int hq, hkv, head_dim;
 };
 // Requirements: K % 128 == 0, N % 128 == 0 (SwiGLU: N % 256 == 0); M * K, N * K and the
 // bytes of an output below 2^31.

@@ -37,7 +37,7 @@ namespace {
 
 constexpr int kBK = 128, kTN = 256;
 constexpr int kMaxWorkers = 256;
-constexpr int kPlanesOut = 3;  // epilogue: fp32 partial sums into planes
+constexpr int kPlanesOut = 4;  // epilogue: fp32 partial sums into planes
 
 struct WidePlan8 {
   int m_tiles, n_tiles, tiles;
@@ -117,14 +117,21 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       va[i] = min(mt * TM + gr, g.M - 1) * g.K + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     }
   };
+  // the column of a wavefront's 128 that column tile r / 32 has at r % 32: kRopeOut with heads of
+  // 128 takes the two halves of rotary pairs in turn, as heads of 64 have them anyway
+  const bool halves = EPI == kRopeOut && g.head_dim == 128;
+  auto column = [&](int r) __attribute__((always_inline)) {
+    return halves ? ((r >> 5) & 1) * 64 + ((r >> 6) & 1) * 32 + (r & 31) : r;
+  };
   auto setup_b = [&]() __attribute__((always_inline)) {
     int mt, nt;
     tile_mn(cb.tile, mt, nt);
 #pragma unroll
     for (int i = 0; i < NLB; ++i) {
       const int row = (NLB * wv + i) * 8 + lrow;
-      const int gr = GLU ? ((row >> 5) & 1) * ffn + nt * (kTN / 2) + (row >> 6) * 32 + (row & 31)
-                         : min(nt * kTN + row, g.N - 1);
+      int gr;
+      if constexpr (GLU) gr = ((row >> 5) & 1) * ffn + nt * (kTN / 2) + (row >> 6) * 32 + (row & 31);
+      else gr = min(nt * kTN + (row & ~127) + column(row & 127), g.N - 1);
       vb[i] = gr * g.K + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     }
   };
@@ -334,6 +341,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       constexpr int JS = SPLIT ? 2 : 4;                 // column tiles per pass
       constexpr int W = GLU ? 128 : 256;                // bytes of a row per pass
       const int cols = GLU ? ffn : g.N;
+      const int D = g.head_dim, hd2 = D >> 1;           // kRopeOut
       const int n0 = GLU ? nt * (kTN / 2) + wn * 64 : nt * kTN + wn * 128;
       char* out = reinterpret_cast<char*>(SPLIT ? static_cast<void*>(g.partial + size_t(part) * g.M * g.N) : g.out);
       // N % 128 == 0: all of the wavefront's columns, or none
@@ -344,12 +352,32 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int j0 = 0; j0 < J; j0 += JS) {
+          if constexpr (EPI == kRopeOut) {              // tiles j, j + 1: the halves of a head's pairs
+            const float2* cs = g.cs + size_t(min(mw + row * I + i, g.M - 1)) * hd2;
+#pragma unroll
+            for (int j = 0; j < J; j += 2)
+              if (n0 + (halves ? 0 : j * 32) < (g.hq + g.hkv) * D) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                  const float4* p = reinterpret_cast<const float4*>(cs + (halves ? j * 16 : 0) + q * 8 + half * 4);
+                  const float4 t0 = p[0], t1 = p[1];
+                  const float c[4] = {t0.x, t0.z, t1.x, t1.z}, sn[4] = {t0.y, t0.w, t1.y, t1.w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const float x1 = acc[i][j][4 * q + e], x2 = acc[i][j + 1][4 * q + e];
+                    acc[i][j][4 * q + e] = x1 * c[e] - x2 * sn[e];
+                    acc[i][j + 1][4 * q + e] = x2 * c[e] + x1 * sn[e];
+                  }
+                }
+              }
+            __builtin_amdgcn_sched_barrier(0);
+          }
 #pragma unroll
           for (int j = 0; j < JS; j += GLU ? 2 : 1)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const f32x16& v = acc[i][j0 + j];
-              const int c = ((GLU ? j / 2 : j) * 32 + q * 8 + half * 4) * OUT;   // byte of the row
+              const int c = ((GLU ? j * 16 : column(j * 32)) + q * 8 + half * 4) * OUT;   // byte of the row
               char* to = mine + row * W + ((c >> 4) ^ (row & (W / 16 - 1))) * 16 + (c & 15);
               if constexpr (SPLIT)
                 *reinterpret_cast<float4*>(to) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
@@ -362,7 +390,16 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
           for (int x = 0; x < 32 * LR / 64; ++x) {
             const int r = x * (64 / LR) + lane / LR, c = lane % LR;
             const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * W + (c ^ (r & (LR - 1))) * 16);
-            __builtin_amdgcn_raw_buffer_store_b128(v, ro, ((mw + r * I + i) * cols + n0 + j0 * 32) * OUT + c * 16, 0, 0);
+            if constexpr (EPI == kRopeOut) {
+              const int m = mw + r * I + i, n = n0 + c * 8, head = n / D;
+              uint16_t* base = head < g.hq ? g.q : head < g.hq + g.hkv ? g.k : g.v;
+              const int heads = head < g.hq ? g.hq : g.hkv;
+              const int hd = head < g.hq ? head : head < g.hq + g.hkv ? head - g.hq : head - g.hq - g.hkv;
+              if (m < g.M && n < g.N)
+                *reinterpret_cast<u32x4*>(base + (size_t(m) * heads + hd) * D + (n - head * D)) = v;
+            } else {
+              __builtin_amdgcn_raw_buffer_store_b128(v, ro, ((mw + r * I + i) * cols + n0 + j0 * 32) * OUT + c * 16, 0, 0);
+            }
           }
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -393,6 +430,7 @@ void launch_wide_tm(const Gemm8Args& g, int epi, hipStream_t stream) {
   const WidePlan8 p = plan_of(g, TM);
   if (epi == kBf16Out) gemm8_wide_kernel<kBf16Out, TM><<<p.G, 256, 0, stream>>>(g, p);
   else if (epi == kGluOut) gemm8_wide_kernel<kGluOut, TM><<<p.G, 256, 0, stream>>>(g, p);
+  else if (epi == kRopeOut) gemm8_wide_kernel<kRopeOut, TM><<<p.G, 256, 0, stream>>>(g, p);
   else gemm8_wide_kernel<kGluQuantOut, TM><<<p.G, 256, 0, stream>>>(g, p);
 }
 

@@ -45,5 +45,8 @@ void launch_rmsnorm(const float* x, const uint16_t* w, uint16_t* out_bf16, float
 void launch_rmsnorm_start(const float* x, const uint16_t* w, uint16_t* out_bf16, int rows, int hidden, float eps,
                           const int32_t* s_pos, float2* cs, int head_dim, double theta, int* cnt, int n_cnt,
                           hipStream_t stream);
+// The rotary table on its own, and x += d (d bf16, n % 4 == 0).
+void launch_rope_table(const int32_t* s_pos, float2* cs, int rows, int head_dim, double theta, hipStream_t stream);
+void launch_add_bf16(float* x, const uint16_t* d, size_t n, hipStream_t stream);
 
 }  // namespace epic

@@ -176,7 +176,33 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_kernel(const float* __re
     put(i, xr[i], *reinterpret_cast<const uint2*>(w + 4 * i));
 }
 
+__global__ __launch_bounds__(kNormThreads) void rope_table_kernel(RopeTable table) {
+  rope_entry(table, blockIdx.x * kNormThreads + threadIdx.x);
+}
+
+// x += d, four values per thread.
+__global__ __launch_bounds__(kNormThreads) void add_bf16_kernel(float4* __restrict__ x, const uint2* __restrict__ d, size_t n4) {
+  const size_t i = size_t(blockIdx.x) * kNormThreads + threadIdx.x;
+  if (i >= n4) return;
+  const float4 o = x[i];
+  const uint2 b = d[i];
+  x[i] = make_float4(o.x + __uint_as_float(b.x << 16), o.y + __uint_as_float(b.x & 0xFFFF0000u),
+                     o.z + __uint_as_float(b.y << 16), o.w + __uint_as_float(b.y & 0xFFFF0000u));
+}
+
 }  // namespace
+
+void launch_rope_table(const int32_t* s_pos, float2* cs, int rows, int head_dim, double theta, hipStream_t stream) {
+  if (rows == 0) return;
+  const RopeTable t{s_pos, cs, rows, head_dim / 2, std::log2(theta)};
+  rope_table_kernel<<<(rows * (head_dim / 2) + kNormThreads - 1) / kNormThreads, kNormThreads, 0, stream>>>(t);
+}
+
+void launch_add_bf16(float* x, const uint16_t* d, size_t n, hipStream_t stream) {
+  if (n == 0) return;
+  add_bf16_kernel<<<unsigned((n / 4 + kNormThreads - 1) / kNormThreads), kNormThreads, 0, stream>>>(
+      reinterpret_cast<float4*>(x), reinterpret_cast<const uint2*>(d), n / 4);
+}
 
 void launch_rmsnorm(const float* x, const uint16_t* w, uint16_t* out_bf16, float* out_f32, int rows, int hidden,
                     float eps, hipStream_t stream) {

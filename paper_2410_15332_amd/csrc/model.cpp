@@ -17,6 +17,7 @@
 #include "gemm.h"
 #include "link_write.h"
 #include "kernels.h"
+#include "model_internal.h"
 #include "plan_internal.h"
 #include "stream_sum.h"
 #include "status.h"
@@ -65,6 +66,10 @@ LayerWs carve(const epic_model_cfg* c, const epic_plan_sizes* s, char* base) {
   return w;
 }
 
+}  // namespace
+
+namespace epic {
+
 epic_status validate_model(const epic_model_cfg* c) {
   EPIC_CHECK_ARG(c != nullptr, "model config is NULL");
   epic_status st = validate_attn_cfg(&c->attn);
@@ -81,6 +86,49 @@ epic_status validate_model(const epic_model_cfg* c) {
   return EPIC_OK;
 }
 
+epic_status check_model_call(const epic_model_cfg* c, const epic_plan_sizes* s, const epic_plan* p, const float* h) {
+  epic_status st = validate_model(c);
+  if (st != EPIC_OK) return st;
+  EPIC_CHECK_ARG(s && p, "plan is NULL");
+  EPIC_CHECK_ARG(valid_tile_rows(s->tile_rows), "plan tile rows %d unsupported", s->tile_rows);
+  EPIC_CHECK_ARG(s->n_rerotated >= 0 && s->n_rerotated <= s->n_private, "bad plan sizes (re-rotated blocks)");
+  if (s->n_private > 0) EPIC_CHECK_ARG(p->priv_block && p->priv_src && p->priv_rows, "private block arrays are NULL");
+  if (s->n_rerotated > 0) EPIC_CHECK_ARG(p->priv_rot != nullptr, "priv_rot is NULL");
+  if (s->n_s == 0) return EPIC_OK;
+  EPIC_CHECK_ARG(p->s_pos && p->tiles && p->work && p->linked_blocks, "device plan arrays are NULL");
+  EPIC_CHECK_ARG(h != nullptr && (reinterpret_cast<uintptr_t>(h) & 15u) == 0, "hidden_s must be 16-byte aligned");
+  return EPIC_OK;
+}
+
+epic_status check_workspace(const void* ws, size_t ws_bytes, size_t need) {
+  if (ws == nullptr || ws_bytes < need)
+    return fail(EPIC_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", ws_bytes, need);
+  EPIC_CHECK_ARG((reinterpret_cast<uintptr_t>(ws) & 255u) == 0, "workspace must be 256-byte aligned");
+  return EPIC_OK;
+}
+
+epic_status link_write_only(const epic_model_cfg* c, const epic_plan_sizes* s, const epic_plan* p, uint16_t* const* kc,
+                            uint16_t* const* vc, int n_layers, void* stream) {
+  if (s->n_rerotated == 0) return EPIC_OK;
+  EPIC_CHECK_ARG(kc && vc, "KV cache pointers are NULL");
+  for (int l = 0; l < n_layers; ++l) {
+    EPIC_CHECK_ARG(kc[l] && vc[l], "layer %d: KV cache pointers are NULL", l);
+    launch_link_write_rotated(p, s->n_private, c->attn.num_kv_heads, c->attn.head_dim, c->rope_theta, nullptr, nullptr,
+                              kc[l], vc[l], static_cast<hipStream_t>(stream));
+  }
+  return hip_ok("link write launch");
+}
+
+epic_status hip_ok(const char* what) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(EPIC_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+  return EPIC_OK;
+}
+
+}  // namespace epic
+
+namespace {
+
 epic_status check_weights(const epic_layer_weights* w) {
   EPIC_CHECK_ARG(w != nullptr, "layer weights are NULL");
   EPIC_CHECK_ARG(w->attn_norm && w->wqkv && w->wo && w->mlp_norm && w->w_gate_up && w->w_down,
@@ -88,12 +136,6 @@ epic_status check_weights(const epic_layer_weights* w) {
   auto al = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
   EPIC_CHECK_ARG(al(w->attn_norm) && al(w->wqkv) && al(w->wo) && al(w->mlp_norm) && al(w->w_gate_up) && al(w->w_down),
                  "weights must be 16-byte aligned");
-  return EPIC_OK;
-}
-
-epic_status hip_ok(const char* what) {
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(EPIC_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
   return EPIC_OK;
 }
 
@@ -185,16 +227,8 @@ epic_status run_layer(const epic_model_cfg* c, const epic_layer_weights* w, cons
 
 epic_status check_common(const epic_model_cfg* c, const epic_plan_sizes* s, const epic_plan* p, const float* h,
                          void* ws, size_t ws_bytes) {
-  epic_status st = validate_model(c);
-  if (st != EPIC_OK) return st;
-  EPIC_CHECK_ARG(s && p, "plan is NULL");
-  EPIC_CHECK_ARG(valid_tile_rows(s->tile_rows), "plan tile rows %d unsupported", s->tile_rows);
-  EPIC_CHECK_ARG(s->n_rerotated >= 0 && s->n_rerotated <= s->n_private, "bad plan sizes (re-rotated blocks)");
-  if (s->n_private > 0) EPIC_CHECK_ARG(p->priv_block && p->priv_src && p->priv_rows, "private block arrays are NULL");
-  if (s->n_rerotated > 0) EPIC_CHECK_ARG(p->priv_rot != nullptr, "priv_rot is NULL");
-  if (s->n_s == 0) return EPIC_OK;
-  EPIC_CHECK_ARG(p->s_pos && p->tiles && p->work && p->linked_blocks, "device plan arrays are NULL");
-  EPIC_CHECK_ARG(h != nullptr && (reinterpret_cast<uintptr_t>(h) & 15u) == 0, "hidden_s must be 16-byte aligned");
+  epic_status st = check_model_call(c, s, p, h);
+  if (st != EPIC_OK || s->n_s == 0) return st;
   // GEMM byte offsets are 31-bit: every operand and output (rows padded to a whole
   // 256-row tile) below 2^31 bytes
   const int64_t rows = int64_t(s->n_s) + 256;
@@ -204,11 +238,7 @@ epic_status check_common(const epic_model_cfg* c, const epic_plan_sizes* s, cons
   if (rows * kmax * 2 >= lim || rows * std::max<int64_t>(qkv_n, c->hidden) * 4 >= lim ||
       int64_t(4) * c->ffn * c->hidden >= lim)
     return fail(EPIC_ERR_UNSUPPORTED, "%d rows or the weights exceed the 2^31-byte GEMM operand limit", s->n_s);
-  const size_t need = carve(c, s, nullptr).total;
-  if (ws == nullptr || ws_bytes < need)
-    return fail(EPIC_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", ws_bytes, need);
-  EPIC_CHECK_ARG((reinterpret_cast<uintptr_t>(ws) & 255u) == 0, "workspace must be 256-byte aligned");
-  return EPIC_OK;
+  return check_workspace(ws, ws_bytes, carve(c, s, nullptr).total);
 }
 
 }  // namespace
@@ -225,13 +255,8 @@ extern "C" epic_status epic_link_layer(const epic_model_cfg* cfg, const epic_lay
   clear_error();
   epic_status st = check_common(cfg, sizes, plan_dev, hidden_s, workspace, workspace_bytes);
   if (st != EPIC_OK) return st;
-  if (sizes->n_s == 0) {                    // no rows: only the re-rotated copies, if any
-    if (sizes->n_rerotated == 0) return EPIC_OK;
-    EPIC_CHECK_ARG(k_cache && v_cache, "KV cache pointers are NULL");
-    launch_link_write_rotated(plan_dev, sizes->n_private, cfg->attn.num_kv_heads, cfg->attn.head_dim,
-                              cfg->rope_theta, nullptr, nullptr, k_cache, v_cache, static_cast<hipStream_t>(stream));
-    return hip_ok("link write launch");
-  }
+  if (sizes->n_s == 0)                      // no rows: only the re-rotated copies, if any
+    return link_write_only(cfg, sizes, plan_dev, &k_cache, &v_cache, 1, stream);
   st = check_weights(w);
   if (st != EPIC_OK) return st;
   EPIC_CHECK_ARG(k_cache && v_cache, "KV cache pointers are NULL");
@@ -255,17 +280,8 @@ extern "C" epic_status epic_link_model(const epic_model_cfg* cfg, const epic_lay
   clear_error();
   epic_status st = check_common(cfg, sizes, plan_dev, hidden_s, workspace, workspace_bytes);
   if (st != EPIC_OK) return st;
-  if (sizes->n_s == 0) {                    // no rows: only the re-rotated copies, if any
-    if (sizes->n_rerotated == 0) return EPIC_OK;
-    EPIC_CHECK_ARG(k_caches && v_caches, "KV cache pointers are NULL");
-    for (int l = 0; l < cfg->n_layers; ++l) {
-      EPIC_CHECK_ARG(k_caches[l] && v_caches[l], "layer %d: KV cache pointers are NULL", l);
-      launch_link_write_rotated(plan_dev, sizes->n_private, cfg->attn.num_kv_heads, cfg->attn.head_dim,
-                                cfg->rope_theta, nullptr, nullptr, k_caches[l], v_caches[l],
-                                static_cast<hipStream_t>(stream));
-    }
-    return hip_ok("link write launch");
-  }
+  if (sizes->n_s == 0)                      // no rows: only the re-rotated copies, if any
+    return link_write_only(cfg, sizes, plan_dev, k_caches, v_caches, cfg->n_layers, stream);
   EPIC_CHECK_ARG(layers && k_caches && v_caches && final_norm && out_hidden, "NULL model argument");
   for (int l = 0; l < cfg->n_layers; ++l) {
     st = check_weights(&layers[l]);

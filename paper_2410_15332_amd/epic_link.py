@@ -85,6 +85,11 @@ class epic_layer_weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("attn_norm", "wqkv", "wo", "mlp_norm", "w_gate_up", "w_down")]
 
 
+class epic_layer_weights_fp8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("attn_norm", "wqkv", "wqkv_scale", "wo", "wo_scale", "mlp_norm", "w_gate_up",
+                                          "w_gate_up_scale", "w_down", "w_down_scale")]
+
+
 def _proto(name, restype, argtypes):
     f = getattr(_lib, name)
     f.restype = restype
@@ -147,12 +152,22 @@ _gemm_fp8 = _proto("epic_gemm_fp8", C.c_int,
                    [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p])
 
+_model_fp8_ws = _proto("epic_model_fp8_workspace_bytes", C.c_size_t, [_P(epic_model_cfg), _P(epic_plan_sizes)])
+_link_layer_fp8 = _proto("epic_link_layer_fp8", C.c_int,
+                         [_P(epic_model_cfg), _P(epic_layer_weights_fp8), _P(epic_plan_sizes), _P(epic_plan),
+                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p])
+_link_model_fp8 = _proto("epic_link_model_fp8", C.c_int,
+                         [_P(epic_model_cfg), _P(epic_layer_weights_fp8), C.c_void_p, _P(epic_plan_sizes),
+                          _P(epic_plan), C.c_void_p, _P(C.c_void_p), _P(C.c_void_p), C.c_void_p, C.c_void_p,
+                          C.c_size_t, C.c_void_p])
+
 EXPORTED = ["epic_status_string", "epic_last_error", "epic_version", "epic_plan_sizes_get", "epic_plan_layout",
             "epic_plan_link", "epic_link_workspace_bytes", "epic_link_attention", "epic_set_profile_events",
             "epic_model_workspace_bytes", "epic_link_layer", "epic_link_model", "epic_gemm_workspace_bytes",
             "epic_gemm", "epic_plan_decode_sizes", "epic_plan_decode", "epic_plan_compile_sizes",
             "epic_plan_compile", "epic_link_attention_noalloc", "epic_fp8_scale_bytes", "epic_quant_fp8",
-            "epic_rmsnorm_fp8", "epic_gemm_fp8_workspace_bytes", "epic_gemm_fp8"]
+            "epic_rmsnorm_fp8", "epic_gemm_fp8_workspace_bytes", "epic_gemm_fp8", "epic_model_fp8_workspace_bytes",
+            "epic_link_layer_fp8", "epic_link_model_fp8"]
 
 NOALLOC_SCRATCH_BYTES = 96 << 20      # EPIC_NOALLOC_SCRATCH_BYTES
 
@@ -485,6 +500,32 @@ def epic_gemm_fp8(epilogue: int, a, a_scale, w, w_scale, out, out_scale=None, wo
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_gemm_fp8(epilogue, _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), m, n, k, _ptr(out), _ptr(out_scale),
                      _ptr(workspace), ws_bytes, _stream(stream)), "epic_gemm_fp8")
+
+
+def epic_model_fp8_workspace_bytes(cfg: epic_model_cfg, sizes: epic_plan_sizes) -> int:
+    return int(_model_fp8_ws(C.byref(cfg), C.byref(sizes)))
+
+
+def epic_link_layer_fp8(cfg: epic_model_cfg, weights: epic_layer_weights_fp8, dplan: DevicePlan, hidden_s, k_cache,
+                        v_cache, workspace, stream=None):
+    """epic_link_layer with its projections on 8-bit operands."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_link_layer_fp8(C.byref(cfg), C.byref(weights), C.byref(dplan.sizes), C.byref(dplan.plan), _ptr(hidden_s),
+                           _ptr(k_cache), _ptr(v_cache), _ptr(workspace), ws_bytes, _stream(stream)),
+           "epic_link_layer_fp8")
+
+
+def epic_link_model_fp8(cfg: epic_model_cfg, layers: Sequence[epic_layer_weights_fp8], final_norm, dplan: DevicePlan,
+                        hidden_s, k_caches: Sequence, v_caches: Sequence, out_hidden, workspace, stream=None):
+    """epic_link_model with its projections on 8-bit operands."""
+    n = len(layers)
+    warr = (epic_layer_weights_fp8 * n)(*layers)
+    karr = (C.c_void_p * n)(*[t.data_ptr() for t in k_caches])
+    varr = (C.c_void_p * n)(*[t.data_ptr() for t in v_caches])
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_link_model_fp8(C.byref(cfg), warr, _ptr(final_norm), C.byref(dplan.sizes), C.byref(dplan.plan),
+                           _ptr(hidden_s), karr, varr, _ptr(out_hidden), _ptr(workspace), ws_bytes, _stream(stream)),
+           "epic_link_model_fp8")
 
 
 # ---------------------------------------------------------------- cache layout helpers

@@ -217,11 +217,43 @@ class ModelStage:
     out: object                              # torch fp32 [n_s, hidden]
     workspace: object
     compile_stage: object = None             # kept with keep_compile=True (its out: compiled hidden rows)
+    fp8: bool = False                        # 8-bit projections (layers: epic_layer_weights_fp8)
 
     def run(self, stream=None):
         self.hidden.copy_(self.emb)
-        el.epic_link_model(self.cfg, self.layers, self.final_norm, self.dplan, self.hidden, self.k_caches,
-                           self.v_caches, self.out, self.workspace, stream)
+        _model_call(self.fp8)(self.cfg, self.layers, self.final_norm, self.dplan, self.hidden, self.k_caches,
+                              self.v_caches, self.out, self.workspace, stream)
+
+
+def _model_call(fp8: bool):
+    return el.epic_link_model_fp8 if fp8 else el.epic_link_model
+
+
+def _model_workspace(cfg, sizes, fp8: bool, device):
+    import torch
+
+    need = (el.epic_model_fp8_workspace_bytes if fp8 else el.epic_model_workspace_bytes)(cfg, sizes)
+    return torch.empty(max(256, need), dtype=torch.uint8, device=device)
+
+
+def layer_struct(tw: Dict[str, object]) -> el.epic_layer_weights:
+    """The C struct of a layer's bf16 tensors."""
+    return el.epic_layer_weights(*(tw[k].data_ptr() for k in
+                                   ("attn_norm", "wqkv", "wo", "mlp_norm", "w_gate_up", "w_down")))
+
+
+def quantise_layer(tw: Dict[str, object]):
+    """A layer's weights for the 8-bit projections, rounded on the device by the library.
+    Returns (tensors, C struct)."""
+    import torch
+
+    out = {"attn_norm": tw["attn_norm"], "mlp_norm": tw["mlp_norm"]}
+    for name in ("wqkv", "wo", "w_gate_up", "w_down"):
+        w = tw[name]
+        out[name] = torch.empty(w.shape, dtype=torch.uint8, device=w.device)
+        out[name + "_scale"] = torch.empty(el.fp8_block_scale_shape(*w.shape), dtype=torch.uint8, device=w.device)
+        el.epic_quant_fp8(w, out[name], out[name + "_scale"], block_rows=el.FP8_GROUP)
+    return out, el.epic_layer_weights_fp8(*(out[n].data_ptr() for n, _ in el.epic_layer_weights_fp8._fields_))
 
 
 def model_cfg(wl, n_layers: int, tile_rows: int = 0, split_blocks: int = 0) -> el.epic_model_cfg:
@@ -276,11 +308,12 @@ class CompileStage:
     hidden: object
     out: object
     workspace: object
+    fp8: bool = False
 
     def run(self, k_caches, v_caches, stream=None):
         self.hidden.copy_(self.emb)
-        el.epic_link_model(self.cfg, self.layers, self.final_norm, self.dplan, self.hidden, k_caches, v_caches,
-                           self.out, self.workspace, stream)
+        _model_call(self.fp8)(self.cfg, self.layers, self.final_norm, self.dplan, self.hidden, k_caches, v_caches,
+                              self.out, self.workspace, stream)
 
 
 def compile_rows(wl, n_dummy: int) -> np.ndarray:
@@ -295,22 +328,22 @@ def compile_rows(wl, n_dummy: int) -> np.ndarray:
     return np.concatenate(parts)
 
 
-def stage_compile(wl, cfg, layers, final_norm, chunk_blocks, free, num_blocks, n_dummy, device="cuda"):
+def stage_compile(wl, cfg, layers, final_norm, chunk_blocks, free, num_blocks, n_dummy, device="cuda", fp8=False):
     import torch
 
     csizes, chost, _ = el.epic_plan_compile(list(wl.chunk_lens), chunk_blocks, n_dummy, cfg.attn, free, num_blocks)
     cplan = el.DevicePlan(csizes, chost, device)
     h = torch.from_numpy(compile_rows(wl, n_dummy)).to(device)
-    ws = torch.empty(max(256, el.epic_model_workspace_bytes(cfg, csizes)), dtype=torch.uint8, device=device)
+    ws = _model_workspace(cfg, csizes, fp8, device)
     return CompileStage(cfg=cfg, layers=layers, final_norm=final_norm, sizes=csizes,
                         views=el.plan_views(csizes, chost), dplan=cplan, emb=h, hidden=torch.empty_like(h),
-                        out=torch.empty_like(h), workspace=ws)
+                        out=torch.empty_like(h), workspace=ws, fp8=fp8)
 
 
 def stage_model(wl, n_layers: int = None, caches: str = "compile", cache_scale: float = 0.5, device="cuda",
                 threads: int = 8, weights_on_device: bool = False, n_dummy: int = 0,
                 keep_compile: bool = False, weights: List[Dict[str, object]] = None,
-                rerotate: bool = False, tile_rows: int = 0, split_blocks: int = 0) -> ModelStage:
+                rerotate: bool = False, tile_rows: int = 0, split_blocks: int = 0, fp8: bool = False) -> ModelStage:
     """Weights, per-chunk caches, link plan and S-row embeddings for a model-level workload.
 
     caches="compile": every chunk is compiled on the GPU by the library itself
@@ -322,6 +355,7 @@ def stage_model(wl, n_layers: int = None, caches: str = "compile", cache_scale: 
     rerotate: the link request re-rotates cached K to its linked positions.
     tile_rows: force the attention tile size of the link plan (0: the planner's choice).
     split_blocks: force the split-KV size of the link plan (0: the planner's choice).
+    fp8: 8-bit projections, in the compile and the link; the weights are rounded from the bf16 ones.
     weights_on_device: draw the weights with a seeded device generator (timing runs)
     instead of synth.model_weights (parity runs).
     """
@@ -340,9 +374,12 @@ def stage_model(wl, n_layers: int = None, caches: str = "compile", cache_scale: 
         else:
             w = synth.model_weights(wl.seed, layer, H, wl.ffn, hq, hkv, d, threads=threads)
             tw = {k: _bf16_tensor(v, device) for k, v in w.items()}
+        if fp8:
+            tw, struct = quantise_layer(tw)
+        else:
+            struct = layer_struct(tw)
         weights.append(tw)
-        layers.append(el.epic_layer_weights(*(tw[k].data_ptr() for k in
-                                              ("attn_norm", "wqkv", "wo", "mlp_norm", "w_gate_up", "w_down"))))
+        layers.append(struct)
     final_norm = _bf16_tensor(synth.final_norm_weight(wl.seed, H), device)
 
     m = len(wl.chunk_lens)
@@ -362,7 +399,7 @@ def stage_model(wl, n_layers: int = None, caches: str = "compile", cache_scale: 
     v_caches = [torch.zeros((num_blocks, hkv, d, el.BLOCK), dtype=torch.bfloat16, device=device) for _ in range(L)]
 
     if caches == "compile" and m > 0:
-        cst = stage_compile(wl, cfg, layers, final_norm, chunk_blocks, free, num_blocks, n_dummy, device)
+        cst = stage_compile(wl, cfg, layers, final_norm, chunk_blocks, free, num_blocks, n_dummy, device, fp8)
         cst.run(k_caches, v_caches)
         torch.cuda.synchronize()
         if not keep_compile:
@@ -384,11 +421,11 @@ def stage_model(wl, n_layers: int = None, caches: str = "compile", cache_scale: 
     dplan = el.DevicePlan(sizes, host, device)
     emb = _tok_rows(wl, list(range(m)), wl.chunk_lens, wl.suffix_len, views["s_pos"])
     emb_t = torch.from_numpy(emb).to(device)
-    ws = torch.empty(max(256, el.epic_model_workspace_bytes(cfg, sizes)), dtype=torch.uint8, device=device)
+    ws = _model_workspace(cfg, sizes, fp8, device)
     return ModelStage(wl=wl, cfg=cfg, weights=weights, layers=layers, final_norm=final_norm, k_caches=k_caches,
                       v_caches=v_caches, requests=[req], chunk_block_ids=chunk_blocks, sizes=sizes, views=views,
                       dplan=dplan, emb=emb_t, hidden=torch.empty_like(emb_t), out=torch.empty_like(emb_t),
-                      workspace=ws, compile_stage=cst if caches == "compile" and m > 0 else None)
+                      workspace=ws, compile_stage=cst if caches == "compile" and m > 0 else None, fp8=fp8)
 
 
 def gemm_flops_per_layer(wl, n_rows: int) -> float:

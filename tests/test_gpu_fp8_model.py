@@ -1,0 +1,158 @@
+"""The decoder layer and the model on 8-bit projections (epic_link_layer_fp8, epic_link_model_fp8).
+
+Against the oracle (oracle.fp8.decoder_layer), a layer at a time on the same inputs:
+  - recomputed K and V in the cache: the norm's e4m3 rows agree but for values within 2^-20 of a
+    border of rounding (one in about 2^16, each a step of 2^-3 of one of `hidden` inputs); the
+    product's dropped bits (2^-12 of its 2-norm) and the rounding to bf16 (2^-9 rms at most)
+    follow: 2-norm within 2^-8.
+  - what a layer adds to the stream: o differs by about 2^-8 (bf16 attention weights and its own
+    rounding), so e4m3's steps (up to 2^-3) round otherwise for at most that share of a step,
+    sqrt(2^-8 * 2^-3) = 2.2% rms; the MLP's input, SwiGLU output and products carry that on:
+    2-norm within 6%.  A wrong scale, row or weight is off by its whole size.
+The model and the layers on their own, and replays of a captured call, agree bit for bit.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import oracle  # noqa: E402
+import synth  # noqa: E402
+from oracle import fp8  # noqa: E402
+from synth.configs import ModelWorkload  # noqa: E402
+from test_gpu_model import _bits, _f64, _linked_rows, _s_embeddings  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def _wl(name, lens, suffix, k, hidden=512, ffn=1024, hq=8, hkv=2, d=64, layers=2, seed=51):
+    return ModelWorkload(name, seed, layers, hidden, ffn, hq, hkv, d, 16, 500000.0, 1e-5, lens, suffix, k)
+
+
+# streamed, split and whole products; both head dims, one odd number of KV heads
+CASES = [
+    _wl("streamed_d64", [37, 100, 16, 51], 23, 5),
+    _wl("streamed_d128", [64, 45], 30, 16, ffn=1536, hq=4, hkv=2, d=128),
+    _wl("one_row", [40], 1, 0, hidden=256, ffn=512, hq=4, hkv=4),
+    _wl("split_d128", [200, 100], 150, 100, hidden=1024, ffn=2048, hq=8, hkv=2, d=128),
+    _wl("whole_d128", [700, 300], 250, 250, hidden=256, ffn=768, hq=4, hkv=2, d=128),
+    _wl("whole_d64", [700, 300], 250, 250, hidden=384, ffn=512, hq=6, hkv=3),
+    _wl("whole_crossing_heads", [400, 200], 150, 200, hidden=256, ffn=512, hq=2, hkv=1),
+]
+
+
+def _stage(wl, **kw):
+    from paper_2410_15332_amd import harness
+    print(f"[gpu-test] fp8 model {wl.name} {kw}", flush=True)
+    return harness.stage_model(wl, fp8=True, **kw)
+
+
+def _layer_call(st, layer, hidden):
+    from paper_2410_15332_amd import epic_link as el
+    el.epic_link_layer_fp8(st.cfg, st.layers[layer], st.dplan, hidden, st.k_caches[layer], st.v_caches[layer],
+                           st.workspace)
+
+
+def _norm(x):
+    return float(np.linalg.norm(x))
+
+
+@pytest.mark.parametrize("wl", CASES, ids=[w.name for w in CASES])
+def test_layers_against_the_oracle(wl):
+    st = _stage(wl, caches="synthetic")
+    s_pos = oracle.legolink_positions(wl.chunk_lens, wl.suffix_len, wl.k)
+    hq, hkv, d = wl.num_q_heads, wl.num_kv_heads, wl.head_dim
+    st.hidden.copy_(st.emb)
+    for layer in range(wl.n_layers):
+        caches = [synth.chunk_cache(wl.seed, j, n, hkv, d, 0.5, layer=layer) for j, n in enumerate(wl.chunk_lens)]
+        h_in = st.hidden.double().cpu().numpy()
+        _layer_call(st, layer, st.hidden)
+        torch.cuda.synchronize()
+        w = fp8.weights(synth.model_weights(wl.seed, layer, wl.hidden, wl.ffn, hq, hkv, d))
+        h, k, v, added = fp8.decoder_layer(h_in, s_pos, w, [_f64(c[0]) for c in caches], [_f64(c[1]) for c in caches],
+                                           wl.linked_len, wl.ffn, hq, hkv, d, wl.rope_theta, wl.rms_eps)
+        gk, gv = _linked_rows(st, layer, s_pos)
+        ek, ev = _norm(gk - k) / _norm(k), _norm(gv - v) / _norm(v)
+        eh = _norm(st.hidden.double().cpu().numpy() - h) / _norm(added[0] + added[1])
+        print(f"[gpu-test] layer {layer}: k {ek:.2e} v {ev:.2e} added {eh:.2e}", flush=True)
+        assert ek <= 2.0 ** -8 and ev <= 2.0 ** -8 and eh <= 0.06
+
+
+@pytest.mark.parametrize("wl", CASES, ids=[w.name for w in CASES])
+def test_model_is_its_layers(wl):
+    st = _stage(wl, caches="compile")
+    st.run()
+    torch.cuda.synchronize()
+    out, k = st.out.clone(), [c.clone() for c in st.k_caches]
+    st.hidden.copy_(st.emb)
+    for layer in range(wl.n_layers):
+        _layer_call(st, layer, st.hidden)
+    h = st.hidden.double()
+    ref = h * torch.rsqrt(h.square().mean(-1, keepdim=True) + wl.rms_eps) * st.final_norm.double()
+    assert all(torch.equal(a, b) for a, b in zip(k, st.k_caches))
+    assert bool(((out - ref).abs() <= 2.0 ** -20 * ref.abs()).all())
+
+
+@pytest.mark.parametrize("wl", [CASES[0], CASES[3], CASES[4]], ids=lambda w: w.name)
+def test_replays_of_a_captured_call(wl):
+    from paper_2410_15332_amd import harness
+    st = _stage(wl, caches="compile")
+    st.run()
+    torch.cuda.synchronize()
+    ref = [st.out.clone(), st.k_caches[1].clone()]
+    graph = harness.capture_graph(st.run)
+    for _ in range(3):
+        st.out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(ref[0], st.out) and torch.equal(ref[1], st.k_caches[1])
+        st.run()                                            # an eager step between replays
+        torch.cuda.synchronize()
+
+
+def test_near_the_bf16_model():
+    """Compile and link in 8 bits against the same model in bf16: e4m3's rounding, 2^-4 at most and
+    about 2^-5.5 rms on each operand of four products a layer, independent between values: the
+    rows of the last hidden state agree to a tenth in 2-norm, and point the same way."""
+    from paper_2410_15332_amd import harness
+    wl = CASES[0]
+    a, b = harness.stage_model(wl, caches="compile"), _stage(wl, caches="compile")
+    a.run()
+    b.run()
+    torch.cuda.synchronize()
+    x, y = a.out.double(), b.out.double()
+    off = float((x - y).norm() / x.norm())
+    print(f"[gpu-test] fp8 against bf16 model: {off:.3f}", flush=True)
+    assert off <= 0.1
+    assert float(torch.cosine_similarity(x, y, -1).min()) > 0.99
+
+
+def test_re_rotated_chunks():
+    """Private copies of re-rotated chunks take the other write path; with n_s = 0 they are all there is."""
+    from paper_2410_15332_amd import epic_link as el
+    wl = CASES[0]
+    st = _stage(wl, caches="synthetic", rerotate=True)
+    st.run()
+    torch.cuda.synchronize()
+    s_pos = oracle.legolink_positions(wl.chunk_lens, wl.suffix_len, wl.k)
+    K, _ = el.read_linked_kv(_bits(st.k_caches[0]), _bits(st.v_caches[0]), st.views, 0)
+    cached = [_f64(synth.chunk_cache(wl.seed, j, n, wl.num_kv_heads, wl.head_dim, 0.5, layer=0)[0])
+              for j, n in enumerate(wl.chunk_lens)]
+    moved = np.concatenate(oracle.rerotate_cached(cached, wl.chunk_lens, wl.rope_theta, True))
+    keep = np.setdiff1d(np.arange(len(moved)), s_pos)
+    assert np.abs(_f64(K[keep]) - moved[keep]).max() <= 2.0 ** -7 * np.abs(moved).max()
+
+
+def test_refusals():
+    """Checked before anything is enqueued."""
+    from paper_2410_15332_amd import epic_link as el
+    st = _stage(CASES[0], caches="none")
+    for bad in (dict(workspace=None), dict(workspace=st.workspace[:-256]), dict(hidden_s=None), dict(k_cache=None)):
+        args = {**dict(hidden_s=st.hidden, k_cache=st.k_caches[0], v_cache=st.v_caches[0], workspace=st.workspace), **bad}
+        with pytest.raises(el.EpicError):
+            el.epic_link_layer_fp8(st.cfg, st.layers[0], st.dplan, **args)
+    w = el.epic_layer_weights_fp8(*(getattr(st.layers[0], n) for n, _ in el.epic_layer_weights_fp8._fields_))
+    w.wo_scale = None
+    with pytest.raises(el.EpicError):
+        el.epic_link_layer_fp8(st.cfg, w, st.dplan, st.hidden, st.k_caches[0], st.v_caches[0], st.workspace)
