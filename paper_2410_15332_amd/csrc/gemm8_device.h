@@ -17,11 +17,6 @@ __device__ __forceinline__ f32x16 mfma8(const i32x8& a, const i32x8& b, const f3
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, SEL_A, sa, SEL_B, sb);
 }
 
-// One byte per lane from global memory to LDS, widened: lane l's at dst[l].
-__device__ __forceinline__ void dma_byte(const uint8_t* src, int* dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (lds_void*)dst, 1, 0, 0);
-}
-
 // 32 bytes of an operand row from two 16-byte chunks in LDS.
 __device__ __forceinline__ i32x8 read32(const char* p, int c0, int c1) {
   typedef int i32x4 __attribute__((ext_vector_type(4)));

@@ -5,10 +5,9 @@
 // group), the tiles' stages dealt in G equal contiguous shares, a share's part of a tile
 // to a plane of its own (stream_sum.h), LDS a ring of NS stages.
 //
-// Scales ride in the ring: beside its operand loads, every wavefront loads for each stage
-// one byte per lane into LDS, widened to a word: lanes 0 .. 31 the scales of its 32 rows,
-// lanes 32 .. 63 the one of its columns' weight block (a wavefront's columns never cross
-// a block).  The matrix instruction takes both as they are.
+// Scales: a worker's are few (a byte per row and stage, and one per unit for the weight
+// block, which a tile's columns never leave), so they go to LDS once, while the first
+// stages are in flight.
 //
 // Stage layout: (TM + TN) rows of 128 bytes, A rows then W rows, in groups of 8 rows
 // (1 KB, one load instruction); the eight 16-byte chunks of row r are XOR-swizzled by
@@ -28,15 +27,21 @@ constexpr int kBK = 128;
 constexpr int kWorkers = 256;                           // one workgroup per CU
 constexpr int kMinUnits = 4;                            // K stages per worker, at least
 
+constexpr int kRowScales = 14336, kUnitScales = 2048;   // bytes of LDS for them: what the ring leaves
+
 template <int TM, int TN, int NW, int CT, int NS>
 __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, StreamSum s) {
   constexpr int NG = (TM + TN) / 8;                     // 1 KB row groups per stage
   constexpr int NL = NG / NW;                           // ... per wavefront
   static_assert(NG % NW == 0, "row groups per wavefront");
   static_assert((TM / 32) * (TN / 32 / CT) == NW, "a wavefront per 32 rows x 32 CT columns");
+  static_assert(TN <= 128, "one weight scale per unit");
   constexpr int SB = (TM + TN) * 128;                   // operand bytes per stage
-  __shared__ __attribute__((aligned(1024))) char lds[NS][SB];
-  __shared__ int scales[NS][NW][64];
+  // One array: with several, the compiler sees that reads of the scales cannot be told from
+  // the loads in flight to LDS, and has every stage wait for all of them.
+  __shared__ __attribute__((aligned(1024))) char lds[NS * SB + kRowScales + kUnitScales];
+  char* const row_scale = lds + NS * SB;                // [K stage][ld]
+  char* const unit_scale = row_scale + kRowScales;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int w = blockIdx.x, G = s.G;
@@ -58,8 +63,6 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
                                               kBufWord3);
   }
   const int ld = (g.M + 3) & ~3;
-  const uint8_t* sp;                                    // this lane's scale of stage 0 of the tile
-  const size_t sp_step = lane < 32 ? size_t(ld) : 1;    // ... to the next stage's
   auto setup = [&](int tile) __attribute__((always_inline)) {
     const int nt = tile / m_tiles, mt = tile - nt * m_tiles;
 #pragma unroll
@@ -70,14 +73,12 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       const int gr = is_a ? min(mt * TM + row, g.M - 1) : nt * TN + row;
       vo[i] = gr * g.K + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     }
-    sp = lane < 32 ? g.sa + min(mt * TM + rt * 32 + lane, g.M - 1) : g.sw + size_t((nt * TN + ct * 32) >> 7) * ks;
   };
   int du = u0, dtile = u0 / ks, dkt = u0 - dtile * ks;   // next unit to load
   setup(dtile);
   auto dma_next = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) dma16(rs[i], lds[buf] + (wv * NL + i) * 1024, vo[i], dkt * kBK);
-    dma_byte(sp + size_t(dkt) * sp_step, scales[buf][wv]);
+    for (int i = 0; i < NL; ++i) dma16(rs[i], lds + buf * SB + (wv * NL + i) * 1024, vo[i], dkt * kBK);
     if (du + 1 < u1) {                                  // past the last unit: that one again
       ++du;
       if (++dkt == ks) {
@@ -92,7 +93,19 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
 
 #pragma unroll
   for (int b = 0; b < NS - 1; ++b) dma_next(b);
-  int buf = 0, u = u0, tile = u0 / ks;
+  {
+    const int words = ld / 4, n = min(u1 - u0, ks) * words, k0 = (u0 % ks) * words, all = ks * words;
+    for (int i = tid; i < n; i += NW * 64) {            // the K stages of this worker, at their places
+      const int at = k0 + i < all ? k0 + i : k0 + i - all;
+      reinterpret_cast<uint32_t*>(row_scale)[at] = reinterpret_cast<const uint32_t*>(g.sa)[at];
+    }
+    for (int i = tid; i < u1 - u0; i += NW * 64) {
+      const int t = (u0 + i) / ks;
+      unit_scale[i] = char(g.sw[size_t((t / m_tiles * TN) >> 7) * ks + (u0 + i - t * ks)]);
+    }
+  }
+  int buf = 0, u = u0, tile = u0 / ks, kt = u0 - tile * ks, at = 0;   // kt, at: of the unit fetched next
+  const int srow = min(rt * 32 + (lane & 31), g.M - 1);
   while (u < u1) {
     const int ue = min(u1, (tile + 1) * ks);
     f32x16 sums[2][CT];                                 // a chain of additions for each half of a stage
@@ -106,12 +119,13 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       int sa, sb;
     } f0, f1;
     auto fetch = [&](Frags& f) __attribute__((always_inline)) {
-      wait_vmem<(NS - 2) * (NL + 1)>();                 // this wavefront's loads of unit u
+      wait_vmem<(NS - 2) * NL>();                       // this wavefront's loads of unit u
       barrier_lds();                                    // everyone's; and unit u - 1 is read
       dma_next(buf == 0 ? NS - 1 : buf - 1);            // unit u + NS - 1, where u - 1 was
-      const char* p = lds[buf];
-      f.sa = scales[buf][wv][lane & 31];
-      f.sb = scales[buf][wv][32];
+      const char* p = lds + buf * SB;
+      f.sa = uint8_t(row_scale[kt * ld + srow]);
+      f.sb = uint8_t(unit_scale[at++]);
+      kt = kt + 1 == ks ? 0 : kt + 1;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int c0 = ((4 * i + 2 * half) ^ lsw) * 16, c1 = c0 ^ 16;
@@ -187,11 +201,12 @@ bool gemm8_stream_fits(int M, int N, int K) {
   if (units >= (1 << 23)) return false;                 // 32-bit arithmetic of StreamSum::owner
   const int64_t per = std::max<int64_t>(units / kWorkers, 1);
   const int64_t planes = (K / kBK + per - 1) / per + 1;
+  if (M > 128 || K / kBK * ((M + 3) / 4 * 4) > kRowScales || units / kWorkers + 1 > kUnitScales) return false;
   return planes * M * N * 4 <= int64_t(kPartial8Bytes);
 }
 
 StreamSum launch_gemm8_stream(const Gemm8Args& g, hipStream_t stream) {
-  if (g.M <= 32) return launch_tm<32, 64, 2, 1, 10>(g, stream);
+  if (g.M <= 32) return launch_tm<32, 64, 2, 1, 11>(g, stream);
   if (g.M <= 64) return launch_tm<64, 64, 4, 1, 9>(g, stream);
   return launch_tm<128, 64, 8, 1, 6>(g, stream);
 }
