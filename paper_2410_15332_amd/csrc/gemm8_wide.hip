@@ -24,6 +24,7 @@
 // up in turn, 32 rows each.  Rows past M and columns past N are read clamped and never
 // stored.
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "gemm8.h"
@@ -166,13 +167,25 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
   };
   struct Scales {
     int a, w, u;                                        // I rows of a lane; the columns' block (gate, up)
-  } sc0, sc1, sc2;                                      // of this stage, the next, and the last ones loaded
-  auto load_scales = [&](Scales& s) __attribute__((always_inline)) {
-    if constexpr (I == 4) s.a = int(__builtin_amdgcn_raw_buffer_load_b32(rsc, vsa, cs.kt * ld, 0));
-    else s.a = int(__builtin_amdgcn_raw_buffer_load_b16(rsc, vsa, cs.kt * ld, 0));
-    s.w = int(__builtin_amdgcn_raw_buffer_load_b8(rsd, vsw, cs.kt, 0));
-    if constexpr (GLU) s.u = int(__builtin_amdgcn_raw_buffer_load_b8(rsd, vsu, cs.kt, 0));
+  } sc0, sc1;                                           // of this stage and the next
+  // the last ones loaded, in the types loaded: widened here, they would be waited for here
+  struct Loaded {
+    std::conditional_t<I == 4, uint32_t, uint16_t> a;
+    uint8_t w, u;
+  } sc2;
+  auto load_scales = [&](Loaded& s) __attribute__((always_inline)) {
+    if constexpr (I == 4) s.a = __builtin_amdgcn_raw_buffer_load_b32(rsc, vsa, cs.kt * ld, 0);
+    else s.a = __builtin_amdgcn_raw_buffer_load_b16(rsc, vsa, cs.kt * ld, 0);
+    s.w = __builtin_amdgcn_raw_buffer_load_b8(rsd, vsw, cs.kt, 0);
+    if constexpr (GLU) s.u = __builtin_amdgcn_raw_buffer_load_b8(rsd, vsu, cs.kt, 0);
     if (advance(cs)) setup_s();
+  };
+  // after sync(), where the loads have landed: left to the compiler, the copies move in
+  // front of the next stage's sync() and wait for them
+  auto take = [&](Scales& to, const Loaded& from) __attribute__((always_inline)) {
+    __asm__ volatile("v_mov_b32 %0, %1" : "=v"(to.a) : "v"(int(from.a)));
+    __asm__ volatile("v_mov_b32 %0, %1" : "=v"(to.w) : "v"(int(from.w)));
+    if constexpr (GLU) __asm__ volatile("v_mov_b32 %0, %1" : "=v"(to.u) : "v"(int(from.u)));
   };
 
   // ---- fragments
@@ -230,7 +243,8 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
     barrier_lds();
   };
 
-  load_scales(sc0);
+  Loaded first;
+  load_scales(first);
 #pragma unroll
   for (int i = 0; i < NLA; ++i) dma_a(i);
 #pragma unroll
@@ -242,6 +256,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
   for (int i = 0; i < NLB; ++i) dma_b(i);
   wait_vmem<NLA + NLB + (GLU ? 3 : 2)>();               // stage 0
   __asm__ volatile("s_barrier" ::: "memory");
+  take(sc0, first);
 #pragma unroll
   for (int i = 0; i < I + J; ++i) read1(f0, lds[0], lds[1], 0, i);
 
@@ -257,7 +272,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       sync();
       sa = bump(sa);
       sb = bump(sb);
-      sc1 = sc2;
+      take(sc1, sc2);
       load_scales(sc2);
       slice(f1, f0, lds[sa], lds[sb], 0, std::integral_constant<int, 0>{});
       sc0 = sc1;
@@ -269,58 +284,88 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
     // which held this stage's W and has been read by everyone.
     int mt, nt;
     tile_mn(tile, mt, nt);
+    // Lane numbers that the compiler cannot see through, or it keeps the offsets derived from
+    // them over the whole K loop, and spills.
+    int el = lane;
+    __asm__ volatile("" : "+v"(el));
+    const int eh = el >> 5, er = el & 31;
+    // Nothing is computed from these tiles before this point: the compiler starts on all of
+    // them at once, and runs out of registers.
+    auto from_here = [&](int i, int j, int n) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < n; ++x) __asm__ volatile("" : "+a"(acc[i][j + x]));
+    };
     const int mw = mt * TM + wm * (TM / 2);             // the wavefront's first row
     char* room = lds[ca.slot];
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    if constexpr (GLU) {
+    if constexpr (EPI == kGluQuantOut) {
+      // a row's other columns are in lane l ^ 32 and in the wavefront with the other wn: the
+      // room takes first the maxima, then the tile
+      // the values of a lane wait for their scale where the gate's sums were
+      float top[I];
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        top[i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < J; j += 2) {
+          from_here(i, j, 2);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = silu(acc[i][j][r]) * acc[i][j + 1][r];
+#pragma unroll
+          for (int r = 0; r < 16; r += 2)               // NaN is passed over
+            top[i] = fmaxf(fmaxf(fabsf(acc[i][j][r]), fabsf(acc[i][j][r + 1])), top[i]);
+          from_here(i, j, 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        top[i] = fmaxf(top[i], __shfl_xor(top[i], 32));
+      }
+      bool inf = false;
+#pragma unroll
+      for (int i = 0; i < I; ++i) inf |= top[i] == INFINITY;
+      if (__any(inf)) {                                 // e4m3 has no infinities: NaN instead
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+          top[i] = 0.0f;
+#pragma unroll
+          for (int j = 0; j < J; j += 2) {
+            from_here(i, j, 1);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              acc[i][j][r] = fabsf(acc[i][j][r]) == INFINITY ? NAN : acc[i][j][r];
+              top[i] = fmaxf(top[i], fabsf(acc[i][j][r]));
+            }
+            from_here(i, j, 1);
+          }
+          top[i] = fmaxf(top[i], __shfl_xor(top[i], 32));
+        }
+      }
+      float* tops = reinterpret_cast<float*>(room);     // [wm][wn][i][32]
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+        if (eh == 0) tops[(wv * I + i) * 32 + er] = top[i];
+      barrier_lds();
+      int byte[I];
+#pragma unroll
+      for (int i = 0; i < I; ++i) byte[i] = scale_byte(__float_as_uint(fmaxf(top[i], tops[((wv ^ 1) * I + i) * 32 + er])));
+      barrier_lds();                                    // the maxima are read
+      const int row0 = wm * (TM / 2) + er * I;  // of the tile
 #pragma unroll
       for (int i = 0; i < I; ++i) {
 #pragma unroll
         for (int j = 0; j < J; j += 2) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] = silu(acc[i][j][r]) * acc[i][j + 1][r];
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-    }
-    if constexpr (EPI == kGluQuantOut) {
-      // a row's other columns are in lane l ^ 32 and in the wavefront with the other wn: the
-      // room takes first the maxima, then the tile
-      uint32_t top[I];
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-        top[i] = 0;
-#pragma unroll
-        for (int j = 0; j < J; j += 2)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) top[i] = max(top[i], finite_abs(acc[i][j][r]));
-        top[i] = max(top[i], uint32_t(__shfl_xor(int(top[i]), 32)));
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      uint32_t* tops = reinterpret_cast<uint32_t*>(room);   // [wm][wn][i][32]
-#pragma unroll
-      for (int i = 0; i < I; ++i)
-        if (half == 0) tops[(wv * I + i) * 32 + (lane & 31)] = top[i];
-      barrier_lds();
-      int byte[I];
-#pragma unroll
-      for (int i = 0; i < I; ++i) byte[i] = scale_byte(max(top[i], tops[((wv ^ 1) * I + i) * 32 + (lane & 31)]));
-      barrier_lds();                                    // the maxima are read
-      const int row0 = wm * (TM / 2) + (lane & 31) * I;  // of the tile
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-#pragma unroll
-        for (int j = 0; j < J; j += 2)
+          from_here(i, j, 1);
+          const f32x16& v = acc[i][j];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const int row = row0 + i, c = wn * 64 + j * 16 + q * 8 + half * 4;
+            const int row = row0 + i, c = wn * 64 + j * 16 + q * 8 + eh * 4;
             *reinterpret_cast<uint32_t*>(room + row * 128 + ((c >> 4) ^ ((row / I) & 7)) * 16 + (c & 15)) =
-                pack_e4m3x4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3], byte[i]);
+                pack_finite_e4m3x4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], byte[i]);
           }
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
-      const int first = mw + (lane & 31) * I;
-      if (wn == 0 && half == 0 && first < g.M) {        // I neighbouring rows; those past M are padding
+      const int first = mw + er * I;
+      if (wn == 0 && eh == 0 && first < g.M) {        // I neighbouring rows; those past M are padding
         uint8_t* to = g.out_scale + size_t(nt) * ld + first;
         if constexpr (I == 4) *reinterpret_cast<uint32_t*>(to) = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
         else *reinterpret_cast<uint16_t*>(to) = uint16_t(byte[0] | byte[1] << 8);
@@ -329,7 +374,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(g.out, 0, g.M * ffn, kBufWord3);
 #pragma unroll
       for (int x = 0; x < TM / 32; ++x) {               // eight lanes a row
-        const int row = x * 32 + (tid >> 3), c = tid & 7;
+        const int row = x * 32 + wv * 8 + (el >> 3), c = el & 7;
         const u32x4 v = *reinterpret_cast<const u32x4*>(room + row * 128 + (c ^ ((row / I) & 7)) * 16);
         __builtin_amdgcn_raw_buffer_store_b128(v, ro, (mt * TM + row) * ffn + nt * (kTN / 2) + c * 16, 0, 0);
       }
@@ -340,6 +385,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       constexpr int OUT = SPLIT ? 4 : 2;                // bytes of a result
       constexpr int JS = SPLIT ? 2 : 4;                 // column tiles per pass
       constexpr int W = GLU ? 128 : 256;                // bytes of a row per pass
+      constexpr int PAIR = GLU || EPI == kRopeOut ? 2 : 1;   // column tiles that make a result
       const int cols = GLU ? ffn : g.N;
       const int D = g.head_dim, hd2 = D >> 1;           // kRopeOut
       const int n0 = GLU ? nt * (kTN / 2) + wn * 64 : nt * kTN + wn * 128;
@@ -347,48 +393,55 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       // N % 128 == 0: all of the wavefront's columns, or none
       const __amdgpu_buffer_rsrc_t ro =
           __builtin_amdgcn_make_buffer_rsrc(out, 0, n0 < cols ? g.M * cols * OUT : 0, kBufWord3);
-      const int row = lane & 31;
+      const int row = er;
 #pragma unroll
       for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int j0 = 0; j0 < J; j0 += JS) {
-          if constexpr (EPI == kRopeOut) {              // tiles j, j + 1: the halves of a head's pairs
-            const float2* cs = g.cs + size_t(min(mw + row * I + i, g.M - 1)) * hd2;
+          // four results of the lane's row from column c of the pass on
+          auto put = [&](int c, float a, float b, float d, float e) __attribute__((always_inline)) {
+            char* to = mine + row * W + ((c * OUT >> 4) ^ (row & (W / 16 - 1))) * 16 + (c * OUT & 15);
+            if constexpr (SPLIT) *reinterpret_cast<float4*>(to) = make_float4(a, b, d, e);
+            else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(d, e));
+          };
+          const float2* cs = nullptr;
+          if constexpr (EPI == kRopeOut) cs = g.cs + size_t(min(mw + row * I + i, g.M - 1)) * hd2;
 #pragma unroll
-            for (int j = 0; j < J; j += 2)
-              if (n0 + (halves ? 0 : j * 32) < (g.hq + g.hkv) * D) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                  const float4* p = reinterpret_cast<const float4*>(cs + (halves ? j * 16 : 0) + q * 8 + half * 4);
-                  const float4 t0 = p[0], t1 = p[1];
-                  const float c[4] = {t0.x, t0.z, t1.x, t1.z}, sn[4] = {t0.y, t0.w, t1.y, t1.w};
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    const float x1 = acc[i][j][4 * q + e], x2 = acc[i][j + 1][4 * q + e];
-                    acc[i][j][4 * q + e] = x1 * c[e] - x2 * sn[e];
-                    acc[i][j + 1][4 * q + e] = x2 * c[e] + x1 * sn[e];
-                  }
-                }
-              }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-#pragma unroll
-          for (int j = 0; j < JS; j += GLU ? 2 : 1)
+          for (int j = 0; j < JS; j += PAIR) {
+            from_here(i, j0 + j, PAIR);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              const f32x16& v = acc[i][j0 + j];
-              const int c = ((GLU ? j * 16 : column(j * 32)) + q * 8 + half * 4) * OUT;   // byte of the row
-              char* to = mine + row * W + ((c >> 4) ^ (row & (W / 16 - 1))) * 16 + (c & 15);
-              if constexpr (SPLIT)
-                *reinterpret_cast<float4*>(to) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-              else
-                *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(v[4 * q], v[4 * q + 1]),
-                                                           pack_bf16x2(v[4 * q + 2], v[4 * q + 3]));
+              const f32x16 &v = acc[i][j0 + j], &u = acc[i][j0 + (j + 1) % JS];
+              const int c = q * 8 + eh * 4;
+              if constexpr (GLU) {
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = silu(v[4 * q + e]) * u[4 * q + e];
+                put(j * 16 + c, x[0], x[1], x[2], x[3]);
+              } else if constexpr (EPI == kRopeOut) {   // tiles j, j + 1: the halves of a head's pairs
+                float x[4], y[4], t[8] = {1.0f, 0.0f, 1.0f, 0.0f, 1.0f, 0.0f, 1.0f, 0.0f};
+                if (n0 + (halves ? 0 : j * 32) < (g.hq + g.hkv) * D) {
+                  const float4* p = reinterpret_cast<const float4*>(cs + (halves ? j * 16 : 0) + c);
+                  const float4 t0 = p[0], t1 = p[1];
+                  t[0] = t0.x, t[1] = t0.y, t[2] = t0.z, t[3] = t0.w, t[4] = t1.x, t[5] = t1.y, t[6] = t1.z, t[7] = t1.w;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  x[e] = v[4 * q + e] * t[2 * e] - u[4 * q + e] * t[2 * e + 1];
+                  y[e] = u[4 * q + e] * t[2 * e] + v[4 * q + e] * t[2 * e + 1];
+                }
+                put(column(j * 32) + c, x[0], x[1], x[2], x[3]);
+                put(column(j * 32 + 32) + c, y[0], y[1], y[2], y[3]);
+              } else {
+                put(j * 32 + c, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+              }
             }
+            __builtin_amdgcn_sched_barrier(0);
+          }
           constexpr int LR = W / 16;                    // lanes a row
 #pragma unroll
           for (int x = 0; x < 32 * LR / 64; ++x) {
-            const int r = x * (64 / LR) + lane / LR, c = lane % LR;
+            const int r = x * (64 / LR) + el / LR, c = el % LR;
             const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * W + (c ^ (r & (LR - 1))) * 16);
             if constexpr (EPI == kRopeOut) {
               const int m = mw + r * I + i, n = n0 + c * 8, head = n / D;

@@ -31,6 +31,15 @@ __device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(in(c), in(d), r, true));
 }
 
+// The same for values without infinities, in two instructions: the conversion divides by a
+// power of two itself.
+__device__ __forceinline__ uint32_t pack_finite_e4m3x4(float a, float b, float c, float d, int byte) {
+  typedef short i16x2 __attribute__((ext_vector_type(2)));
+  const float s = __uint_as_float(uint32_t(byte) << 23);
+  i16x2 r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(i16x2{0, 0}, a, b, s, false);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, s, true));
+}
+
 // Largest of the 16 lanes of a DPP row, in all of them.
 __device__ __forceinline__ uint32_t row16_max(uint32_t v) {
   v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x128, 0xF, 0xF, false)));   // row_ror:8
