@@ -21,7 +21,8 @@ PROBE_LIB = os.path.join(PKG, "probe", "libepic_probe.so")
 
 SOURCES = ["status.cpp", "plan.cpp", "api.cpp", "model.cpp", "link_write.hip", "attention.hip", "gemm.hip",
            "gemm_stream.hip", "gemm_wide.hip", "layer.hip", "decode_attention.hip", "noalloc.hip", "api_fp8.cpp",
-           "model_fp8.cpp", "quant.hip", "gemm8.hip", "gemm8_stream.hip", "gemm8_wide.hip"]
+           "model_fp8.cpp", "quant.hip", "gemm8.hip", "gemm8_few.hip", "gemm8_stream.hip",
+           "gemm8_wide.hip"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms are disabled: hipcc must not emit them for this target.

@@ -101,7 +101,10 @@ extern "C" const char* epic_gemm_fp8_route_name(int32_t epilogue, int32_t m, int
   if (epilogue < kBf16Out || epilogue > kGluQuantOut || m <= 0 || n <= 0 || k <= 0 || n % kGroup != 0 || k % kGroup != 0)
     return "";
   const Gemm8Plan p = gemm8_plan(m, n, k, epilogue);
-  if (p.stream) return "stream";
-  if (p.parts > 1) return p.tm == 256 ? "split256" : "split128";
+  if (p.kind == Gemm8Kind::kFew) return "few";
+  if (p.kind == Gemm8Kind::kStream) return "stream";
+  if (p.kind == Gemm8Kind::kNarrow)
+    return p.tm == 128 ? "narrow128x128" : p.tn == 256 ? "narrow64x256" : p.tn == 128 ? "narrow64x128" : "narrow64x64";
+  if (p.kind == Gemm8Kind::kSplit) return p.tm == 256 ? "split256" : "split128";
   return p.tm == 256 ? "whole256" : "whole128";
 }

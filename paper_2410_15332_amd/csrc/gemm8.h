@@ -40,11 +40,14 @@ struct Gemm8Args {
 
 constexpr size_t kPartial8Bytes = size_t(64) << 20;
 
-// How a product runs: weights streamed past a short row set, or 256-column tiles of 128 or
-// 256 rows in equal parts of K; parts == 0: whole tiles, epilogue fused, no planes.
+// How a product runs: up to 32 rows in one launch (kFew), weights streamed past a short row
+// set (kStream), whole tiles of 64 or 128 rows and columns (kNarrow), or 256-column tiles of
+// 128 or 256 rows, whole (kWhole) or in equal parts of K (kSplit).  kStream and kSplit leave
+// partial sums in planes.
+enum class Gemm8Kind { kFew, kStream, kNarrow, kWhole, kSplit };
 struct Gemm8Plan {
-  bool stream;
-  int tm, parts;
+  Gemm8Kind kind;
+  int tm, tn, parts;
 };
 Gemm8Plan gemm8_plan(int M, int N, int K, int epi);
 void launch_gemm8(const Gemm8Args& g, int epi, hipStream_t stream);
@@ -53,8 +56,12 @@ StreamSum launch_gemm8_partial(const Gemm8Args& g, const Gemm8Plan& p, hipStream
 // The pass that adds the planes and runs the epilogue.
 void launch_gemm8_finish(const StreamSum& s, const Gemm8Args& g, int epi, hipStream_t stream);
 
-// of gemm8_stream.hip and gemm8_wide.hip
+// of gemm8_few.hip, gemm8_stream.hip and gemm8_wide.hip
+void launch_gemm8_few(const Gemm8Args& g, int epi, hipStream_t stream);       // not kGluQuantOut
+StreamSum launch_gemm8_few_plane(const Gemm8Args& g, hipStream_t stream);     // one fp32 plane
 StreamSum launch_gemm8_stream(const Gemm8Args& g, hipStream_t stream);
+bool gemm8_narrow_fits(int N, int K, int epi, int tm, int tn);
+void launch_gemm8_narrow(const Gemm8Args& g, int epi, int tm, int tn, hipStream_t stream);
 bool gemm8_stream_fits(int M, int N, int K);
 StreamSum launch_gemm8_split(const Gemm8Args& g, int tm, int parts, hipStream_t stream);
 void launch_gemm8_wide(const Gemm8Args& g, int epi, int tm, hipStream_t stream);

@@ -1,5 +1,6 @@
 // How 8-bit products are divided, and the pass that finishes those left in planes.
 #include <algorithm>
+#include <cmath>
 
 #include "gemm8.h"
 #include "quant.h"
@@ -44,32 +45,78 @@ __global__ __launch_bounds__(256) void finish_quant_kernel(StreamSum s, uint8_t*
 
 int cdiv(int a, int b) { return (a + b - 1) / b; }
 
+// Estimates in us, fitted to kernels replayed in a graph, that gemm8_plan chooses by.
+
+// What reading the operands from memory takes at best.
+double read_time(int M, int N, int K) { return (double(N) * K + double(M) * K) / 5.4e6; }
+
+// A workgroup per 16 columns reads its rows of W and, from the caches, the rows of A: 30 bytes a
+// ns.  1 row, N = K = 4096: 5.8 us (streamed 9.5); 16 rows, N 6144: 10.5 (11.8); but 32 rows,
+// 6144: 15.2 (12.2), and 16 rows, N 1024, K 14336: 16 (11).
+double few_time(int M, int N, int K, int epi) {
+  const bool glu = epi == kGluOut;
+  const double wgs = double(cdiv(glu ? N / 2 : N, 16));
+  const double bytes = std::ceil(wgs / kWorkers) * 16.0 * K * ((glu ? 2 : 1) + M / 16.0);
+  return 2.5 + std::max(bytes / 30e3, read_time(M, N, K)) + (epi == kGluQuantOut ? 3.0 : 0.0);
+}
+
+// Every worker has the same share of stages; the planes are added by a second launch.
+double stream_time(int M, int N, int K) {
+  const int tm = M <= 32 ? 32 : M <= 64 ? 64 : 128;
+  return 7.0 + double(N / 64) * (K / kGroup) / kWorkers * (tm == 32 ? 0.38 : tm == 64 ? 0.47 : 0.6);
+}
+
+// Whole tiles of tm x tn, a workgroup each: LDS traffic paces a stage (64 x 256: two stages in
+// flight do not cover the latency).  256 rows, N = K = 4096:
+// 64 x 64 13.9 us, 64 x 128 17.3 (split 128-row tiles 17.5); 501 rows: 25 and 18.4 (21.7);
+// SwiGLU of 100 rows, N 28672: 128 x 128 31.4 (streamed 42).
+double narrow_time(int M, int N, int K, int tm, int tn) {
+  const double rounds = cdiv(cdiv(M, tm) * (N / tn), kWorkers);
+  const double stage = tm == 128 ? 0.6 : tn == 64 ? 0.257 : tn == 128 ? 0.37 : 0.95;
+  const double run = rounds * (K / kGroup * stage) + (rounds - 1) * 4.0, read = read_time(M, N, K);
+  return 4.5 + std::max(run, read) + 0.1 * std::min(run, read);
+}
+
+// 256-column tiles in equal parts of K: with more than half of the CUs at work a stage takes
+// longer (power, and what they read), and what W takes from memory hides only in part.
+// Planes: 2 us and 0.35 us a MB.  736 rows, K 14336, N 4096: 128-row tiles in 2 parts 62 us,
+// 256 in 4 56, whole 78; 200 rows of gate|up, N 28672: whole 128-row tiles 40, 256 47.
+double wide_time(int M, int N, int K, int tm, int parts) {
+  const int work = cdiv(M, tm) * cdiv(N, 256) * parts;
+  const double rounds = cdiv(work, kWorkers), busy = std::max(work / rounds / kWorkers - 0.5, 0.0);
+  const double stage = tm == 256 ? 0.965 + busy : 0.685 + 0.4 * busy;
+  const double run = rounds * (cdiv(K / kGroup, parts) * stage + (tm == 256 ? 6.0 : 3.6)), read = read_time(M, N, K);
+  return std::max(run, read) + 0.45 * std::min(run, read) + (parts > 1 ? 2.0 + 0.35e-6 * 4 * parts * M * N : 0.0);
+}
+
 }  // namespace
 
-// Up to 128 rows: streamed.  Past that the cheaper of whole tiles and equal parts of K, by
-// the time of the stages that the busiest CU runs and of what the planes move.
 Gemm8Plan gemm8_plan(int M, int N, int K, int epi) {
-  if (M <= 128 && gemm8_stream_fits(M, N, K)) return Gemm8Plan{true, 0, 0};
-  const int ks = K / kGroup;
-  Gemm8Plan best{};
-  double best_time = 0.0;
-  for (const int tm : {256, 128}) {
-    const int64_t tiles = int64_t(cdiv(M, tm)) * cdiv(N, 256);
-    const double stage = tm == 256 ? 1.1 : 0.75;
-    for (int parts = 1; parts <= 32 && parts <= ks; ++parts) {
-      if (parts > 1 && (tiles * parts > kWorkers || int64_t(parts) * M * N * 4 > int64_t(kPartial8Bytes) || ks / parts < 4))
+  Gemm8Plan best{Gemm8Kind::kWhole, 256, 256, 1};
+  double time = wide_time(M, N, K, 256, 1);
+  auto consider = [&](const Gemm8Plan& p, double t) {
+    if (t < time) best = p, time = t;
+  };
+  if (M <= 32) consider(Gemm8Plan{Gemm8Kind::kFew, 0, 0, 0}, few_time(M, N, K, epi));
+  if (gemm8_stream_fits(M, N, K)) consider(Gemm8Plan{Gemm8Kind::kStream, 0, 0, 0}, stream_time(M, N, K));
+  constexpr int kNarrow[][2] = {{64, 64}, {64, 128}, {128, 128}, {64, 256}};
+  for (const auto& t : kNarrow)
+    if (gemm8_narrow_fits(N, K, epi, t[0], t[1]))
+      consider(Gemm8Plan{Gemm8Kind::kNarrow, t[0], t[1], 0}, narrow_time(M, N, K, t[0], t[1]));
+  for (const int tm : {256, 128})
+    for (int parts = 1; parts <= 16; ++parts) {
+      const int64_t work = int64_t(cdiv(M, tm)) * cdiv(N, 256) * parts;
+      if (parts > 1 && (work > kWorkers || int64_t(parts) * M * N * 4 > int64_t(kPartial8Bytes) || K / kGroup / parts < 2))
         break;
-      const double rounds = double((tiles * parts + kWorkers - 1) / kWorkers);
-      double time = 6.0 + rounds * (cdiv(ks, parts) * stage + (tm == 256 ? 3.0 : 1.5));
-      if (parts > 1) time += 4.0 + double(parts) * M * N * 8 * 0.25e-6;
-      if (best.tm == 0 || time < best_time) best = Gemm8Plan{false, tm, parts == 1 ? 0 : parts}, best_time = time;
+      consider(Gemm8Plan{parts == 1 ? Gemm8Kind::kWhole : Gemm8Kind::kSplit, tm, 256, parts}, wide_time(M, N, K, tm, parts));
     }
-  }
   return best;
 }
 
 StreamSum launch_gemm8_partial(const Gemm8Args& g, const Gemm8Plan& p, hipStream_t stream) {
-  return p.stream ? launch_gemm8_stream(g, stream) : launch_gemm8_split(g, p.tm, std::max(p.parts, 1), stream);
+  if (p.kind == Gemm8Kind::kFew) return launch_gemm8_few_plane(g, stream);
+  if (p.kind == Gemm8Kind::kStream) return launch_gemm8_stream(g, stream);
+  return launch_gemm8_split(g, p.tm, p.parts, stream);
 }
 
 void launch_gemm8_finish(const StreamSum& s, const Gemm8Args& g, int epi, hipStream_t stream) {
@@ -83,8 +130,10 @@ void launch_gemm8_finish(const StreamSum& s, const Gemm8Args& g, int epi, hipStr
 
 void launch_gemm8(const Gemm8Args& g, int epi, hipStream_t stream) {
   const Gemm8Plan p = gemm8_plan(g.M, g.N, g.K, epi);
-  if (p.stream || p.parts > 1) launch_gemm8_finish(launch_gemm8_partial(g, p, stream), g, epi, stream);
-  else launch_gemm8_wide(g, epi, p.tm, stream);
+  if (p.kind == Gemm8Kind::kWhole) launch_gemm8_wide(g, epi, p.tm, stream);
+  else if (p.kind == Gemm8Kind::kNarrow) launch_gemm8_narrow(g, epi, p.tm, p.tn, stream);
+  else if (p.kind == Gemm8Kind::kFew && epi != kGluQuantOut) launch_gemm8_few(g, epi, stream);
+  else launch_gemm8_finish(launch_gemm8_partial(g, p, stream), g, epi, stream);
 }
 
 }  // namespace epic

@@ -14,10 +14,12 @@
 // (r / 2) % 8, so the 16 lanes of each ds_read_b128 group touch distinct banks.
 // Rows past M are read as row M - 1 and never stored.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm8.h"
 #include "gemm8_device.h"
 #include "quant.h"
+#include "quant_device.h"
 
 namespace epic {
 
@@ -27,15 +29,24 @@ constexpr int kBK = 128;
 constexpr int kWorkers = 256;                           // one workgroup per CU
 constexpr int kMinUnits = 4;                            // K stages per worker, at least
 
+__device__ __forceinline__ float silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(-x * kLog2e)); }
+
 constexpr int kRowScales = 14336, kUnitScales = 2048;   // bytes of LDS for them: what the ring leaves
 
-template <int TM, int TN, int NW, int CT, int NS>
+// A wavefront has 32 RT rows x 32 CT columns of a tile.  OUT: kPlanesOut, or kBf16Out, kGluOut or
+// kGluQuantOut for whole tiles: worker w has tile w, and stores its result itself (GLU: the
+// tile's columns are gate and up in turn, 32 each).
+constexpr int kPlanesOut = 4;
+template <int OUT, int TM, int TN, int RT, int CT, int NS>
 __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, StreamSum s) {
+  constexpr bool WHOLE = OUT != kPlanesOut, GLU = OUT == kGluOut || OUT == kGluQuantOut;
+  constexpr int NW = (TM / 32 / RT) * (TN / 32 / CT);
   constexpr int NG = (TM + TN) / 8;                     // 1 KB row groups per stage
   constexpr int NL = NG / NW;                           // ... per wavefront
   static_assert(NG % NW == 0, "row groups per wavefront");
-  static_assert((TM / 32) * (TN / 32 / CT) == NW, "a wavefront per 32 rows x 32 CT columns");
-  static_assert(TN <= 128, "one weight scale per unit");
+  static_assert(!GLU || CT == 2, "a wavefront holds the gate and up of its columns");
+  static_assert(TN <= (GLU ? 256 : 128), "one weight scale per unit (GLU: two)");
+  static_assert(OUT != kGluQuantOut || TN == 256, "a tile has whole groups of the result");
   constexpr int SB = (TM + TN) * 128;                   // operand bytes per stage
   // One array: with several, the compiler sees that reads of the scales cannot be told from
   // the loads in flight to LDS, and has every stage wait for all of them.
@@ -50,7 +61,8 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
   const int u0 = s.begin(wr), u1 = s.begin(wr + 1);
   if (u0 >= u1) return;
   constexpr int WC = TN / 32 / CT;                      // wavefronts along N
-  const int rt = wv / WC, ct = wv % WC * CT;            // row block, first column block
+  const int rt = wv / WC * RT, ct = wv % WC * CT;       // first row block, first column block
+  const int ffn = g.N / 2;
 
   // ---- loads: row group gi of a stage, A rows first
   const int lrow = lane >> 3;
@@ -70,7 +82,8 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       const int gi = wv * NL + i;
       const bool is_a = gi < TM / 8;
       const int row = (is_a ? gi : gi - TM / 8) * 8 + lrow;
-      const int gr = is_a ? min(mt * TM + row, g.M - 1) : nt * TN + row;
+      int gr = is_a ? min(mt * TM + row, g.M - 1) : nt * TN + row;
+      if (GLU && !is_a) gr = ((row >> 5) & 1) * ffn + nt * (TN / 2) + (row >> 6) * 32 + (row & 31);
       vo[i] = gr * g.K + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     }
   };
@@ -94,42 +107,59 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
 #pragma unroll
   for (int b = 0; b < NS - 1; ++b) dma_next(b);
   {
-    const int words = ld / 4, n = min(u1 - u0, ks) * words, k0 = (u0 % ks) * words, all = ks * words;
-    for (int i = tid; i < n; i += NW * 64) {            // the K stages of this worker, at their places
-      const int at = k0 + i < all ? k0 + i : k0 + i - all;
-      reinterpret_cast<uint32_t*>(row_scale)[at] = reinterpret_cast<const uint32_t*>(g.sa)[at];
+    // a stage's scales of the tile's rows (planes: of all rows, M <= 128), at the stage's place
+    const int words = min(ld, TM) / 4, all = ks * words;
+    const int mt0 = WHOLE ? (u0 / ks) % m_tiles * (TM / 4) : 0;
+    const int n = min(u1 - u0, ks) * words, k0 = (u0 % ks) * words;
+    for (int i = tid; i < n; i += NW * 64) {
+      const int at = k0 + i < all ? k0 + i : k0 + i - all, k = at / words;
+      reinterpret_cast<uint32_t*>(row_scale)[at] =
+          reinterpret_cast<const uint32_t*>(g.sa)[size_t(k) * (ld / 4) + min(mt0 + at - k * words, ld / 4 - 1)];
     }
     for (int i = tid; i < u1 - u0; i += NW * 64) {
-      const int t = (u0 + i) / ks;
-      unit_scale[i] = char(g.sw[size_t((t / m_tiles * TN) >> 7) * ks + (u0 + i - t * ks)]);
+      const int t = (u0 + i) / ks, k = u0 + i - t * ks;
+      const int col = t / m_tiles * TN / (GLU ? 2 : 1);
+      unit_scale[i] = char(g.sw[size_t(col >> 7) * ks + k]);
+      if (GLU) unit_scale[i + ks] = char(g.sw[size_t((ffn + col) >> 7) * ks + k]);
     }
   }
   int buf = 0, u = u0, tile = u0 / ks, kt = u0 - tile * ks, at = 0;   // kt, at: of the unit fetched next
-  const int srow = min(rt * 32 + (lane & 31), g.M - 1);
+  const int swords = min(ld, TM);
+  int srow[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) srow[r] = min((rt + r) * 32 + (lane & 31), swords - 1);
   while (u < u1) {
     const int ue = min(u1, (tile + 1) * ks);
-    f32x16 sums[2][CT];                                 // a chain of additions for each half of a stage
+    // a chain of additions for each half of a stage where a wavefront has one tile
+    constexpr int NA = RT * CT == 1 ? 2 : 1;
+    f32x16 sums[NA][RT][CT];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NA; ++i)
 #pragma unroll
-      for (int j = 0; j < CT; ++j) sums[i][j] = f32x16{};
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int j = 0; j < CT; ++j) sums[i][r][j] = f32x16{};
     // unit u is read while unit u - 1 is on the matrix cores
     struct Frags {
-      i32x8 a[2], b[2][CT];
-      int sa, sb;
+      i32x8 a[2][RT], b[2][CT];
+      int sa[RT], sb[GLU ? 2 : 1];
     } f0, f1;
     auto fetch = [&](Frags& f) __attribute__((always_inline)) {
       wait_vmem<(NS - 2) * NL>();                       // this wavefront's loads of unit u
       barrier_lds();                                    // everyone's; and unit u - 1 is read
       dma_next(buf == 0 ? NS - 1 : buf - 1);            // unit u + NS - 1, where u - 1 was
       const char* p = lds + buf * SB;
-      f.sa = uint8_t(row_scale[kt * ld + srow]);
-      f.sb = uint8_t(unit_scale[at++]);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) f.sa[r] = uint8_t(row_scale[kt * swords + srow[r]]);
+      f.sb[0] = uint8_t(unit_scale[at]);
+      if (GLU) f.sb[GLU] = uint8_t(unit_scale[at + ks]);
+      ++at;
       kt = kt + 1 == ks ? 0 : kt + 1;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int c0 = ((4 * i + 2 * half) ^ lsw) * 16, c1 = c0 ^ 16;
-        f.a[i] = read32(p + abase, c0, c1);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) f.a[i][r] = read32(p + abase + r * 4096, c0, c1);
 #pragma unroll
         for (int j = 0; j < CT; ++j) f.b[i][j] = read32(p + bbase + j * 4096, c0, c1);
       }
@@ -140,7 +170,10 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < CT; ++j) sums[i][j] = mfma8<0, 0>(f.a[i], f.b[i][j], sums[i][j], f.sa, f.sb);
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int j = 0; j < CT; ++j)
+            sums[i % NA][r][j] = mfma8<0, 0>(f.a[i][r], f.b[i][j], sums[i % NA][r][j], f.sa[r], f.sb[GLU ? j : 0]);
       __builtin_amdgcn_sched_barrier(0);
     };
     fetch(f0);
@@ -158,20 +191,71 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
     } else {
       mma(f0);
     }
-    // this worker's part of the tile: plane (worker - first worker of the tile)
     const int nt = tile / m_tiles, mt = tile - nt * m_tiles;
+    if constexpr (WHOLE) {
+      // through LDS, so that a row's columns are written in runs (and, quantised, meet)
+      typedef std::conditional_t<OUT == kGluQuantOut, float, uint16_t> Value;
+      constexpr int COLS = GLU ? TN / 2 : TN, LDO = COLS + 16 / int(sizeof(Value));
+      static_assert(TM * LDO * sizeof(Value) <= NS * SB, "the tile fits the ring");
+      wait_vmem<0>();                                   // loads past the end land first
+      barrier_lds();
+      Value* room = reinterpret_cast<Value*>(lds);
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int j = 0; j < CT; j += GLU ? 2 : 1)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            float x = sums[0][r][j][e];
+            if constexpr (NA == 2) x += sums[1][r][j][e];
+            if constexpr (GLU) x = silu(x) * sums[0][r][j + 1][e];
+            const int row = (rt + r) * 32 + half * 4 + (e >> 2) * 8 + (e & 3);
+            const int col = (GLU ? ct / 2 + j / 2 : ct + j) * 32 + (lane & 31);
+            if constexpr (OUT == kGluQuantOut) room[row * LDO + col] = x;
+            else room[row * LDO + col] = uint16_t(pack_bf16x2(x, 0.0f));
+          }
+      barrier_lds();
+      const int cols = GLU ? ffn : g.N;
+      if constexpr (OUT == kGluQuantOut) {              // 32 lanes a row, one group
+        for (int i = tid; i < TM * 32; i += NW * 64) {
+          const int row = i >> 5, c = (i & 31) * 4, m = mt * TM + row;
+          const float4 v = *reinterpret_cast<const float4*>(room + row * LDO + c);
+          const int byte = scale_byte(half_max(max(max(finite_abs(v.x), finite_abs(v.y)), max(finite_abs(v.z), finite_abs(v.w)))));
+          if (m < g.M) {
+            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(g.out) + size_t(m) * cols + nt * COLS + c) =
+                pack_e4m3x4(v.x, v.y, v.z, v.w, byte);
+            if (c == 0) g.out_scale[size_t(nt) * ld + m] = uint8_t(byte);
+          }
+        }
+      } else {
+        constexpr int LR = COLS / 8;                    // lanes a row
+        for (int i = tid; i < TM * LR; i += NW * 64) {
+          const int row = i / LR, c = i % LR * 8, m = mt * TM + row;
+          if (m < g.M)
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(g.out) + size_t(m) * cols + nt * COLS + c) =
+                *reinterpret_cast<const uint4*>(room + row * LDO + c);
+        }
+      }
+      return;
+    }
+    // this worker's part of the tile: plane (worker - first worker of the tile)
     const int plane = wr - s.owner(tile * ks);
     const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
         g.partial + size_t(plane) * g.M * g.N, 0, g.M * g.N * 4, kBufWord3);   // rows past M: dropped
-    const int m0 = mt * TM + rt * 32 + half * 4, n = nt * TN + ct * 32 + (lane & 31);
+    const int n = nt * TN + ct * 32 + (lane & 31);
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+    for (int q = 0; q < RT; ++q) {
+      const int m0 = mt * TM + (rt + q) * 32 + half * 4;
 #pragma unroll
-      for (int j = 0; j < CT; ++j) {
-        const float x = sums[0][j][r] + sums[1][j][r];
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), ro,
-                                              ((m0 + (r >> 2) * 8 + (r & 3)) * g.N + n + j * 32) * 4, 0, 0);
-      }
+      for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int j = 0; j < CT; ++j) {
+          float x = sums[0][q][j][r];
+          if constexpr (NA == 2) x += sums[1][q][j][r];
+          __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), ro,
+                                                ((m0 + (r >> 2) * 8 + (r & 3)) * g.N + n + j * 32) * 4, 0, 0);
+        }
+    }
     ++tile;
   }
   wait_vmem<0>();                                       // no load may land in LDS after the workgroup ends
@@ -179,7 +263,7 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
 
 int cdiv(int a, int b) { return (a + b - 1) / b; }
 
-template <int TM, int TN, int NW, int CT, int NS>
+template <int TM, int TN, int RT, int CT, int NS>
 StreamSum launch_tm(const Gemm8Args& g, hipStream_t stream) {
   StreamSum s{};
   s.partial = g.partial;
@@ -189,8 +273,20 @@ StreamSum launch_tm(const Gemm8Args& g, hipStream_t stream) {
   s.ks = g.K / kBK;
   s.units = s.m_tiles * (g.N / TN) * s.ks;
   s.G = s.units < kWorkers * kMinUnits ? cdiv(s.units, kMinUnits) : kWorkers;
-  gemm8_stream_kernel<TM, TN, NW, CT, NS><<<s.G, NW * 64, 0, stream>>>(g, s);
+  gemm8_stream_kernel<kPlanesOut, TM, TN, RT, CT, NS><<<s.G, (TM / 32 / RT) * (TN / 32 / CT) * 64, 0, stream>>>(g, s);
   return s;
+}
+
+template <int OUT, int TM, int TN, int RT, int CT, int NS>
+void launch_whole(const Gemm8Args& g, hipStream_t stream) {
+  StreamSum s{};
+  s.M = g.M, s.N = g.N;
+  s.tm = TM, s.tn = TN;
+  s.m_tiles = cdiv(g.M, TM);
+  s.ks = g.K / kBK;
+  s.G = s.m_tiles * cdiv(g.N, TN);
+  s.units = s.G * s.ks;
+  gemm8_stream_kernel<OUT, TM, TN, RT, CT, NS><<<s.G, (TM / 32 / RT) * (TN / 32 / CT) * 64, 0, stream>>>(g, s);
 }
 
 }  // namespace
@@ -205,10 +301,31 @@ bool gemm8_stream_fits(int M, int N, int K) {
   return planes * M * N * 4 <= int64_t(kPartial8Bytes);
 }
 
+// Whole tiles of tm x tn, a workgroup each: what LDS has left holds the scales of so many stages.
+bool gemm8_narrow_fits(int N, int K, int epi, int tm, int tn) {
+  const int ks = K / kBK;
+  if (epi == kGluQuantOut ? tm != 64 || tn != 256 : tn > 128) return false;
+  return epi != kRopeOut && N % tn == 0 && ks * tm <= kRowScales && 2 * ks <= kUnitScales;
+}
+
+void launch_gemm8_narrow(const Gemm8Args& g, int epi, int tm, int tn, hipStream_t stream) {
+  if (epi == kGluQuantOut) {
+    launch_whole<kGluQuantOut, 64, 256, 2, 2, 3>(g, stream);
+  } else if (epi == kGluOut) {
+    if (tm == 64 && tn == 64) launch_whole<kGluOut, 64, 64, 1, 2, 9>(g, stream);
+    else if (tm == 64) launch_whole<kGluOut, 64, 128, 1, 2, 6>(g, stream);
+    else launch_whole<kGluOut, 128, 128, 2, 2, 4>(g, stream);
+  } else {
+    if (tm == 64 && tn == 64) launch_whole<kBf16Out, 64, 64, 1, 1, 9>(g, stream);
+    else if (tm == 64) launch_whole<kBf16Out, 64, 128, 1, 2, 6>(g, stream);
+    else launch_whole<kBf16Out, 128, 128, 2, 2, 4>(g, stream);
+  }
+}
+
 StreamSum launch_gemm8_stream(const Gemm8Args& g, hipStream_t stream) {
-  if (g.M <= 32) return launch_tm<32, 64, 2, 1, 11>(g, stream);
-  if (g.M <= 64) return launch_tm<64, 64, 4, 1, 9>(g, stream);
-  return launch_tm<128, 64, 8, 1, 6>(g, stream);
+  if (g.M <= 32) return launch_tm<32, 64, 1, 1, 11>(g, stream);
+  if (g.M <= 64) return launch_tm<64, 64, 1, 1, 9>(g, stream);
+  return launch_tm<128, 64, 1, 1, 6>(g, stream);
 }
 
 }  // namespace epic

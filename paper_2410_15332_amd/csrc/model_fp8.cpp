@@ -126,9 +126,11 @@ Gemm8Args product(const Rows8& a, const uint8_t* w, const uint8_t* sw, int m, in
 // The product, left pending for the norm that follows.
 Pending residual_product(Gemm8Args g, uint16_t* delta, hipStream_t stream) {
   const Gemm8Plan p = gemm8_plan(g.M, g.N, g.K, kBf16Out);
-  if (p.stream || p.parts > 1) return Pending{launch_gemm8_partial(g, p, stream), nullptr};
+  const bool whole = p.kind == Gemm8Kind::kWhole || p.kind == Gemm8Kind::kNarrow;
+  if (!whole) return Pending{launch_gemm8_partial(g, p, stream), nullptr};
   g.out = delta;
-  launch_gemm8_wide(g, kBf16Out, p.tm, stream);
+  if (p.kind == Gemm8Kind::kNarrow) launch_gemm8_narrow(g, kBf16Out, p.tm, p.tn, stream);
+  else launch_gemm8_wide(g, kBf16Out, p.tm, stream);
   return Pending{StreamSum{}, delta};
 }
 
@@ -164,7 +166,7 @@ epic_status run_layer(const epic_model_cfg* c, const epic_layer_weights_fp8* w, 
   Gemm8Args qkv = product(ws.x, w->wqkv, w->wqkv_scale, n, (hq + 2 * hkv) * D, H, ws.partial);
   qkv.q = ws.q, qkv.k = ws.k, qkv.v = ws.v, qkv.cs = ws.cs, qkv.hq = hq, qkv.hkv = hkv, qkv.head_dim = D;
   const Gemm8Plan qp = gemm8_plan(n, qkv.N, H, kRopeOut);
-  const bool partial = qp.stream || qp.parts > 1, write = partial && s->n_rerotated == 0;
+  const bool partial = qp.kind != Gemm8Kind::kWhole, write = partial && s->n_rerotated == 0;
   if (partial) {
     const StreamSum sum = launch_gemm8_partial(qkv, qp, stream);
     GemmArgs g{};

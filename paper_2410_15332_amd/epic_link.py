@@ -421,24 +421,50 @@ def fp8_block_scale_shape(n: int, k: int):
     return -(-n // FP8_GROUP), k // FP8_GROUP
 
 
-def _expect(name: str, t, shape, *dtypes):
-    """The 8-bit operators take packed tensors of the current device: others are refused."""
+_fp8_types = None
+
+
+def _dtypes():
+    """(bf16, fp32, what e4m3 values come in, what e8m0 scales come in); torch is imported late."""
+    global _fp8_types
+    if _fp8_types is None:
+        import torch
+
+        _fp8_types = ((torch.bfloat16,), (torch.float32,), (torch.uint8, torch.float8_e4m3fn),
+                      (torch.uint8, torch.float8_e8m0fnu))
+    return _fp8_types
+
+
+def _device_of(name: str, t) -> int:
+    """The device of a call's first tensor, which has to be the current one."""
     import torch
 
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"{name}: a tensor of the current GPU expected, got one of {t.device}")
+    return device
+
+
+def _expect(name: str, t, shape, dtypes, device: int) -> int:
+    """The address of an argument of the 8-bit operators, which take packed tensors of one device."""
     if t is None:
         raise ValueError(f"{name} is missing")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous {tuple(shape)} expected, got {tuple(t.shape)} with strides {t.stride()}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: {' or '.join(map(str, dtypes))} expected, got {t.dtype}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: a tensor of the current device expected, got {t.device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: expected on device {device}, got {t.device}")
+    return t.data_ptr()
 
 
-def _bytes_of(kind: str):
+def _raw_stream(stream, device: int) -> int:
+    """_stream() for calls of a few us: the current stream's handle without an object around it."""
+    if stream is not None:
+        return stream.cuda_stream
     import torch
 
-    return torch.uint8, getattr(torch, kind)
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def epic_fp8_scale_bytes(m: int, k: int) -> int:
@@ -449,32 +475,26 @@ def epic_quant_fp8(x, q, scale, block_rows: int = 1, stream=None):
     """Enqueue x bf16 [m, k] -> e4m3 values q [m, k] and e8m0 scales (see include/epic_link.h):
     rows (block_rows 1, scale fp8_row_scale_shape(m, k)) or weights (128,
     fp8_block_scale_shape(m, k)).  q and scale: uint8 or torch's 8-bit float types."""
-    import torch
-
+    bf16, _, e4m3, e8m0 = _dtypes()
+    dev = _device_of("x", x)
     m, k = x.shape
-    _expect("x", x, (m, k), torch.bfloat16)
-    _expect("q", q, (m, k), *_bytes_of("float8_e4m3fn"))
-    _expect("scale", scale, fp8_row_scale_shape(m, k) if block_rows == 1 else fp8_block_scale_shape(m, k),
-            *_bytes_of("float8_e8m0fnu"))
-    _check(_quant_fp8(_ptr(x), m, k, block_rows, _ptr(q), _ptr(scale), _stream(stream)), "epic_quant_fp8")
+    shape = fp8_row_scale_shape(m, k) if block_rows == 1 else fp8_block_scale_shape(m, k)
+    _check(_quant_fp8(_expect("x", x, (m, k), bf16, dev), m, k, block_rows, _expect("q", q, (m, k), e4m3, dev),
+                      _expect("scale", scale, shape, e8m0, dev), _raw_stream(stream, dev)), "epic_quant_fp8")
 
 
 def epic_rmsnorm_fp8(x, weight, eps: float, q, scale, delta=None, x_out=None, stream=None):
     """Enqueue s = x + delta, x_out = s (x itself or None are fine) and RMSNorm(s) weight -> q, scale
     as rows (see include/epic_link.h); x, x_out fp32, delta bf16 or None."""
-    import torch
-
-    m, hidden = x.shape
-    _expect("x", x, (m, hidden), torch.float32)
-    _expect("weight", weight, (hidden,), torch.bfloat16)
-    _expect("q", q, (m, hidden), *_bytes_of("float8_e4m3fn"))
-    _expect("scale", scale, fp8_row_scale_shape(m, hidden), *_bytes_of("float8_e8m0fnu"))
-    if delta is not None:
-        _expect("delta", delta, (m, hidden), torch.bfloat16)
-    if x_out is not None:
-        _expect("x_out", x_out, (m, hidden), torch.float32)
-    _check(_rmsnorm_fp8(_ptr(x), _ptr(delta), _ptr(weight), m, hidden, eps, _ptr(x_out), _ptr(q), _ptr(scale),
-                        _stream(stream)), "epic_rmsnorm_fp8")
+    bf16, f32, e4m3, e8m0 = _dtypes()
+    dev = _device_of("x", x)
+    m, hidden = rows = x.shape
+    _check(_rmsnorm_fp8(_expect("x", x, rows, f32, dev), None if delta is None else _expect("delta", delta, rows, bf16, dev),
+                        _expect("weight", weight, (hidden,), bf16, dev), m, hidden, eps,
+                        None if x_out is None else _expect("x_out", x_out, rows, f32, dev),
+                        _expect("q", q, rows, e4m3, dev),
+                        _expect("scale", scale, fp8_row_scale_shape(m, hidden), e8m0, dev), _raw_stream(stream, dev)),
+           "epic_rmsnorm_fp8")
 
 
 def epic_gemm_fp8_workspace_bytes() -> int:
@@ -485,21 +505,18 @@ def epic_gemm_fp8(epilogue: int, a, a_scale, w, w_scale, out, out_scale=None, wo
     """Enqueue the 8-bit projection GEMM (see include/epic_link.h): a [m, k] with row scales, w
     [n, k] with block scales; out bf16 [m, n] (FP8_BF16) or [m, n/2] (FP8_SWIGLU), or e4m3
     [m, n/2] with out_scale (FP8_SWIGLU_FP8)."""
-    import torch
-
+    bf16, _, e4m3, e8m0 = _dtypes()
+    dev = _device_of("a", a)
     (m, k), n = a.shape, w.shape[0]
-    e4m3, e8m0 = _bytes_of("float8_e4m3fn"), _bytes_of("float8_e8m0fnu")
-    _expect("a", a, (m, k), *e4m3)
-    _expect("w", w, (n, k), *e4m3)
-    _expect("a_scale", a_scale, fp8_row_scale_shape(m, k), *e8m0)
-    _expect("w_scale", w_scale, fp8_block_scale_shape(n, k), *e8m0)
-    _expect("out", out, (m, n if epilogue == FP8_BF16 else n // 2),
-            *(e4m3 if epilogue == FP8_SWIGLU_FP8 else (torch.bfloat16,)))
-    if epilogue == FP8_SWIGLU_FP8:
-        _expect("out_scale", out_scale, fp8_row_scale_shape(m, n // 2), *e8m0)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_gemm_fp8(epilogue, _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), m, n, k, _ptr(out), _ptr(out_scale),
-                     _ptr(workspace), ws_bytes, _stream(stream)), "epic_gemm_fp8")
+    quant = epilogue == FP8_SWIGLU_FP8
+    cols = n if epilogue == FP8_BF16 else n // 2
+    _check(_gemm_fp8(epilogue, _expect("a", a, (m, k), e4m3, dev),
+                     _expect("a_scale", a_scale, fp8_row_scale_shape(m, k), e8m0, dev), _expect("w", w, (n, k), e4m3, dev),
+                     _expect("w_scale", w_scale, fp8_block_scale_shape(n, k), e8m0, dev), m, n, k,
+                     _expect("out", out, (m, cols), e4m3 if quant else bf16, dev),
+                     _expect("out_scale", out_scale, fp8_row_scale_shape(m, cols), e8m0, dev) if quant else None,
+                     _ptr(workspace), 0 if workspace is None else workspace.nbytes, _raw_stream(stream, dev)),
+           "epic_gemm_fp8")
 
 
 def epic_model_fp8_workspace_bytes(cfg: epic_model_cfg, sizes: epic_plan_sizes) -> int:
