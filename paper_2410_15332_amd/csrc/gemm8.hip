@@ -68,25 +68,26 @@ double stream_time(int M, int N, int K) {
 
 // Whole tiles of tm x tn, a workgroup each: LDS traffic paces a stage (64 x 256: two stages in
 // flight do not cover the latency).  256 rows, N = K = 4096:
-// 64 x 64 13.9 us, 64 x 128 17.3 (split 128-row tiles 17.5); 501 rows: 25 and 18.4 (21.7);
-// SwiGLU of 100 rows, N 28672: 128 x 128 31.4 (streamed 42).
+// 64 x 64 13.3 us, 64 x 128 16 (split 128-row tiles 17.5); 501 rows: 25 and 17.1 (21.7);
+// SwiGLU of 100 rows, N 28672: 128 x 128 30.4 (streamed 42).
 double narrow_time(int M, int N, int K, int tm, int tn) {
-  const double rounds = cdiv(cdiv(M, tm) * (N / tn), kWorkers);
-  const double stage = tm == 128 ? 0.6 : tn == 64 ? 0.257 : tn == 128 ? 0.37 : 0.95;
+  const int tiles = cdiv(M, tm) * (N / tn);
+  const double rounds = cdiv(tiles, kWorkers), busy = std::max(tiles / rounds / kWorkers - 0.6, 0.0);
+  const double stage = (tm == 128 ? 0.56 : tn == 64 ? 0.24 : tn == 128 ? 0.35 : 0.66) * (1.0 + 0.5 * busy);
   const double run = rounds * (K / kGroup * stage) + (rounds - 1) * 4.0, read = read_time(M, N, K);
   return 4.5 + std::max(run, read) + 0.1 * std::min(run, read);
 }
 
 // 256-column tiles in equal parts of K: with more than half of the CUs at work a stage takes
 // longer (power, and what they read), and what W takes from memory hides only in part.
-// Planes: 2 us and 0.35 us a MB.  736 rows, K 14336, N 4096: 128-row tiles in 2 parts 62 us,
+// Planes: 2 us and 0.27 us a MB.  736 rows, K 14336, N 4096: 128-row tiles in 2 parts 62 us,
 // 256 in 4 56, whole 78; 200 rows of gate|up, N 28672: whole 128-row tiles 40, 256 47.
 double wide_time(int M, int N, int K, int tm, int parts) {
   const int work = cdiv(M, tm) * cdiv(N, 256) * parts;
   const double rounds = cdiv(work, kWorkers), busy = std::max(work / rounds / kWorkers - 0.5, 0.0);
   const double stage = tm == 256 ? 0.965 + busy : 0.685 + 0.4 * busy;
   const double run = rounds * (cdiv(K / kGroup, parts) * stage + (tm == 256 ? 6.0 : 3.6)), read = read_time(M, N, K);
-  return std::max(run, read) + 0.45 * std::min(run, read) + (parts > 1 ? 2.0 + 0.35e-6 * 4 * parts * M * N : 0.0);
+  return std::max(std::max(run, read) + 0.45 * std::min(run, read), 7.0) + (parts > 1 ? 2.0 + 0.27e-6 * 4 * parts * M * N : 0.0);
 }
 
 }  // namespace

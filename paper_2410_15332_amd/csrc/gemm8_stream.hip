@@ -37,10 +37,11 @@ constexpr int kRowScales = 14336, kUnitScales = 2048;   // bytes of LDS for them
 // kGluQuantOut for whole tiles: worker w has tile w, and stores its result itself (GLU: the
 // tile's columns are gate and up in turn, 32 each).
 constexpr int kPlanesOut = 4;
-template <int OUT, int TM, int TN, int RT, int CT, int NS>
+// KS = 2: two wavefronts share a place, each with half of every stage.
+template <int OUT, int TM, int TN, int RT, int CT, int KS, int NS>
 __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, StreamSum s) {
   constexpr bool WHOLE = OUT != kPlanesOut, GLU = OUT == kGluOut || OUT == kGluQuantOut;
-  constexpr int NW = (TM / 32 / RT) * (TN / 32 / CT);
+  constexpr int NW = (TM / 32 / RT) * (TN / 32 / CT) * KS;
   constexpr int NG = (TM + TN) / 8;                     // 1 KB row groups per stage
   constexpr int NL = NG / NW;                           // ... per wavefront
   static_assert(NG % NW == 0, "row groups per wavefront");
@@ -61,7 +62,8 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
   const int u0 = s.begin(wr), u1 = s.begin(wr + 1);
   if (u0 >= u1) return;
   constexpr int WC = TN / 32 / CT;                      // wavefronts along N
-  const int rt = wv / WC * RT, ct = wv % WC * CT;       // first row block, first column block
+  const int place = wv / KS, kh = wv % KS;
+  const int rt = place / WC * RT, ct = place % WC * CT;   // first row block, first column block
   const int ffn = g.N / 2;
 
   // ---- loads: row group gi of a stage, A rows first
@@ -131,7 +133,8 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
   while (u < u1) {
     const int ue = min(u1, (tile + 1) * ks);
     // a chain of additions for each half of a stage where a wavefront has one tile
-    constexpr int NA = RT * CT == 1 ? 2 : 1;
+    constexpr int NA = RT * CT * KS == 1 ? 2 : 1;
+    constexpr int NH = 2 / KS;                          // halves of a stage per wavefront
     f32x16 sums[NA][RT][CT];
 #pragma unroll
     for (int i = 0; i < NA; ++i)
@@ -141,7 +144,7 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
         for (int j = 0; j < CT; ++j) sums[i][r][j] = f32x16{};
     // unit u is read while unit u - 1 is on the matrix cores
     struct Frags {
-      i32x8 a[2][RT], b[2][CT];
+      i32x8 a[NH][RT], b[NH][CT];
       int sa[RT], sb[GLU ? 2 : 1];
     } f0, f1;
     auto fetch = [&](Frags& f) __attribute__((always_inline)) {
@@ -156,8 +159,8 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       ++at;
       kt = kt + 1 == ks ? 0 : kt + 1;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int c0 = ((4 * i + 2 * half) ^ lsw) * 16, c1 = c0 ^ 16;
+      for (int i = 0; i < NH; ++i) {
+        const int c0 = ((4 * (KS == 2 ? kh : i) + 2 * half) ^ lsw) * 16, c1 = c0 ^ 16;
 #pragma unroll
         for (int r = 0; r < RT; ++r) f.a[i][r] = read32(p + abase + r * 4096, c0, c1);
 #pragma unroll
@@ -168,7 +171,7 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
     };
     auto mma = [&](const Frags& f) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < NH; ++i)
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -200,20 +203,34 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       wait_vmem<0>();                                   // loads past the end land first
       barrier_lds();
       Value* room = reinterpret_cast<Value*>(lds);
+      if constexpr (KS == 2) {                          // the two halves meet
+        constexpr int ROOM = (TM * LDO * int(sizeof(Value)) + 1023) / 1024 * 1024;
+        static_assert(ROOM + TM * TN * 4 <= NS * SB, "the sums fit beside the tile");
+        float* sum = reinterpret_cast<float*>(lds + ROOM) + place * RT * CT * 1024 + lane;
 #pragma unroll
-      for (int r = 0; r < RT; ++r)
+        for (int x = 0; x < RT * CT * 16; ++x)
+          if (kh == 1) sum[x * 64] = sums[0][x / 16 / CT][x / 16 % CT][x % 16];
+        barrier_lds();
 #pragma unroll
-        for (int j = 0; j < CT; j += GLU ? 2 : 1)
+        for (int x = 0; x < RT * CT * 16; ++x)
+          if (kh == 0) sums[0][x / 16 / CT][x / 16 % CT][x % 16] += sum[x * 64];
+      }
+      if (kh == 0) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float x = sums[0][r][j][e];
-            if constexpr (NA == 2) x += sums[1][r][j][e];
-            if constexpr (GLU) x = silu(x) * sums[0][r][j + 1][e];
-            const int row = (rt + r) * 32 + half * 4 + (e >> 2) * 8 + (e & 3);
-            const int col = (GLU ? ct / 2 + j / 2 : ct + j) * 32 + (lane & 31);
-            if constexpr (OUT == kGluQuantOut) room[row * LDO + col] = x;
-            else room[row * LDO + col] = uint16_t(pack_bf16x2(x, 0.0f));
-          }
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int j = 0; j < CT; j += GLU ? 2 : 1)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float x = sums[0][r][j][e];
+              if constexpr (NA == 2) x += sums[1][r][j][e];
+              if constexpr (GLU) x = silu(x) * sums[0][r][j + 1][e];
+              const int row = (rt + r) * 32 + half * 4 + (e >> 2) * 8 + (e & 3);
+              const int col = (GLU ? ct / 2 + j / 2 : ct + j) * 32 + (lane & 31);
+              if constexpr (OUT == kGluQuantOut) room[row * LDO + col] = x;
+              else room[row * LDO + col] = uint16_t(pack_bf16x2(x, 0.0f));
+            }
+      }
       barrier_lds();
       const int cols = GLU ? ffn : g.N;
       if constexpr (OUT == kGluQuantOut) {              // 32 lanes a row, one group
@@ -263,7 +280,7 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
 
 int cdiv(int a, int b) { return (a + b - 1) / b; }
 
-template <int TM, int TN, int RT, int CT, int NS>
+template <int TM, int TN, int NS>
 StreamSum launch_tm(const Gemm8Args& g, hipStream_t stream) {
   StreamSum s{};
   s.partial = g.partial;
@@ -273,11 +290,11 @@ StreamSum launch_tm(const Gemm8Args& g, hipStream_t stream) {
   s.ks = g.K / kBK;
   s.units = s.m_tiles * (g.N / TN) * s.ks;
   s.G = s.units < kWorkers * kMinUnits ? cdiv(s.units, kMinUnits) : kWorkers;
-  gemm8_stream_kernel<kPlanesOut, TM, TN, RT, CT, NS><<<s.G, (TM / 32 / RT) * (TN / 32 / CT) * 64, 0, stream>>>(g, s);
+  gemm8_stream_kernel<kPlanesOut, TM, TN, 1, 1, 1, NS><<<s.G, (TM / 32) * (TN / 32) * 64, 0, stream>>>(g, s);
   return s;
 }
 
-template <int OUT, int TM, int TN, int RT, int CT, int NS>
+template <int OUT, int TM, int TN, int RT, int CT, int KS, int NS>
 void launch_whole(const Gemm8Args& g, hipStream_t stream) {
   StreamSum s{};
   s.M = g.M, s.N = g.N;
@@ -286,7 +303,7 @@ void launch_whole(const Gemm8Args& g, hipStream_t stream) {
   s.ks = g.K / kBK;
   s.G = s.m_tiles * cdiv(g.N, TN);
   s.units = s.G * s.ks;
-  gemm8_stream_kernel<OUT, TM, TN, RT, CT, NS><<<s.G, (TM / 32 / RT) * (TN / 32 / CT) * 64, 0, stream>>>(g, s);
+  gemm8_stream_kernel<OUT, TM, TN, RT, CT, KS, NS><<<s.G, (TM / 32 / RT) * (TN / 32 / CT) * KS * 64, 0, stream>>>(g, s);
 }
 
 }  // namespace
@@ -310,22 +327,22 @@ bool gemm8_narrow_fits(int N, int K, int epi, int tm, int tn) {
 
 void launch_gemm8_narrow(const Gemm8Args& g, int epi, int tm, int tn, hipStream_t stream) {
   if (epi == kGluQuantOut) {
-    launch_whole<kGluQuantOut, 64, 256, 2, 2, 3>(g, stream);
+    launch_whole<kGluQuantOut, 64, 256, 1, 2, 1, 3>(g, stream);
   } else if (epi == kGluOut) {
-    if (tm == 64 && tn == 64) launch_whole<kGluOut, 64, 64, 1, 2, 9>(g, stream);
-    else if (tm == 64) launch_whole<kGluOut, 64, 128, 1, 2, 6>(g, stream);
-    else launch_whole<kGluOut, 128, 128, 2, 2, 4>(g, stream);
+    if (tm == 64 && tn == 64) launch_whole<kGluOut, 64, 64, 1, 2, 2, 9>(g, stream);
+    else if (tm == 64) launch_whole<kGluOut, 64, 128, 1, 2, 2, 6>(g, stream);
+    else launch_whole<kGluOut, 128, 128, 1, 2, 1, 4>(g, stream);
   } else {
-    if (tm == 64 && tn == 64) launch_whole<kBf16Out, 64, 64, 1, 1, 9>(g, stream);
-    else if (tm == 64) launch_whole<kBf16Out, 64, 128, 1, 2, 6>(g, stream);
-    else launch_whole<kBf16Out, 128, 128, 2, 2, 4>(g, stream);
+    if (tm == 64 && tn == 64) launch_whole<kBf16Out, 64, 64, 1, 1, 2, 9>(g, stream);
+    else if (tm == 64) launch_whole<kBf16Out, 64, 128, 1, 1, 1, 6>(g, stream);
+    else launch_whole<kBf16Out, 128, 128, 1, 2, 1, 4>(g, stream);
   }
 }
 
 StreamSum launch_gemm8_stream(const Gemm8Args& g, hipStream_t stream) {
-  if (g.M <= 32) return launch_tm<32, 64, 1, 1, 11>(g, stream);
-  if (g.M <= 64) return launch_tm<64, 64, 1, 1, 9>(g, stream);
-  return launch_tm<128, 64, 1, 1, 6>(g, stream);
+  if (g.M <= 32) return launch_tm<32, 64, 11>(g, stream);
+  if (g.M <= 64) return launch_tm<64, 64, 9>(g, stream);
+  return launch_tm<128, 64, 6>(g, stream);
 }
 
 }  // namespace epic

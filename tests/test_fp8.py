@@ -140,3 +140,23 @@ def route(epi, m, n, k):
 def test_every_size_has_a_kernel(m, n, k):
     for epi in range(3):
         assert route(epi, m, n, k) != ""
+
+
+def test_gpu_cases_take_the_kernels_they_name():
+    import test_gpu_fp8 as gpu
+    for (m, n, k), kernels in gpu.ROUTES:
+        assert tuple(route(e, m, n, k) for e in range(3)) == kernels, (m, n, k)
+    seen = {name for _, kernels in gpu.ROUTES for name in kernels}
+    assert seen == {"few", "stream", "narrow64x64", "narrow64x128", "narrow128x128", "narrow64x256", "whole128", "whole256",
+                    "split128", "split256"}
+
+
+def test_plans_keep_within_what_they_need():
+    """Planes fit the workspace, whatever the sizes."""
+    rng = np.random.default_rng(9)
+    for _ in range(3000):
+        m, n, k = (int(np.exp(rng.uniform(0, np.log(hi)))) for hi in (5000, 200, 130))
+        n, k = 256 * n, 128 * k
+        for e in range(3):
+            name = route(e, m, n, k)
+            assert name and (name != "few" or m <= 32) and (name != "stream" or m <= 128)

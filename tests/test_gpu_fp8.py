@@ -129,7 +129,9 @@ def _check_rounded(q, t, y, e):
     """Bytes q and exponents t against values y known to within e (elementwise), by the bars above."""
     m, k = y.shape
     top, slack = fp8.group_top(y), fp8.group_top(np.broadcast_to(e, y.shape))
-    lo, hi = fp8.scale_exponent(np.maximum(top - slack, 0.0)), fp8.scale_exponent(top + slack)
+    # (a maximum of 0 has t = 0, which is not the limit of small ones: nothing is known below then)
+    lo = np.where(top > slack, fp8.scale_exponent(np.maximum(top - slack, 0.0)), -127)
+    hi = np.maximum(fp8.scale_exponent(top + slack), np.where(top > slack, -127, 0))
     assert np.all((t >= lo) & (t <= hi)), "scale"
     step = np.ldexp(1.0, fp8.spread(t, m, k))
     bar = np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * step) * (1 + 2.0 ** -4) + e
@@ -261,11 +263,14 @@ def _silu(x):
     return x / (1 + np.exp(-x))
 
 
-def _check_gemm(epi, m, n, k, seed=0):
-    rng = np.random.default_rng([m, n, k, seed])
+def _check_gemm(epi, m, n, k, sample=None):
+    """sample: so many rows, the first, the last and others, are compared."""
+    rng = np.random.default_rng([m, n, k])
     qa, ta, qw, tw = _operands(rng, m, n, k)
-    y, e = _products(fp8.dequantise(qa, ta), fp8.dequantise(qw, tw, 128))
+    at = np.arange(m) if sample is None else np.unique(np.r_[0, m - 1, rng.integers(0, m, sample)])
+    y, e = _products(fp8.dequantise(qa[at], ta[at]), fp8.dequantise(qw, tw, 128))
     got = _run_gemm(epi, qa, ta, qw, tw)
+    got = tuple(x[at] for x in got) if epi == "swiglu_fp8" else got[at]
     if epi != "bf16":
         gate, up, eg, eu = y[:, :n // 2], y[:, n // 2:], e[:, :n // 2], e[:, n // 2:]
         y = _silu(gate) * up
@@ -298,6 +303,32 @@ SHAPES = [(1, 256, 128), (4, 256, 14336), (17, 2304, 256), (33, 768, 1920), (100
 def test_gemm_shapes(m, n, k, epi):
     _say("gemm shapes", m, n, k, epi)
     _check_gemm(epi, m, n, k)
+
+
+# (m, n, k), and the kernel that runs each epilogue (checked without a GPU in test_fp8.py): whole
+# and cut tiles of every kind, one and several rounds, odd numbers of K stages
+ROUTES = [
+    ((5, 512, 640), ("few", "few", "few")), ((16, 768, 1152), ("few", "few", "few")),
+    ((29, 512, 1920), ("few", "few", "stream")), ((20, 256, 8192), ("stream", "stream", "stream")),
+    ((60, 2048, 4096), ("stream", "stream", "stream")), ((100, 2048, 4096), ("stream", "stream", "stream")),
+    ((90, 1024, 640), ("narrow64x64", "narrow64x64", "whole128")),
+    ((257, 768, 1152), ("narrow64x64", "narrow64x64", "split128")),
+    ((129, 6144, 1152), ("narrow64x128", "narrow64x128", "whole128")),
+    ((150, 12288, 640), ("narrow128x128", "narrow128x128", "whole128")),
+    ((77, 12288, 1152), ("narrow64x128", "narrow64x128", "narrow64x256")),
+    ((520, 8192, 1152), ("whole128", "whole128", "whole128")),
+    ((2049, 4096, 384), ("whole256", "whole256", "whole256")),
+    ((4200, 8192, 640), ("whole256", "whole256", "whole256")),
+    ((300, 2048, 8192), ("split128", "split128", "split128")), ((150, 512, 8192), ("split128", "split128", "split128")),
+    ((700, 4096, 14336), ("split256", "split256", "split256")),
+]
+
+
+@pytest.mark.parametrize("epi", list(EPI))
+@pytest.mark.parametrize("shape,kernels", ROUTES, ids=lambda x: "x".join(map(str, x)) if isinstance(x[0], int) else None)
+def test_gemm_every_kernel(shape, kernels, epi):
+    _say("gemm kernel", *shape, epi, kernels[EPI[epi]])
+    _check_gemm(epi, *shape, sample=None if shape[0] * shape[1] * shape[2] < 1 << 30 else 40)
 
 
 @pytest.mark.parametrize("m,n,k", [(7, 128, 128), (70, 384, 256), (200, 128, 512), (300, 1408, 384)])
@@ -356,3 +387,183 @@ def test_gemm_nan_stays_in_its_row_and_column(m):
     bad = np.zeros(got.shape, bool)
     bad[m // 2], bad[:, 17] = True, True
     assert np.all(np.isnan(got[bad])) and np.array_equal(got[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("m", [9, 90, 300])
+def test_gemm_swiglu_of_infinities_and_nan(m):
+    """Sums that overflow fp32: e4m3 has no infinities, so they become NaN, and the other values of
+    their group keep the scale that they have without them."""
+    _say("gemm swiglu overflow", m)
+    rng = np.random.default_rng(m)
+    n, k = 512, 640
+    qa, ta, qw, tw = _operands(rng, m, n, k)
+    clean = _run_gemm("swiglu_fp8", qa, ta, qw, tw)
+    bad = m // 3
+    ta = ta.copy()
+    ta[bad] = 110                                           # gate and up of about 2^110: their product overflows
+    ta[0] = 127
+    qa[0], qa[m - 1, 3] = 0x7E, 0x7F                        # +448 * 2^127 already overflows; a NaN row
+    q, t = _run_gemm("swiglu_fp8", qa, ta, qw, tw)
+    assert np.all((q[m - 1] & 0x7F) == 0x7F) and np.all(t[m - 1] == 0)
+    assert np.any((q[bad] & 0x7F) == 0x7F)
+    same = np.setdiff1d(np.arange(m), [0, bad, m - 1])
+    assert np.array_equal(q[same], clean[0][same]) and np.array_equal(t[same], clean[1][same])
+
+
+# ---------------------------------------------------------------- together, and as a program calls them
+
+def _mlp(el, x, delta, norm, wgu, sgu, wd, sd, bufs):
+    """A decoder layer's MLP half on the public calls: bufs holds every result and the workspace."""
+    el.epic_rmsnorm_fp8(x, norm, EPS, bufs["q"], bufs["s"], delta=delta, x_out=bufs["x"])
+    el.epic_gemm_fp8(el.FP8_SWIGLU_FP8, bufs["q"], bufs["s"], wgu, sgu, bufs["act"], out_scale=bufs["acts"], workspace=bufs["ws"])
+    el.epic_gemm_fp8(el.FP8_BF16, bufs["act"], bufs["acts"], wd, sd, bufs["out"], workspace=bufs["ws"])
+    el.epic_rmsnorm_fp8(bufs["x"], norm, EPS, bufs["q2"], bufs["s2"], delta=bufs["out"], x_out=bufs["x2"])
+
+
+def _mlp_bufs(el, m, h, f):
+    u8 = lambda *s: torch.empty(s, dtype=torch.uint8, device="cuda")  # noqa: E731
+    return {"q": u8(m, h), "s": u8(*el.fp8_row_scale_shape(m, h)), "x": torch.empty(m, h, device="cuda"),
+            "act": u8(m, f), "acts": u8(*el.fp8_row_scale_shape(m, f)), "ws": u8(el.epic_gemm_fp8_workspace_bytes()),
+            "out": torch.empty(m, h, dtype=torch.bfloat16, device="cuda"), "q2": u8(m, h),
+            "s2": u8(*el.fp8_row_scale_shape(m, h)), "x2": torch.empty(m, h, device="cuda")}
+
+
+def _mlp_inputs(el, rng, m, h, f):
+    x = torch.from_numpy(rng.normal(size=(m, h)).astype(np.float32)).cuda()
+    delta, norm = _bf16(0.5 * rng.normal(size=(m, h))).cuda(), _bf16(1 + 0.1 * rng.normal(size=h)).cuda()
+    out = [x, delta, norm]
+    for n, k in ((2 * f, h), (h, f)):
+        w = _bf16(rng.normal(size=(n, k)) / np.sqrt(k)).cuda()
+        q = torch.empty(n, k, dtype=torch.uint8, device="cuda")
+        s = torch.empty(el.fp8_block_scale_shape(n, k), dtype=torch.uint8, device="cuda")
+        el.epic_quant_fp8(w, q, s, block_rows=128)
+        out += [q, s]
+    return out
+
+
+@pytest.mark.parametrize("m", [1, 30, 100, 260])
+def test_mlp_of_a_layer(m):
+    """The calls in the order of a decoder layer against the same steps in float64.  The steps before a
+    rounding to e4m3 agree to 2^-8 at worst, so of its steps (2^-3 at most) that share goes
+    the other way: sqrt(2^-8 * 2^-3) rms after the SwiGLU, once more after the product: 6%."""
+    _say("mlp", m)
+    el = _el()
+    rng = np.random.default_rng(m)
+    h, f = 512, 1024
+    args, bufs = _mlp_inputs(el, rng, m, h, f), _mlp_bufs(el, m, h, f)
+    _mlp(el, *args, bufs)
+    torch.cuda.synchronize()
+    x, delta, norm, wgu, sgu, wd, sd = (t.double().cpu().numpy() if t.dtype != torch.uint8 else t.cpu().numpy() for t in args)
+    w1, w2 = fp8.dequantise(wgu, sgu.astype(int) - 127, 128), fp8.dequantise(wd, sd.astype(int) - 127, 128)
+    s = x + delta
+    gu = fp8.rows(s / np.sqrt(np.mean(s * s, -1, keepdims=True) + EPS) * norm) @ w1.T
+    out = fp8.rows(_silu(gu[:, :f]) * gu[:, f:]) @ w2.T
+    got = bufs["x2"].double().cpu().numpy()
+    assert np.linalg.norm(got - (s + out)) <= 0.06 * np.linalg.norm(out)
+    assert np.array_equal(bufs["x2"].cpu().numpy(), (bufs["x"] + bufs["out"].float()).cpu().numpy())
+
+
+def _results(bufs):
+    return {k: v.clone() for k, v in bufs.items() if k not in ("ws", "s", "acts", "s2")}
+
+
+@pytest.mark.parametrize("m", [3, 100, 300])
+def test_replays_and_streams(m):
+    """A captured run replayed with eager work between, and two runs in flight at a time on streams of
+    their own (each with its workspace): the same bits as a run alone."""
+    _say("replays", m)
+    el = _el()
+    h, f = 1024, 2048
+    args = [_mlp_inputs(el, np.random.default_rng([m, i]), m, h, f) for i in range(2)]
+    bufs = [_mlp_bufs(el, m, h, f) for _ in range(2)]
+    ref = []
+    for a, b in zip(args, bufs):
+        _mlp(el, *a, b)
+        torch.cuda.synchronize()
+        ref.append(_results(b))
+    side = [torch.cuda.Stream() for _ in range(2)]
+    for s in side:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for s, a, b in zip(side, args, bufs):
+            with torch.cuda.stream(s):
+                _mlp(el, *a, b)
+    torch.cuda.synchronize()
+    for r, b in zip(ref, bufs):
+        assert all(torch.equal(r[k], b[k]) for k in r)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _mlp(el, *args[0], bufs[0])
+    for _ in range(3):
+        for k in ref[0]:
+            bufs[0][k].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(ref[0][k], bufs[0][k]) for k in ref[0])
+        _mlp(el, *args[1], bufs[0])                         # eager work on the same buffers
+        torch.cuda.synchronize()
+
+
+def test_stream_argument():
+    el = _el()
+    x = _bf16(np.random.default_rng(1).normal(size=(6, 256))).cuda()
+    q, s = torch.zeros(6, 256, dtype=torch.uint8, device="cuda"), torch.zeros(2, 8, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    el.epic_quant_fp8(x, q, s, stream=side)
+    side.synchronize()
+    assert np.array_equal(q.cpu().numpy(), fp8.quantise(x.double().cpu().numpy())[0])
+
+
+def test_offsets_past_31_bits():
+    """More than 2^31 values: the last rows come out as on their own."""
+    _say("large offsets")
+    el = _el()
+    m, k = 270001, 8192
+    x = torch.empty(m, k, dtype=torch.bfloat16, device="cuda").normal_()
+    q, s = torch.empty(m, k, dtype=torch.uint8, device="cuda"), torch.empty(el.fp8_row_scale_shape(m, k), dtype=torch.uint8, device="cuda")
+    el.epic_quant_fp8(x, q, s)
+    torch.cuda.synchronize()
+    for rows in (slice(0, 3), slice(262143, 262146), slice(m - 3, m)):
+        rq, rt = fp8.quantise(x[rows].double().cpu().numpy())
+        assert np.array_equal(q[rows].cpu().numpy(), rq)
+        assert np.array_equal(s[:, rows].cpu().numpy().T.astype(int) - 127, rt)
+    f = x.float()
+    del x
+    w = torch.ones(k, dtype=torch.bfloat16, device="cuda")
+    el.epic_rmsnorm_fp8(f, w, EPS, q, s)
+    torch.cuda.synchronize()
+    for rows in (slice(0, 3), slice(262143, 262146), slice(m - 3, m)):
+        y = _normed(f[rows].double().cpu().numpy(), torch.ones(k))
+        _check_rounded(q[rows].cpu().numpy(), s[:, rows].cpu().numpy().T.astype(int) - 127, y, 2.0 ** -20 * np.abs(y))
+
+
+def test_binding_refuses_what_the_kernels_cannot_read():
+    """Other types, shapes, strides and devices: ValueError before any launch."""
+    el = _el()
+    x = torch.zeros(4, 256, dtype=torch.bfloat16, device="cuda")
+    u8 = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda")  # noqa: E731
+    q, s, w, sw, ws = u8(4, 256), u8(2, 4), u8(256, 256), u8(2, 2), u8(el.epic_gemm_fp8_workspace_bytes())
+    out = torch.zeros(4, 256, dtype=torch.bfloat16, device="cuda")
+    quant, gemm = dict(x=x, q=q, scale=s), dict(epilogue=el.FP8_BF16, a=q, a_scale=s, w=w, w_scale=sw, out=out, workspace=ws)
+    norm = dict(x=x.float(), weight=x[0].contiguous(), eps=EPS, q=q, scale=s)
+    el.epic_quant_fp8(**quant), el.epic_gemm_fp8(**gemm), el.epic_rmsnorm_fp8(**norm)
+    for call, good, bad in (
+            (el.epic_quant_fp8, quant, dict(x=x.float())), (el.epic_quant_fp8, quant, dict(x=u8(256, 4).t().bfloat16())),
+            (el.epic_quant_fp8, quant, dict(x=x.cpu())), (el.epic_quant_fp8, quant, dict(q=q.cpu())),
+            (el.epic_quant_fp8, quant, dict(q=q[:, :128])), (el.epic_quant_fp8, quant, dict(q=q.to(torch.int8))),
+            (el.epic_quant_fp8, quant, dict(scale=u8(2, 3))), (el.epic_quant_fp8, quant, dict(scale=None)),
+            (el.epic_rmsnorm_fp8, norm, dict(x=x)), (el.epic_rmsnorm_fp8, norm, dict(weight=x[0, :128])),
+            (el.epic_rmsnorm_fp8, norm, dict(delta=x.float())), (el.epic_rmsnorm_fp8, norm, dict(delta=x[:2])),
+            (el.epic_rmsnorm_fp8, norm, dict(x_out=x)), (el.epic_rmsnorm_fp8, norm, dict(q=u8(8, 256)[::2])),
+            (el.epic_gemm_fp8, gemm, dict(a=u8(4, 128))), (el.epic_gemm_fp8, gemm, dict(a_scale=u8(4, 2).t())),
+            (el.epic_gemm_fp8, gemm, dict(w=w.t())), (el.epic_gemm_fp8, gemm, dict(w_scale=u8(2, 1))),
+            (el.epic_gemm_fp8, gemm, dict(out=out.float())), (el.epic_gemm_fp8, gemm, dict(out=out[:, :128])),
+            (el.epic_gemm_fp8, gemm, dict(epilogue=el.FP8_SWIGLU)),
+            (el.epic_gemm_fp8, gemm, dict(epilogue=el.FP8_SWIGLU_FP8, out=u8(4, 128)))):
+        with pytest.raises(ValueError):
+            call(**{**good, **bad})
+    for bad in (dict(workspace=None), dict(workspace=ws[:-1]), dict(epilogue=7, out=u8(4, 128).bfloat16())):
+        with pytest.raises(el.EpicError):
+            el.epic_gemm_fp8(**{**gemm, **bad})
+    torch.cuda.synchronize()
