@@ -95,10 +95,10 @@ extern "C" epic_status epic_gemm_fp8(int32_t epilogue, const uint8_t* a, const u
   return hip_status("8-bit GEMM launch");
 }
 
-// The kernel that a product of these sizes runs, or "" for sizes that are refused.  Host only and
+// The kernel that a product of these sizes runs (epilogue: Gemm8Epilogue, kRopeOut too), or "" for sizes that are refused.  Host only and
 // not in the public header: it is for tests, each of which is about one kernel.
 extern "C" const char* epic_gemm_fp8_route_name(int32_t epilogue, int32_t m, int32_t n, int32_t k) {
-  if (epilogue < kBf16Out || epilogue > kGluQuantOut || m <= 0 || n <= 0 || k <= 0 || n % kGroup != 0 || k % kGroup != 0)
+  if (epilogue < kBf16Out || epilogue > kRopeOut || m <= 0 || n <= 0 || k <= 0 || n % kGroup != 0 || k % kGroup != 0)
     return "";
   const Gemm8Plan p = gemm8_plan(m, n, k, epilogue);
   if (p.kind == Gemm8Kind::kFew) return "few";

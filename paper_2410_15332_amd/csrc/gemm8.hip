@@ -94,7 +94,7 @@ double wide_time(int M, int N, int K, int tm, int parts) {
 
 Gemm8Plan gemm8_plan(int M, int N, int K, int epi) {
   Gemm8Plan best{Gemm8Kind::kWhole, 256, 256, 1};
-  double time = wide_time(M, N, K, 256, 1);
+  double time = 1e30;                                   // whole tiles run every size
   auto consider = [&](const Gemm8Plan& p, double t) {
     if (t < time) best = p, time = t;
   };
@@ -109,7 +109,9 @@ Gemm8Plan gemm8_plan(int M, int N, int K, int epi) {
       const int64_t work = int64_t(cdiv(M, tm)) * cdiv(N, 256) * parts;
       if (parts > 1 && (work > kWorkers || int64_t(parts) * M * N * 4 > int64_t(kPartial8Bytes) || K / kGroup / parts < 2))
         break;
-      consider(Gemm8Plan{parts == 1 ? Gemm8Kind::kWhole : Gemm8Kind::kSplit, tm, 256, parts}, wide_time(M, N, K, tm, parts));
+      // whole Q|K|V tiles leave the link write to a launch of its own
+      consider(Gemm8Plan{parts == 1 ? Gemm8Kind::kWhole : Gemm8Kind::kSplit, tm, 256, parts},
+               wide_time(M, N, K, tm, parts) + (epi == kRopeOut && parts == 1 ? 3.0 : 0.0));
     }
   return best;
 }

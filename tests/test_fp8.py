@@ -151,6 +151,14 @@ def test_gpu_cases_take_the_kernels_they_name():
                     "split128", "split256"}
 
 
+def test_model_cases_take_the_kernels_they_name():
+    import oracle
+    import test_gpu_fp8_model as gpu
+    for wl, kernel in zip(gpu.CASES, gpu.QKV):
+        rows = len(oracle.legolink_positions(wl.chunk_lens, wl.suffix_len, wl.k))
+        assert route(3, rows, (wl.num_q_heads + 2 * wl.num_kv_heads) * wl.head_dim, wl.hidden) == kernel, wl.name
+
+
 def test_plans_keep_within_what_they_need():
     """Planes fit the workspace, whatever the sizes."""
     rng = np.random.default_rng(9)
