@@ -33,7 +33,7 @@ extern "C" epic_status epic_quant_fp8(const uint16_t* x, int32_t m, int32_t k, i
   EPIC_CHECK_ARG(m >= 0 && k > 0, "m, k = %d, %d", m, k);
   EPIC_CHECK_ARG(block_rows == 1 || block_rows == kGroup, "block_rows %d (expected 1 or %d)", block_rows, kGroup);
   if (k % kGroup != 0) return fail(EPIC_ERR_UNSUPPORTED, "k %d must be a multiple of %d", k, kGroup);
-  if (m > INT32_MAX - 4 || int64_t(m) * k / kGroup > INT32_MAX || (block_rows == kGroup && m > 65535 * kGroup))
+  if (m > INT32_MAX - 4 || int64_t(m) * k / 8 > kMaxThreads || (block_rows == kGroup && m > 65535 * kGroup))
     return fail(EPIC_ERR_UNSUPPORTED, "%d x %d values are too many", m, k);
   if (m == 0) return EPIC_OK;
   EPIC_CHECK_ARG(x && q && scale, "NULL tensor argument");
@@ -52,7 +52,8 @@ extern "C" epic_status epic_rmsnorm_fp8(const float* x, const uint16_t* delta, c
   EPIC_CHECK_ARG(eps > 0.0f, "eps must be > 0");
   if (hidden % kGroup != 0 || hidden > kMaxNormHidden)
     return fail(EPIC_ERR_UNSUPPORTED, "hidden %d must be a multiple of %d, at most %d", hidden, kGroup, kMaxNormHidden);
-  if (m > INT32_MAX - 4) return fail(EPIC_ERR_UNSUPPORTED, "%d rows are too many", m);
+  if (m > INT32_MAX - 4 || int64_t(m) * norm_threads(hidden) > kMaxThreads)
+    return fail(EPIC_ERR_UNSUPPORTED, "%d rows of %d are too many", m, hidden);
   if (m == 0) return EPIC_OK;
   EPIC_CHECK_ARG(x && weight && q && scale, "NULL tensor argument");
   EPIC_CHECK_ARG(aligned(x, 16) && aligned(weight, 16) && aligned(q, 16) && aligned(delta, 16) && aligned(x_out, 16),

@@ -17,6 +17,10 @@ constexpr int kMaxNormHidden = 32768;                   // longest row of the 8-
 // GEMM tile's come in one load per K stage; padded so that four rows are one aligned load.
 inline int scale_ld(int m) { return (m + 3) & ~3; }
 
+// Threads of a launch have to stay below 2^32: 8 values a thread, norm_threads() a row.
+constexpr int64_t kMaxThreads = (int64_t(1) << 32) - 1024;
+inline int norm_threads(int hidden) { return hidden > 4 * 8 * 512 ? 1024 : hidden >= 4 * 512 ? 512 : (hidden / 4 + 63) / 64 * 64; }
+
 void launch_quant_rows(const uint16_t* x, int m, int k, uint8_t* q, uint8_t* scale, hipStream_t stream);
 void launch_quant_blocks(const uint16_t* x, int m, int k, uint8_t* q, uint8_t* scale, hipStream_t stream);
 // x + delta (bf16 [m][hidden]) or + the planes of s, where one is given, into x_out (where not

@@ -69,6 +69,7 @@ def _gemm(epi=0, a=P, sa=P, w=P, sw=P, m=4, n=256, k=128, out=P, ss=P, ws=P, siz
     (dict(x=None), INVALID), (dict(q=None), INVALID), (dict(scale=None), INVALID), (dict(x=P + 8), INVALID),
     (dict(q=P + 4), INVALID), (dict(k=64), UNSUPPORTED), (dict(k=192), UNSUPPORTED),
     (dict(m=(1 << 31) - 1, k=128), UNSUPPORTED), (dict(m=1 << 30, k=1024), UNSUPPORTED),
+    (dict(m=1 << 28, k=128), UNSUPPORTED),
     (dict(m=65536 * 128, rows=128), UNSUPPORTED)])
 def test_quant_refuses(kw, status):
     assert _quant(**kw) == status
@@ -79,7 +80,8 @@ def test_quant_refuses(kw, status):
     (dict(m=-1), INVALID), (dict(k=0), INVALID), (dict(eps=0.0), INVALID),
     (dict(eps=float("nan")), INVALID), (dict(x=None), INVALID), (dict(w=None), INVALID),
     (dict(q=None), INVALID), (dict(scale=None), INVALID), (dict(out=P + 4), INVALID), (dict(delta=P + 8), INVALID),
-    (dict(k=130), UNSUPPORTED), (dict(k=32768 + 128), UNSUPPORTED), (dict(m=(1 << 31) - 1), UNSUPPORTED)])
+    (dict(k=130), UNSUPPORTED), (dict(k=32768 + 128), UNSUPPORTED), (dict(m=(1 << 31) - 1), UNSUPPORTED),
+    (dict(m=1 << 23, k=4096), UNSUPPORTED)])
 def test_norm_refuses(kw, status):
     assert _norm(**kw) == status
     assert el._last_error()
