@@ -106,6 +106,6 @@ extern "C" const char* epic_gemm_fp8_route_name(int32_t epilogue, int32_t m, int
   if (p.kind == Gemm8Kind::kStream) return "stream";
   if (p.kind == Gemm8Kind::kNarrow)
     return p.tm == 128 ? "narrow128x128" : p.tn == 256 ? "narrow64x256" : p.tn == 128 ? "narrow64x128" : "narrow64x64";
-  if (p.kind == Gemm8Kind::kSplit) return p.tm == 256 ? "split256" : "split128";
-  return p.tm == 256 ? "whole256" : "whole128";
+  if (p.kind == Gemm8Kind::kSplit) return p.tm == 256 ? "split256" : p.tm == 192 ? "split192" : "split128";
+  return p.tm == 256 ? "whole256" : p.tm == 192 ? "whole192" : "whole128";
 }

@@ -85,9 +85,9 @@ double narrow_time(int M, int N, int K, int tm, int tn) {
 double wide_time(int M, int N, int K, int tm, int parts) {
   const int work = cdiv(M, tm) * cdiv(N, 256) * parts;
   const double rounds = cdiv(work, kWorkers), busy = std::max(work / rounds / kWorkers - 0.5, 0.0);
-  const double stage = tm == 256 ? 0.965 + busy : 0.685 + 0.4 * busy;
-  const double run = rounds * (cdiv(K / kGroup, parts) * stage + (tm == 256 ? 6.0 : 3.6)), read = read_time(M, N, K);
-  return std::max(std::max(run, read) + 0.45 * std::min(run, read), 7.0) + (parts > 1 ? 2.0 + 0.27e-6 * 4 * parts * M * N : 0.0);
+  const double stage = tm == 256 ? 0.965 + busy : tm == 192 ? 0.82 + 0.7 * busy : 0.685 + 0.4 * busy;
+  const double run = rounds * (cdiv(K / kGroup, parts) * stage + (tm == 256 ? 6.0 : tm == 192 ? 4.8 : 3.6)), read = read_time(M, N, K);
+  return std::max(std::max(run, read) + 0.45 * std::min(run, read), 3.0 + tm / 32.0) + (parts > 1 ? 2.0 + 0.27e-6 * 4 * parts * M * N : 0.0);
 }
 
 }  // namespace
@@ -104,7 +104,7 @@ Gemm8Plan gemm8_plan(int M, int N, int K, int epi) {
   for (const auto& t : kNarrow)
     if (gemm8_narrow_fits(N, K, epi, t[0], t[1]))
       consider(Gemm8Plan{Gemm8Kind::kNarrow, t[0], t[1], 0}, narrow_time(M, N, K, t[0], t[1]));
-  for (const int tm : {256, 128})
+  for (const int tm : {256, 192, 128})
     for (int parts = 1; parts <= 16; ++parts) {
       const int64_t work = int64_t(cdiv(M, tm)) * cdiv(N, 256) * parts;
       if (parts > 1 && (work > kWorkers || int64_t(parts) * M * N * 4 > int64_t(kPartial8Bytes) || K / kGroup / parts < 2))

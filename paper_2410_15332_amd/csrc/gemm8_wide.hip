@@ -1,4 +1,4 @@
-// 8-bit GEMMs of more rows: C[M x N] = A[M x K] . W[N x K]^T on tiles of 256 or 128 rows x
+// 8-bit GEMMs of more rows: C[M x N] = A[M x K] . W[N x K]^T on tiles of 256, 192 or 128 rows x
 // 256 columns, one workgroup of four wavefronts per CU, epilogues fused.
 //
 // A stage is 128 of K, which are 128 bytes of a row, as 64 of K are in the bf16 kernel
@@ -171,11 +171,19 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
   // the last ones loaded, in the types loaded: widened here, they would be waited for here
   struct Loaded {
     std::conditional_t<I == 4, uint32_t, uint16_t> a;
+    uint8_t a1, a2;                                     // I == 3
     uint8_t w, u;
   } sc2;
   auto load_scales = [&](Loaded& s) __attribute__((always_inline)) {
-    if constexpr (I == 4) s.a = __builtin_amdgcn_raw_buffer_load_b32(rsc, vsa, cs.kt * ld, 0);
-    else s.a = __builtin_amdgcn_raw_buffer_load_b16(rsc, vsa, cs.kt * ld, 0);
+    if constexpr (I == 4) {
+      s.a = __builtin_amdgcn_raw_buffer_load_b32(rsc, vsa, cs.kt * ld, 0);
+    } else if constexpr (I == 2) {
+      s.a = __builtin_amdgcn_raw_buffer_load_b16(rsc, vsa, cs.kt * ld, 0);
+    } else {                                            // any alignment: three bytes
+      s.a = __builtin_amdgcn_raw_buffer_load_b8(rsc, vsa, cs.kt * ld, 0);
+      s.a1 = __builtin_amdgcn_raw_buffer_load_b8(rsc, vsa + 1, cs.kt * ld, 0);
+      s.a2 = __builtin_amdgcn_raw_buffer_load_b8(rsc, vsa + 2, cs.kt * ld, 0);
+    }
     s.w = __builtin_amdgcn_raw_buffer_load_b8(rsd, vsw, cs.kt, 0);
     if constexpr (GLU) s.u = __builtin_amdgcn_raw_buffer_load_b8(rsd, vsu, cs.kt, 0);
     if (advance(cs)) setup_s();
@@ -184,6 +192,10 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
   // front of the next stage's sync() and wait for them
   auto take = [&](Scales& to, const Loaded& from) __attribute__((always_inline)) {
     __asm__ volatile("v_mov_b32 %0, %1" : "=v"(to.a) : "v"(int(from.a)));
+    if constexpr (I == 3) {
+      __asm__ volatile("v_lshl_or_b32 %0, %1, 8, %0" : "+v"(to.a) : "v"(int(from.a1)));
+      __asm__ volatile("v_lshl_or_b32 %0, %1, 16, %0" : "+v"(to.a) : "v"(int(from.a2)));
+    }
     __asm__ volatile("v_mov_b32 %0, %1" : "=v"(to.w) : "v"(int(from.w)));
     if constexpr (GLU) __asm__ volatile("v_mov_b32 %0, %1" : "=v"(to.u) : "v"(int(from.u)));
   };
@@ -254,7 +266,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
   for (int i = 0; i < NLA; ++i) dma_a(i);
 #pragma unroll
   for (int i = 0; i < NLB; ++i) dma_b(i);
-  wait_vmem<NLA + NLB + (GLU ? 3 : 2)>();               // stage 0
+  wait_vmem<NLA + NLB + (I == 3 ? 4 : 2) + (GLU ? 1 : 0)>();   // stage 0
   __asm__ volatile("s_barrier" ::: "memory");
   take(sc0, first);
 #pragma unroll
@@ -367,8 +379,15 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       const int first = mw + er * I;
       if (wn == 0 && eh == 0 && first < g.M) {        // I neighbouring rows; those past M are padding
         uint8_t* to = g.out_scale + size_t(nt) * ld + first;
-        if constexpr (I == 4) *reinterpret_cast<uint32_t*>(to) = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
-        else *reinterpret_cast<uint16_t*>(to) = uint16_t(byte[0] | byte[1] << 8);
+        if constexpr (I == 4) {
+          *reinterpret_cast<uint32_t*>(to) = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
+        } else if constexpr (I == 2) {
+          *reinterpret_cast<uint16_t*>(to) = uint16_t(byte[0] | byte[1] << 8);
+        } else {
+#pragma unroll
+          for (int i = 0; i < I; ++i)
+            if (first + i < g.M) to[i] = uint8_t(byte[i]);
+        }
       }
       barrier_lds();
       const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(g.out, 0, g.M * ffn, kBufWord3);
@@ -491,6 +510,7 @@ void launch_wide_tm(const Gemm8Args& g, int epi, hipStream_t stream) {
 
 void launch_gemm8_wide(const Gemm8Args& g, int epi, int tm, hipStream_t stream) {
   if (tm == 256) launch_wide_tm<256>(g, epi, stream);
+  else if (tm == 192) launch_wide_tm<192>(g, epi, stream);
   else launch_wide_tm<128>(g, epi, stream);
 }
 
@@ -502,6 +522,7 @@ StreamSum launch_gemm8_split(const Gemm8Args& g, int tm, int parts, hipStream_t 
   s.partial = g.partial;
   s.M = g.M, s.N = g.N, s.fixed = parts;
   if (tm == 256) gemm8_wide_kernel<kPlanesOut, 256><<<p.G, 256, 0, stream>>>(g, p);
+  else if (tm == 192) gemm8_wide_kernel<kPlanesOut, 192><<<p.G, 256, 0, stream>>>(g, p);
   else gemm8_wide_kernel<kPlanesOut, 128><<<p.G, 256, 0, stream>>>(g, p);
   return s;
 }

@@ -149,8 +149,8 @@ def test_gpu_cases_take_the_kernels_they_name():
     for (m, n, k), kernels in gpu.ROUTES:
         assert tuple(route(e, m, n, k) for e in range(3)) == kernels, (m, n, k)
     seen = {name for _, kernels in gpu.ROUTES for name in kernels}
-    assert seen == {"few", "stream", "narrow64x64", "narrow64x128", "narrow128x128", "narrow64x256", "whole128", "whole256",
-                    "split128", "split256"}
+    assert seen == {"few", "stream", "narrow64x64", "narrow64x128", "narrow128x128", "narrow64x256", "whole128", "whole192",
+                    "whole256", "split128", "split192", "split256"}
 
 
 def test_model_cases_take_the_kernels_they_name():

@@ -317,10 +317,13 @@ ROUTES = [
     ((150, 12288, 640), ("narrow128x128", "narrow128x128", "whole128")),
     ((77, 12288, 1152), ("narrow64x128", "narrow64x128", "narrow64x256")),
     ((520, 8192, 1152), ("whole128", "whole128", "whole128")),
-    ((2049, 4096, 384), ("whole256", "whole256", "whole256")),
-    ((4200, 8192, 640), ("whole256", "whole256", "whole256")),
+    ((2049, 4096, 384), ("whole192", "whole192", "whole192")),
+    ((4200, 8192, 640), ("whole192", "whole192", "whole192")),
+    ((2049, 6144, 384), ("whole256", "whole256", "whole256")),
+    ((4600, 12288, 384), ("whole256", "whole256", "whole256")),
     ((300, 2048, 8192), ("split128", "split128", "split128")), ((150, 512, 8192), ("split128", "split128", "split128")),
-    ((700, 4096, 14336), ("split256", "split256", "split256")),
+    ((700, 4096, 14336), ("split192", "split192", "split192")),
+    ((1165, 3584, 11008), ("split256", "split256", "split256")),
 ]
 
 

@@ -39,10 +39,12 @@ CASES = [
     _wl("whole_d128", [700, 300], 250, 250, hidden=256, ffn=768, hq=4, hkv=2, d=128),
     _wl("whole_d64", [700, 300], 250, 250, hidden=384, ffn=512, hq=6, hkv=3),
     _wl("whole_crossing_heads", [400, 200], 150, 200, hidden=256, ffn=512, hq=2, hkv=1),
-    _wl("whole256_d128", [64], 2049, 0, hidden=384, ffn=512, hq=16, hkv=8, d=128, layers=1),
-    _wl("whole256_d64", [30], 2049, 0, hidden=384, ffn=512, hq=32, hkv=16, layers=1),
+    _wl("whole192_d128", [64], 2049, 0, hidden=384, ffn=512, hq=16, hkv=8, d=128, layers=1),
+    _wl("whole192_d64", [30], 2049, 0, hidden=384, ffn=512, hq=32, hkv=16, layers=1),
+    _wl("whole256_d128", [64], 2049, 0, hidden=384, ffn=512, hq=32, hkv=8, d=128, layers=1),
+    _wl("whole256_d64", [30], 2049, 0, hidden=384, ffn=512, hq=64, hkv=16, layers=1),
 ]
-QKV = ["stream", "stream", "few", "split128", "whole128", "whole128", "whole128", "whole256", "whole256"]
+QKV = ["stream", "stream", "few", "split128", "whole128", "whole128", "whole128", "whole192", "whole192", "whole256", "whole256"]
 
 
 def _stage(wl, **kw):
