@@ -98,7 +98,8 @@ Gemm8Plan gemm8_plan(int M, int N, int K, int epi) {
   auto consider = [&](const Gemm8Plan& p, double t) {
     if (t < time) best = p, time = t;
   };
-  if (M <= 32) consider(Gemm8Plan{Gemm8Kind::kFew, 0, 0, 0}, few_time(M, N, K, epi));
+  if (M <= 32 && int64_t(M) * N * 4 <= int64_t(kPartial8Bytes))   // one plane, where it is needed
+    consider(Gemm8Plan{Gemm8Kind::kFew, 0, 0, 0}, few_time(M, N, K, epi));
   if (gemm8_stream_fits(M, N, K)) consider(Gemm8Plan{Gemm8Kind::kStream, 0, 0, 0}, stream_time(M, N, K));
   constexpr int kNarrow[][2] = {{64, 64}, {64, 128}, {128, 128}, {64, 256}};
   for (const auto& t : kNarrow)

@@ -162,11 +162,17 @@ def test_model_cases_take_the_kernels_they_name():
 
 
 def test_plans_keep_within_what_they_need():
-    """Planes fit the workspace, whatever the sizes."""
+    """Row limits of the short-row kernels; and no planes where they would not fit the workspace."""
     rng = np.random.default_rng(9)
     for _ in range(3000):
         m, n, k = (int(np.exp(rng.uniform(0, np.log(hi)))) for hi in (5000, 200, 130))
         n, k = 256 * n, 128 * k
-        for e in range(3):
+        for e in range(4):
             name = route(e, m, n, k)
             assert name and (name != "few" or m <= 32) and (name != "stream" or m <= 128)
+    for m in (1, 16, 32, 33, 128, 500):
+        for n in (1 << 19, 1 << 20, 1 << 23):
+            for e in range(4):
+                name = route(e, m, n, 128)
+                planes = {"few": 1, "stream": 2}.get(name, 2 if name.startswith("split") else 0)
+                assert planes * 4 * m * n <= 64 << 20, (m, n, name)

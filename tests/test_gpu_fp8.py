@@ -321,6 +321,8 @@ ROUTES = [
     ((4200, 8192, 640), ("whole192", "whole192", "whole192")),
     ((2049, 6144, 384), ("whole256", "whole256", "whole256")),
     ((4600, 12288, 384), ("whole256", "whole256", "whole256")),
+    ((9000, 8192, 128), ("whole192", "whole192", "whole192")), ((4500, 6144, 128), ("whole256", "whole256", "whole256")),
+    ((2000, 8192, 128), ("whole128", "whole128", "whole128")),
     ((300, 2048, 8192), ("split128", "split128", "split128")), ((150, 512, 8192), ("split128", "split128", "split128")),
     ((700, 4096, 14336), ("split192", "split192", "split192")),
     ((1165, 3584, 11008), ("split256", "split256", "split256")),
@@ -505,6 +507,39 @@ def test_replays_and_streams(m):
         assert all(torch.equal(ref[0][k], bufs[0][k]) for k in ref[0])
         _mlp(el, *args[1], bufs[0])                         # eager work on the same buffers
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("epi", list(EPI))
+@pytest.mark.parametrize("m", [1, 32, 60])
+def test_gemm_of_very_many_columns(m, epi):
+    """2^20 columns, where partial sums of few rows would pass the workspace."""
+    _say("many columns", m, epi)
+    el = _el()
+    n, k = 1 << 20, 128
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m)
+    a = torch.randint(-8, 9, (m, k), device="cuda", generator=g).float().to(torch.float8_e4m3fn)
+    w = torch.randint(-8, 9, (n, k), device="cuda", generator=g).float().to(torch.float8_e4m3fn)
+    sa = torch.full(el.fp8_row_scale_shape(m, k), 127, dtype=torch.uint8, device="cuda")
+    sw = torch.full((n // 128, 1), 120, dtype=torch.uint8, device="cuda")
+    ws, gw = _guarded((el.epic_gemm_fp8_workspace_bytes(),))
+    out, go = _guarded((m, n if epi == "bf16" else n // 2), torch.uint8 if epi == "swiglu_fp8" else torch.bfloat16)
+    ss, gs = _guarded(el.fp8_row_scale_shape(m, n // 2)) if epi == "swiglu_fp8" else (None, gw)
+    el.epic_gemm_fp8(EPI[epi], a, sa, w, sw, out, out_scale=ss, workspace=ws)
+    torch.cuda.synchronize()
+    _untouched(gw, go, gs)
+    y = a.double() @ (w.double() * 2.0 ** -7).t().contiguous()      # integers over 2^7: exact
+    if epi != "bf16":
+        y = y[:, :n // 2] / (1 + torch.exp(-y[:, :n // 2])) * y[:, n // 2:]
+    if epi == "swiglu_fp8":
+        t = ss[:, :m].t().long() - 127
+        step = torch.exp2(t.double())[..., None]
+        off = (out.view(torch.float8_e4m3fn).double().view(m, -1, 128) * step - y.view(m, -1, 128)).abs()
+        assert bool((off <= (2.0 ** -4 + 2.0 ** -18) * y.view(m, -1, 128).abs() + 2.0 ** -10 * step).all())
+    elif epi == "bf16":
+        assert torch.equal(out, y.to(torch.bfloat16))
+    else:
+        assert bool(((out.double() - y).abs() <= (2.0 ** -8 + 2.0 ** -18) * y.abs()).all())
 
 
 def test_stream_argument():
