@@ -417,7 +417,8 @@ epic_status epic_rmsnorm_fp8(const float* x, const uint16_t* delta, const uint16
  *          EPIC_FP8_SWIGLU_FP8: the same as rows, out e4m3 [m][n/2] and out_scale (else unused)
  * Sums are fp32, but the matrix cores drop what lies more than 13 bits below the largest
  * product of eight neighbouring t (all with t / 8 alike): 1.5e-5 to 4e-5 of a result, below
- * what its rounding to bf16 or e4m3 costs.
+ * what its rounding to bf16 or e4m3 costs.  Where the largest value of a group of the
+ * quantised result is within 2^-12 of where its scale changes, its 64-bit sum decides.
  * Shapes: m >= 0, k % 128 == 0, n % 128 == 0 (SwiGLU: n % 256 == 0), and with m rounded up
  * to a multiple of 256 every operand and a bf16 [m][n] below 2^31 bytes; else
  * EPIC_ERR_UNSUPPORTED.  workspace: epic_gemm_fp8_workspace_bytes() bytes, 256-byte

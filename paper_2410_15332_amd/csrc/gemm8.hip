@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "gemm8.h"
+#include "gemm8_device.h"
 #include "quant.h"
 #include "quant_device.h"
 
@@ -30,17 +31,25 @@ __global__ __launch_bounds__(256) void finish_kernel(StreamSum s, uint16_t* __re
 }
 
 // SwiGLU of summed planes, quantised: four columns per thread, 32 lanes a group.
-__global__ __launch_bounds__(256) void finish_quant_kernel(StreamSum s, uint8_t* __restrict__ out,
-                                                           uint8_t* __restrict__ scale, int ffn, int ld) {
+__global__ __launch_bounds__(256) void finish_quant_kernel(StreamSum s, Gemm8Args args) {
+  __shared__ Border<4, 8> list;
+  if (threadIdx.x == 0) list.count = 0;
+  barrier_lds();
+  const int ffn = args.N / 2, ld = (args.M + 3) & ~3;
   const int n4 = ffn / 4;
   const int idx = blockIdx.x * 256 + threadIdx.x;
   const int m = idx / n4, n = (idx - m * n4) * 4;
-  if (m >= s.M) return;                                 // whole half wavefronts: ffn % 128 == 0
-  const float4 g = s.sum4(m, n), u = s.sum4(m, ffn + n);
-  const float a = silu(g.x) * u.x, b = silu(g.y) * u.y, c = silu(g.z) * u.z, d = silu(g.w) * u.w;
-  const int byte = scale_byte(half_max(max(max(finite_abs(a), finite_abs(b)), max(finite_abs(c), finite_abs(d)))));
-  *reinterpret_cast<uint32_t*>(out + size_t(m) * ffn + n) = pack_e4m3x4(a, b, c, d, byte);
-  if ((threadIdx.x & 31) == 0) scale[size_t(n >> 7) * ld + m] = uint8_t(byte);
+  const bool live = m < s.M;                            // the same in a half wavefront: ffn % 128 == 0
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (live) {
+    const float4 g = s.sum4(m, n), u = s.sum4(m, ffn + n);
+    v = make_float4(silu(g.x) * u.x, silu(g.y) * u.y, silu(g.z) * u.z, silu(g.w) * u.w);
+  }
+  const uint32_t top = half_max(max(max(finite_abs(v.x), finite_abs(v.y)), max(finite_abs(v.z), finite_abs(v.w))));
+  const int byte = group_byte(list, args, top, v, m, n, live);
+  if (!live) return;
+  *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(args.out) + size_t(m) * ffn + n) = pack_e4m3x4(v.x, v.y, v.z, v.w, byte);
+  if ((threadIdx.x & 31) == 0) args.out_scale[size_t(n >> 7) * ld + m] = uint8_t(byte);
 }
 
 int cdiv(int a, int b) { return (a + b - 1) / b; }
@@ -129,7 +138,7 @@ void launch_gemm8_finish(const StreamSum& s, const Gemm8Args& g, int epi, hipStr
   uint16_t* out = static_cast<uint16_t*>(g.out);
   if (epi == kBf16Out) finish_kernel<false><<<grid, 256, 0, stream>>>(s, out, cols);
   else if (epi == kGluOut) finish_kernel<true><<<grid, 256, 0, stream>>>(s, out, cols);
-  else finish_quant_kernel<<<grid, 256, 0, stream>>>(s, static_cast<uint8_t*>(g.out), g.out_scale, cols, scale_ld(g.M));
+  else finish_quant_kernel<<<grid, 256, 0, stream>>>(s, g);
 }
 
 void launch_gemm8(const Gemm8Args& g, int epi, hipStream_t stream) {

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
   static_assert(NG % NW == 0, "row groups per wavefront");
   static_assert(!GLU || CT == 2, "a wavefront holds the gate and up of its columns");
   static_assert(TN <= (GLU ? 256 : 128), "one weight scale per unit (GLU: two)");
-  static_assert(OUT != kGluQuantOut || TN == 256, "a tile has whole groups of the result");
+  static_assert(OUT != kGluQuantOut || (TN == 256 && TM * 32 % (NW * 64) == 0), "a tile has whole groups of the result");
   constexpr int SB = (TM + TN) * 128;                   // operand bytes per stage
   // One array: with several, the compiler sees that reads of the scales cannot be told from
   // the loads in flight to LDS, and has every stage wait for all of them.
@@ -203,6 +203,11 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       wait_vmem<0>();                                   // loads past the end land first
       barrier_lds();
       Value* room = reinterpret_cast<Value*>(lds);
+      typedef Border<NW, NW * 2> List;                  // kGluQuantOut: one for each pass over the tile's groups
+      constexpr int LISTS = (TM * LDO * int(sizeof(Value)) + 1023) / 1024 * 1024, PASSES = TM * 32 / (NW * 64);
+      static_assert(OUT != kGluQuantOut || LISTS + PASSES * int(sizeof(List)) <= NS * SB, "the lists fit beside the tile");
+      List* lists = reinterpret_cast<List*>(lds + LISTS);
+      if (OUT == kGluQuantOut && tid < PASSES) lists[tid].count = 0;
       if constexpr (KS == 2) {                          // the two halves meet
         constexpr int ROOM = (TM * LDO * int(sizeof(Value)) + 1023) / 1024 * 1024;
         static_assert(ROOM + TM * TN * 4 <= NS * SB, "the sums fit beside the tile");
@@ -237,7 +242,8 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
         for (int i = tid; i < TM * 32; i += NW * 64) {
           const int row = i >> 5, c = (i & 31) * 4, m = mt * TM + row;
           const float4 v = *reinterpret_cast<const float4*>(room + row * LDO + c);
-          const int byte = scale_byte(half_max(max(max(finite_abs(v.x), finite_abs(v.y)), max(finite_abs(v.z), finite_abs(v.w)))));
+          const uint32_t top = half_max(max(max(finite_abs(v.x), finite_abs(v.y)), max(finite_abs(v.z), finite_abs(v.w))));
+          const int byte = group_byte(lists[i / (NW * 64)], g, top, v, m, nt * COLS + c, m < g.M);
           if (m < g.M) {
             *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(g.out) + size_t(m) * cols + nt * COLS + c) =
                 pack_e4m3x4(v.x, v.y, v.z, v.w, byte);

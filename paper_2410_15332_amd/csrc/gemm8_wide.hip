@@ -352,15 +352,55 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
         }
       }
       float* tops = reinterpret_cast<float*>(room);     // [wm][wn][i][32]
+      int* pick = reinterpret_cast<int*>(room) + 4 * I * 32 + wm * I * 32;   // [wm][i][32]
+      typedef Border<4, TM> List;
+      static_assert(4096 + sizeof(List) <= SLOT, "the list fits behind them");
+      List& list = *reinterpret_cast<List*>(room + 4096);
+      if (tid == 0) list.count = 0;
 #pragma unroll
       for (int i = 0; i < I; ++i)
         if (eh == 0) tops[(wv * I + i) * 32 + er] = top[i];
       barrier_lds();
       int byte[I];
+      bool near = false, mine[I];                       // mine: the largest is one of this wavefront's columns
 #pragma unroll
-      for (int i = 0; i < I; ++i) byte[i] = scale_byte(__float_as_uint(fmaxf(top[i], tops[((wv ^ 1) * I + i) * 32 + er])));
-      barrier_lds();                                    // the maxima are read
-      const int row0 = wm * (TM / 2) + er * I;  // of the tile
+      for (int i = 0; i < I; ++i) {
+        const float other = tops[((wv ^ 1) * I + i) * 32 + er];
+        mine[i] = wn == 0 ? top[i] >= other : top[i] > other;
+        top[i] = fmaxf(top[i], other);
+        byte[i] = scale_byte(__float_as_uint(top[i]));
+        near |= near_border(__float_as_uint(top[i]));
+      }
+      if (__any(near)) {                                // next to a border (Border): the same for both wn
+#pragma unroll
+        for (int i = 0; i < I; ++i) {                   // the first column that has it
+          int col = 64;
+#pragma unroll
+          for (int j = J - 2; j >= 0; j -= 2) {
+            from_here(i, j, 1);
+#pragma unroll
+            for (int r = 15; r >= 0; --r)
+              col = fabsf(acc[i][j][r]) == top[i] ? j * 16 + (r >> 2) * 8 + eh * 4 + (r & 3) : col;
+          }
+          col = min(col, __shfl_xor(col, 32));
+          if (mine[i] && eh == 0 && near_border(__float_as_uint(top[i])))
+            pick[i * 32 + er] = list.add(min(mw + er * I + i, g.M - 1), nt * (kTN / 2) + wn * 64 + col);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      barrier_lds();
+      const int again = list.count;
+      if (again > 0) {
+        list.compute(g, again, wv, el);
+        barrier_lds();
+        if (__any(near)) {
+#pragma unroll
+          for (int i = 0; i < I; ++i)
+            if (near_border(__float_as_uint(top[i]))) byte[i] = list.byte(pick[i * 32 + er], __float_as_uint(top[i]));
+        }
+      }
+      barrier_lds();                                    // the maxima and bytes are read
+      const int row0 = wm * (TM / 2) + er * I;          // of the tile
 #pragma unroll
       for (int i = 0; i < I; ++i) {
 #pragma unroll

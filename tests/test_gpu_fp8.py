@@ -336,6 +336,41 @@ def test_gemm_every_kernel(shape, kernels, epi):
     _check_gemm(epi, *shape, sample=None if shape[0] * shape[1] * shape[2] < 1 << 30 else 40)
 
 
+# a size for each way a quantised result is finished
+BORDERS = [(16, 768, 1152), (29, 512, 1920), (100, 2048, 4096), (77, 12288, 1152), (300, 2048, 8192), (520, 8192, 1152),
+           (2049, 4096, 384), (2049, 6144, 384)]
+
+
+@pytest.mark.parametrize("m,n,k", BORDERS, ids=lambda x: str(x))
+def test_scales_at_their_borders(m, n, k):
+    """Rows picked for a group whose largest value is next to where its scale changes, nearer than the
+    matrix cores' dropped bits: the scales are float64's all the same.  (float64 sums and silu are within
+    2^-53 (k + 8) < 2e-12 of the sum of magnitudes, some 1e2 of the result; rows nearer than 1e-9 are left out.)"""
+    _say("gemm borders", m, n, k)
+    gen = torch.Generator("cuda").manual_seed(m + n + k)
+    every = 1 << 16                                         # rows to pick from
+    draw = lambda *shape: torch.randn(shape, device="cuda", generator=gen)
+    qa, qw = draw(every, k).to(torch.float8_e4m3fn), draw(n, k).to(torch.float8_e4m3fn)
+    ta = torch.randint(-2, 3, (every, k // 128), device="cuda", generator=gen)
+    tw = torch.randint(-1, 2, (n // 128, k // 128), device="cuda", generator=gen) - int(np.log2(k) / 2)
+    w = (qw.double().view(n // 128, 128, k // 128, 128) * torch.exp2(tw.double())[:, None, :, None]).view(n, k).t().contiguous()
+    tops = []
+    for r in range(0, every, 4096):
+        a = (qa[r:r + 4096].double().view(4096, k // 128, 128) * torch.exp2(ta[r:r + 4096].double())[..., None]).view(4096, k)
+        gate, up = (a @ w).split(n // 2, 1)
+        tops.append((gate / (1 + torch.exp(-gate)) * up).abs().view(4096, n // 256, 128).amax(-1))
+    top = torch.cat(tops)
+    far = torch.log2(top / 1.75)
+    far = ((far - torch.round(far)).abs()).amin(-1)
+    order = torch.argsort(far)
+    at = order[far[order] > 1e-9][:m]
+    # 2^16 n / 256 groups, evenly spread over [0, 1/2): 16 of them this near at n = 512
+    assert float(far[at[0]]) < 2.0 ** -14
+    top, t = top[at].cpu().numpy(), ta[at].cpu().numpy()
+    _, got = _run_gemm("swiglu_fp8", qa[at].view(torch.uint8).cpu().numpy(), t, qw.view(torch.uint8).cpu().numpy(), tw.cpu().numpy())
+    assert np.array_equal(got, fp8.scale_exponent(top))
+
+
 @pytest.mark.parametrize("m,n,k", [(7, 128, 128), (70, 384, 256), (200, 128, 512), (300, 1408, 384)])
 def test_gemm_odd_block_counts(m, n, k):
     """n a multiple of 128 but not of 256."""
