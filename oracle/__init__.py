@@ -16,6 +16,8 @@ Contents
   model.py  -- Llama-style decoder layer for the selected rows, the compile step
                (Sec. 2.2), the full-model link step, and the layer's row-set
                projections on their own.
+  fp8.py    -- the 8-bit operands: rounding to e4m3 with power-of-two scales, and
+               the decoder layer with its projections on them.
 
 Pins (tests/test_oracle_pins.py) tie each function to something other than
 itself: library causal attention (FR = full prefill, Sec. 2.3), the Naive

@@ -4,9 +4,10 @@
 //
 // Sums are fp32, but the matrix cores form an 8-bit dot product of eight neighbouring values
 // first, and drop what lies more than 13 bits below the exponent of its largest product
-// (so for every 8-bit instruction; measured).  That leaves 1.5e-5 to 4e-5 of a result,
+// (so for every 8-bit instruction; measured).  That leaves 1.5e-5 to 4e-5 of a result's norm,
 // far below the 2^-4 that the operands were rounded by, and a hundredth of what rounding
-// to bf16 costs: hence results are bf16 or e4m3, and none is fp32.
+// to bf16 costs: hence results are bf16 or e4m3, and none is fp32;
+// the scales of the quantised ones are decided in 64 bits next to their borders (gemm8_device.h).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -42,7 +43,7 @@ constexpr size_t kPartial8Bytes = size_t(64) << 20;
 
 // How a product runs: up to 32 rows in one launch (kFew), weights streamed past a short row
 // set (kStream), whole tiles of 64 or 128 rows and columns (kNarrow), or 256-column tiles of
-// 128 or 256 rows, whole (kWhole) or in equal parts of K (kSplit).  kStream and kSplit leave
+// 128, 192 or 256 rows, whole (kWhole) or in equal parts of K (kSplit).  kStream and kSplit leave
 // partial sums in planes.
 enum class Gemm8Kind { kFew, kStream, kNarrow, kWhole, kSplit };
 struct Gemm8Plan {

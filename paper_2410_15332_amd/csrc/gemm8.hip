@@ -77,8 +77,8 @@ double stream_time(int M, int N, int K) {
 
 // Whole tiles of tm x tn, a workgroup each: LDS traffic paces a stage (64 x 256: two stages in
 // flight do not cover the latency).  256 rows, N = K = 4096:
-// 64 x 64 13.3 us, 64 x 128 16 (split 128-row tiles 17.5); 501 rows: 25 and 17.1 (21.7);
-// SwiGLU of 100 rows, N 28672: 128 x 128 30.4 (streamed 42).
+// 64 x 64 13.3 us, 64 x 128 16 (split 128-row tiles 17.5); 501 rows: 22.9 and 16.4 (21.8);
+// SwiGLU of 100 rows, N 28672: 128 x 128 30 (streamed 41).
 double narrow_time(int M, int N, int K, int tm, int tn) {
   const int tiles = cdiv(M, tm) * (N / tn);
   const double rounds = cdiv(tiles, kWorkers), busy = std::max(tiles / rounds / kWorkers - 0.6, 0.0);

@@ -6,7 +6,9 @@
 // eight wavefronts in blocks of 128 in turn, so that at any time the workgroup reads runs of
 // 1 KB of each row of W; the wavefronts' sums meet in LDS.  Nothing is staged: every byte of W
 // is used once, so it goes from memory to the registers of the 16 x 16 x 128 instruction
-// that multiplies it, four blocks ahead; the rows come from the caches.
+// that multiplies it, four blocks ahead (six: slower); the rows come from the caches.  What
+// bounds it is the latency of memory.  N 6144, K 4096: 1 row 7.8 us (25 MB, 3.2 TB/s), 8 rows 9.3
+// (streamed 11.4 and 11.6); 32 rows 15.0 (12.2), as every workgroup reads all rows.
 //
 // A lane has row l % 16 of either operand and of a block the 16-byte chunks l / 16 and
 // l / 16 + 4 (which values of K does not matter, as both operands agree): each load

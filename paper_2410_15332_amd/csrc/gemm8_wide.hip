@@ -9,6 +9,14 @@
 // 32 KB each), of which a stage frees two: they take the W half of the stage after next
 // and the A half of the one after that.
 //
+// What bounds it: many tiles run at the chip's power limit.  SwiGLU of 20 560 rows, N 28 672,
+// K 4096 to e4m3, 256-row tiles: 1.83-1.91 ms, 2.53-2.64 PFLOP/s, at 1.75 GHz with the
+// matrix cores busy for 68% of the cycles (a large library product without the epilogue: 2.97).
+// Few tiles wait for memory: 736 rows, 192-row tiles, two each on 224 CUs: 89-92 us, 2.15 GHz,
+// busy for 42%, 23% of the wavefronts' time waiting.
+// Tile heights, the same two: 736 rows 107 us (128), 89 (192), 93 (256); 20 560 rows
+// 2109, 1984, 1887.
+//
 // Scales: one per row and stage, applied by the matrix instruction.  A wavefront's rows
 // are dealt to its I row tiles in turn (tile i has rows I r + i), so the I scales of a
 // lane are neighbouring bytes of one load, and the instruction picks byte i.  The scale of
@@ -16,7 +24,8 @@
 // and of the up block).  They are loaded into registers two stages ahead.
 //
 // With few tiles the same kernel runs equal parts of K of every tile, one workgroup each,
-// into fp32 planes that the consumer adds (stream_sum.h).
+// into fp32 planes that the consumer adds (stream_sum.h): 736 rows, N 4096, K 14 336, 192-row
+// tiles in four parts 54 us with the pass that adds them, whole 96.
 //
 // Half-stage layout: rows of 128 bytes in groups of 8 (1 KB, one load instruction); the
 // eight 16-byte chunks of row r are XOR-swizzled by (r / 2) % 8, so the 16 lanes of each
