@@ -75,7 +75,7 @@ double stream_time(int M, int N, int K) {
   return 7.0 + double(N / 64) * (K / kGroup) / kWorkers * (tm == 32 ? 0.38 : tm == 64 ? 0.47 : 0.6);
 }
 
-// Whole tiles of tm x tn, a workgroup each: LDS traffic paces a stage (64 x 256: two stages in
+// Whole tiles of tm x tn, a workgroup each: what a CU can load paces a stage (64 x 256: two stages in
 // flight do not cover the latency).  256 rows, N = K = 4096:
 // 64 x 64 13.3 us, 64 x 128 16 (split 128-row tiles 17.5); 501 rows: 22.9 and 16.4 (21.8);
 // SwiGLU of 100 rows, N 28672: 128 x 128 30 (streamed 41).

@@ -7,11 +7,12 @@
 // to a plane of its own (stream_sum.h), LDS a ring of NS stages.  32 rows, N 4096, K 14 336:
 // 14.2 us (59 MB, 4.2 TB/s) and 1.9 to add the planes.
 //
-// Whole tiles have no second launch.  What bounds them is the traffic between LDS and the
-// matrix cores: a wavefront reads 3 or 4 KB for each 32 x 32 x 64 product, so larger tiles cost
-// less per product, and smaller ones use more CUs.  501 rows, N = K = 4096: 64 x 64 tiles
-// 22.9 us, 64 x 128 16.4, 128 x 128 21.2, 256-column tiles 22 at best.  SwiGLU of 100 rows,
-// N 28 672, K 4096: 128 x 128 30 us (121 MB, 4.0 TB/s), 64 x 128 37, planes 41; to e4m3, where
+// Whole tiles have no second launch.  What bounds them is what a CU can load, some 90 GB/s: one
+// tile alone takes 0.18, 0.29 and 0.44 us a stage for the 16, 24 and 32 KB of 64 x 64, 64 x 128
+// and 128 x 128, and a third less read from LDS per product changes nothing.  So larger
+// tiles cost less per product, and smaller ones use more CUs.  501 rows, N = K = 4096: 64 x 64
+// tiles 22.9 us, 64 x 128 16.4, 128 x 128 21.2, 256-column tiles 22 at best.  SwiGLU of 100 rows,
+// N 28 672, K 4096: 128 x 128 29 us (121 MB, 4.1 TB/s), 64 x 128 37, planes 41; to e4m3, where
 // a tile has to have whole groups, 64 x 256 34, planes 42.  Two wavefronts share a place
 // (KS = 2) where a tile has few: 64 x 64 tiles of 256 rows 13.3 us, 14.9 without.
 //
@@ -99,7 +100,11 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       vo[i] = gr * g.K + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     }
   };
-  int du = u0, dtile = u0 / ks, dkt = u0 - dtile * ks;   // next unit to load
+  // Whole tiles: each XCD's start at a K stage of their own.  Rows a multiple of 4 KB apart have
+  // one stage on the same few memory channels, which all would ask for at once: 256 rows,
+  // N = K = 4096 15.8 -> 15.1 us, SwiGLU of 100 rows, N 28 672 31.3 -> 29.2, K = 5120 1% less.
+  const int rot = WHOLE ? w % 8 * ks / 8 : 0;
+  int du = u0, dtile = u0 / ks, dkt = WHOLE ? rot : u0 - dtile * ks;   // next unit to load
   setup(dtile);
   auto dma_next = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
@@ -108,7 +113,7 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       ++du;
       if (++dkt == ks) {
         dkt = 0;
-        setup(++dtile);
+        if (!WHOLE) setup(++dtile);
       }
     }
   };
@@ -135,7 +140,8 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       if (GLU) unit_scale[i + ks] = char(g.sw[size_t((ffn + col) >> 7) * ks + k]);
     }
   }
-  int buf = 0, u = u0, tile = u0 / ks, kt = u0 - tile * ks, at = 0;   // kt, at: of the unit fetched next
+  int buf = 0, u = u0, tile = u0 / ks;
+  int kt = WHOLE ? rot : u0 - tile * ks, at = WHOLE ? rot : 0;   // of the unit fetched next
   const int swords = min(ld, TM);
   int srow[RT];
 #pragma unroll
@@ -166,8 +172,8 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
       for (int r = 0; r < RT; ++r) f.sa[r] = uint8_t(row_scale[kt * swords + srow[r]]);
       f.sb[0] = uint8_t(unit_scale[at]);
       if (GLU) f.sb[GLU] = uint8_t(unit_scale[at + ks]);
-      ++at;
       kt = kt + 1 == ks ? 0 : kt + 1;
+      at = WHOLE ? kt : at + 1;
 #pragma unroll
       for (int i = 0; i < NH; ++i) {
         const int c0 = ((4 * (KS == 2 ? kh : i) + 2 * half) ^ lsw) * 16, c1 = c0 ^ 16;
