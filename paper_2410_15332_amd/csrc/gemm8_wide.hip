@@ -6,8 +6,10 @@
 // So the schedule is that kernel's: a wavefront owns TM/2 x 128 outputs in AGPRs, the
 // fragments of the next half stage are read and the loads of later stages issued between
 // the MFMAs of this one, and LDS is a ring of five half stages (one operand, 128 of K,
-// 32 KB each), of which a stage frees two: they take the W half of the stage after next
-// and the A half of the one after that.
+// 32 KB each), of which a stage frees two: they take the A half of the stage after next
+// and the W half of the one after that: W comes from memory, most of A from the caches (the
+// other way round: 736 rows, N 27 648, K 5120 121 us, 114.6 now; 200 rows of 28 672 x 4096 43.2,
+// 40.6; 20 560 rows the same).
 //
 // What bounds it: many tiles run at the chip's power limit.  SwiGLU of 20 560 rows, N 28 672,
 // K 4096 to e4m3, 256-row tiles: 1.83-1.91 ms, 2.53-2.64 PFLOP/s, at 1.75 GHz with the
@@ -116,7 +118,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
     int tile, kt, slot, left;
   };
   // next half stages (ca, cb) and scales (cs) to load
-  Cursor ca{tile0, kt0, 0, n_units}, cb{tile0, kt0, 1, n_units}, cs{tile0, kt0, 0, n_units};
+  Cursor ca{tile0, kt0, 1, n_units}, cb{tile0, kt0, 0, n_units}, cs{tile0, kt0, 0, n_units};
   auto setup_a = [&]() __attribute__((always_inline)) {
     int mt, nt;
     tile_mn(ca.tile, mt, nt);
@@ -257,31 +259,31 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
     };
     for_each_index(step, std::make_integer_sequence<int, NM>{});
   };
-  // the next stage's loads landed, everyone's (the A loads past it stay in flight), and
+  // the next stage's loads landed, everyone's (the W loads past it stay in flight), and
   // this stage is read
   auto sync = [&]() __attribute__((always_inline)) {
-    wait_vmem<NLA>();
+    wait_vmem<NLB>();
     barrier_lds();
   };
 
   Loaded first;
   load_scales(first);
 #pragma unroll
-  for (int i = 0; i < NLA; ++i) dma_a(i);
-#pragma unroll
   for (int i = 0; i < NLB; ++i) dma_b(i);
+#pragma unroll
+  for (int i = 0; i < NLA; ++i) dma_a(i);
   load_scales(sc2);
 #pragma unroll
-  for (int i = 0; i < NLA; ++i) dma_a(i);
-#pragma unroll
   for (int i = 0; i < NLB; ++i) dma_b(i);
+#pragma unroll
+  for (int i = 0; i < NLA; ++i) dma_a(i);
   wait_vmem<NLA + NLB + (I == 3 ? 4 : 2) + (GLU ? 1 : 0)>();   // stage 0
   __asm__ volatile("s_barrier" ::: "memory");
   take(sc0, first);
 #pragma unroll
-  for (int i = 0; i < I + J; ++i) read1(f0, lds[0], lds[1], 0, i);
+  for (int i = 0; i < I + J; ++i) read1(f0, lds[1], lds[0], 0, i);
 
-  int sa = 0, sb = 1;
+  int sa = 1, sb = 0;
   for (int tile = tile0, left = n_units; left > 0;) {
     const int n = SPLIT ? n_units : p.ks;
 #pragma unroll
@@ -289,20 +291,20 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
 #pragma unroll
       for (int j = 0; j < J; ++j) acc[i][j] = f32x16{};
     for (int kt = 0; kt < n; ++kt) {
-      slice(f0, f1, lds[sa], lds[sb], 1, std::integral_constant<int, 1>{});
+      slice(f0, f1, lds[sa], lds[sb], 1, std::integral_constant<int, 0>{});
       sync();
       sa = bump(sa);
       sb = bump(sb);
       take(sc1, sc2);
       load_scales(sc2);
-      slice(f1, f0, lds[sa], lds[sb], 0, std::integral_constant<int, 0>{});
+      slice(f1, f0, lds[sa], lds[sb], 0, std::integral_constant<int, 1>{});
       sc0 = sc1;
     }
     // ---- epilogue: lane l has row I (l % 32) + i of the wavefront's in row tile i, and of
     // column tile j the columns 8 q + 4 (l / 32) + 0 .. 3 in registers 4 q .. 4 q + 3.  Results go
     // through LDS, so that a store instruction writes runs of 256 bytes (rows past M fall
-    // outside the descriptors): through the half stage that the next A loads will take,
-    // which held this stage's W and has been read by everyone.
+    // outside the descriptors): through the half stage that the next W loads will take,
+    // which held this stage's A and has been read by everyone.
     int mt, nt;
     tile_mn(tile, mt, nt);
     // Lane numbers that the compiler cannot see through, or it keeps the offsets derived from
@@ -317,7 +319,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
       for (int x = 0; x < n; ++x) __asm__ volatile("" : "+a"(acc[i][j + x]));
     };
     const int mw = mt * TM + wm * (TM / 2);             // the wavefront's first row
-    char* room = lds[ca.slot];
+    char* room = lds[cb.slot];
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     if constexpr (EPI == kGluQuantOut) {
       // a row's other columns are in lane l ^ 32 and in the wavefront with the other wn: the
@@ -525,7 +527,7 @@ __global__ __launch_bounds__(256, 1) void gemm8_wide_kernel(Gemm8Args g, WidePla
           __builtin_amdgcn_sched_barrier(0);
         }
     }
-    barrier_lds();                                      // the room is read: the next A loads may land
+    barrier_lds();                                      // the room is read: the next W loads may land
     left -= n;
     tile += p.G;
   }
