@@ -14,11 +14,11 @@
 // tiles 22.9 us, 64 x 128 16.4, 128 x 128 21.2, 256-column tiles 22 at best.  SwiGLU of 100 rows,
 // N 28 672, K 4096: 128 x 128 29 us (121 MB, 4.1 TB/s), 64 x 128 37, planes 41; to e4m3, where
 // a tile has to have whole groups, 64 x 256 34, planes 42.  Two wavefronts share a place
-// (KS = 2) where a tile has few: 64 x 64 tiles of 256 rows 13.3 us, 14.9 without.
+// (KS = 2) where a tile has few: 64 x 64 tiles of 256 rows 13.3 us then, 14.9 without.
 //
 // Scales: a worker's are few (a byte per row and stage, and one per unit for the weight
-// block, which a tile's columns never leave), so they go to LDS once, while the first
-// stages are in flight.
+// block, which a tile's columns never leave), so they go to LDS once: while the first
+// stages are in flight, or, of whole tiles, in front of them (256 rows, N = K = 4096 12.6 -> 12.1 us).
 //
 // Stage layout: (TM + TN) rows of 128 bytes, A rows then W rows, in groups of 8 rows
 // (1 KB, one load instruction); the eight 16-byte chunks of row r are XOR-swizzled by
@@ -58,6 +58,7 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
   static_assert(NG % NW == 0, "row groups per wavefront");
   static_assert(!GLU || CT == 2, "a wavefront holds the gate and up of its columns");
   static_assert(TN <= (GLU ? 256 : 128), "one weight scale per unit (GLU: two)");
+  static_assert(!WHOLE || NW * 64 >= kRowScales / TM, "a thread loads one of a whole tile's");
   static_assert(OUT != kGluQuantOut || (TN == 256 && TM * 32 % (NW * 64) == 0), "a tile has whole groups of the result");
   constexpr int SB = (TM + TN) * 128;                   // operand bytes per stage
   // One array: with several, the compiler sees that reads of the scales cannot be told from
@@ -121,23 +122,39 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
   const int lbase = (lane & 31) * 128, lsw = (lane >> 1) & 7, half = lane >> 5;
   const int abase = rt * 4096 + lbase, bbase = (TM / 32 + ct) * 4096 + lbase;
 
+  // Whole tiles load their scales in front of the operands, so that the first stage waits for
+  // nothing behind it: all of the tile's rows', at the stage's place, and the blocks'.
+  uint8_t block = 0, up = 0;
+  if constexpr (WHOLE) {
+    const __amdgpu_buffer_rsrc_t rsc =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.sa), 0, ks * ld, kBufWord3);
+    const int words = min(ld, TM) / 4, n = ks * words, m0 = dtile % m_tiles * TM, col = dtile / m_tiles * TN / (GLU ? 2 : 1);
+    for (int i = wv * 64; i < n; i += NW * 64) {
+      const int at = min(i + lane, n - 1), k = at / words;
+      dma4(rsc, row_scale + i * 4, k * ld + min(m0 + (at - k * words) * 4, ld - 4), 0);
+    }
+    const int k = min(tid, ks - 1);
+    block = g.sw[size_t(col >> 7) * ks + k];
+    if (GLU) up = g.sw[size_t((ffn + col) >> 7) * ks + k];
+  }
 #pragma unroll
   for (int b = 0; b < NS - 1; ++b) dma_next(b);
-  {
-    // a stage's scales of the tile's rows (planes: of all rows, M <= 128), at the stage's place
-    const int words = min(ld, TM) / 4, all = ks * words;
-    const int mt0 = WHOLE ? (u0 / ks) % m_tiles * (TM / 4) : 0;
+  if constexpr (WHOLE) {
+    if (tid < ks) {
+      unit_scale[tid] = char(block);
+      if (GLU) unit_scale[tid + ks] = char(up);
+    }
+  } else {
+    // a stage's scales of all rows (M <= 128), at the stage's place
+    const int words = ld / 4, all = ks * words;
     const int n = min(u1 - u0, ks) * words, k0 = (u0 % ks) * words;
     for (int i = tid; i < n; i += NW * 64) {
-      const int at = k0 + i < all ? k0 + i : k0 + i - all, k = at / words;
-      reinterpret_cast<uint32_t*>(row_scale)[at] =
-          reinterpret_cast<const uint32_t*>(g.sa)[size_t(k) * (ld / 4) + min(mt0 + at - k * words, ld / 4 - 1)];
+      const int at = k0 + i < all ? k0 + i : k0 + i - all;
+      reinterpret_cast<uint32_t*>(row_scale)[at] = reinterpret_cast<const uint32_t*>(g.sa)[at];
     }
     for (int i = tid; i < u1 - u0; i += NW * 64) {
       const int t = (u0 + i) / ks, k = u0 + i - t * ks;
-      const int col = t / m_tiles * TN / (GLU ? 2 : 1);
-      unit_scale[i] = char(g.sw[size_t(col >> 7) * ks + k]);
-      if (GLU) unit_scale[i + ks] = char(g.sw[size_t((ffn + col) >> 7) * ks + k]);
+      unit_scale[i] = char(g.sw[size_t(t / m_tiles * TN >> 7) * ks + k]);
     }
   }
   int buf = 0, u = u0, tile = u0 / ks;

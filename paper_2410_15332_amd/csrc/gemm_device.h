@@ -16,6 +16,11 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t rs, char* dst, int 
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, voff, soff, 0, 0);
 }
 
+// ... of 4 bytes per lane (256 bytes per wavefront).
+__device__ __forceinline__ void dma4(__amdgpu_buffer_rsrc_t rs, char* dst, int voff, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 4, voff, soff, 0, 0);
+}
+
 // Workgroup barrier ordering LDS accesses only (waits for this wavefront's LDS
 // reads, not for its buffer->LDS loads still in flight).
 __device__ __forceinline__ void barrier_lds() {
