@@ -12,12 +12,12 @@
 // 40.6; 20 560 rows the same).
 //
 // What bounds it: many tiles run at the chip's power limit.  SwiGLU of 20 560 rows, N 28 672,
-// K 4096 to e4m3, 256-row tiles: 1.83-1.91 ms, 2.53-2.64 PFLOP/s, at 1.75 GHz with the
+// K 4096 to e4m3, 256-row tiles: 1.82-1.92 ms, 2.52-2.65 PFLOP/s, at 1.75 GHz with the
 // matrix cores busy for 68% of the cycles (a large library product without the epilogue: 2.97).
-// Few tiles wait for memory: 736 rows, 192-row tiles, two each on 224 CUs: 89-92 us, 2.15 GHz,
-// busy for 42%, 23% of the wavefronts' time waiting.
-// Tile heights, the same two: 736 rows 107 us (128), 89 (192), 93 (256); 20 560 rows
-// 2109, 1984, 1887.
+// Few tiles wait for memory: 736 rows, 192-row tiles, two each on 224 CUs: 84-87 us, 2.1 GHz,
+// busy for 44%, 19% of the wavefronts' time waiting.
+// Tile heights, the same two, before W had the longer way: 736 rows 107 us (128), 89 (192), 93 (256);
+// 20 560 rows 2109, 1984, 1887.
 //
 // Scales: one per row and stage, applied by the matrix instruction.  A wavefront's rows
 // are dealt to its I row tiles in turn (tile i has rows I r + i), so the I scales of a
