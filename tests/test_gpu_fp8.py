@@ -341,12 +341,11 @@ BORDERS = [(16, 768, 1152), (29, 512, 1920), (100, 2048, 4096), (77, 12288, 1152
            (2049, 4096, 384), (2049, 6144, 384)]
 
 
-@pytest.mark.parametrize("m,n,k", BORDERS, ids=lambda x: str(x))
-def test_scales_at_their_borders(m, n, k):
-    """Rows picked for a group whose largest value is next to where its scale changes, nearer than the
-    matrix cores' dropped bits: the scales are float64's all the same.  (float64 sums and silu are within
-    2^-53 (k + 8) < 2e-12 of the sum of magnitudes, some 1e2 of the result; rows nearer than 1e-9 are left out.)"""
-    _say("gemm borders", m, n, k)
+def _near_borders(m, n, k, copies=1):
+    """Operands, and each group's largest result in float64: m rows picked for one that is next to where its
+    scale changes (each copies times), nearer than the matrix cores' dropped bits.  float64 sums and silu are
+    within 2^-53 (k + 8) < 2e-12 of the sum of magnitudes, some 1e2 of the result; rows nearer than 1e-9 are
+    left out."""
     gen = torch.Generator("cuda").manual_seed(m + n + k)
     every = 1 << 16                                         # rows to pick from
     draw = lambda *shape: torch.randn(shape, device="cuda", generator=gen)
@@ -363,12 +362,29 @@ def test_scales_at_their_borders(m, n, k):
     far = torch.log2(top / 1.75)
     far = ((far - torch.round(far)).abs()).amin(-1)
     order = torch.argsort(far)
-    at = order[far[order] > 1e-9][:m]
+    at = order[far[order] > 1e-9][:m // copies].repeat(copies)
     # 2^16 n / 256 groups, evenly spread over [0, 1/2): 16 of them this near at n = 512
     assert float(far[at[0]]) < 2.0 ** -14
-    top, t = top[at].cpu().numpy(), ta[at].cpu().numpy()
-    _, got = _run_gemm("swiglu_fp8", qa[at].view(torch.uint8).cpu().numpy(), t, qw.view(torch.uint8).cpu().numpy(), tw.cpu().numpy())
+    return [x.cpu().numpy() for x in (qa[at].view(torch.uint8), ta[at], qw.view(torch.uint8), tw, top[at])]
+
+
+@pytest.mark.parametrize("m,n,k", BORDERS, ids=lambda x: str(x))
+def test_scales_at_their_borders(m, n, k):
+    """The scales of groups next to where they change are float64's all the same."""
+    _say("gemm borders", m, n, k)
+    *operands, top = _near_borders(m, n, k)
+    _, got = _run_gemm("swiglu_fp8", *operands)
     assert np.array_equal(got, fp8.scale_exponent(top))
+
+
+@pytest.mark.parametrize("m,n,k", BORDERS, ids=lambda x: str(x))
+def test_every_row_at_a_border(m, n, k):
+    """... of a batch of one row over and over, as padding may be: every row of a tile has such a group."""
+    _say("gemm one border", m, n, k)
+    *operands, top = _near_borders(m, n, k, copies=m)
+    codes, got = _run_gemm("swiglu_fp8", *operands)
+    assert np.array_equal(got, fp8.scale_exponent(top))
+    assert np.array_equal(codes, np.broadcast_to(codes[:1], codes.shape))
 
 
 @pytest.mark.parametrize("m,n,k", [(7, 128, 128), (70, 384, 256), (200, 128, 512), (300, 1408, 384)])
