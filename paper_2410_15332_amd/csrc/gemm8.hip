@@ -13,8 +13,6 @@ namespace {
 
 constexpr int kWorkers = 256;                           // one workgroup per CU
 
-__device__ __forceinline__ float silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(-x * kLog2e)); }
-
 // Summed planes in bf16, or through SwiGLU (GLU): four columns per thread.
 template <bool GLU>
 __global__ __launch_bounds__(256) void finish_kernel(StreamSum s, uint16_t* __restrict__ out, int cols) {

@@ -23,8 +23,6 @@ namespace {
 
 constexpr int kNW = 8, kAhead = 4;                      // wavefronts; blocks in flight per wavefront
 
-__device__ __forceinline__ float silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(-x * kLog2e)); }
-
 // MT: tiles of 16 rows.  OUT: kBf16Out, kGluOut, or kFewPlane: fp32 [M][N] for a pass that does more.
 constexpr int kFewPlane = 4;
 template <int OUT, int MT>

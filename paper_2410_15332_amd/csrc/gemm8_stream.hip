@@ -40,8 +40,6 @@ constexpr int kBK = 128;
 constexpr int kWorkers = 256;                           // one workgroup per CU
 constexpr int kMinUnits = 4;                            // K stages per worker, at least
 
-__device__ __forceinline__ float silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(-x * kLog2e)); }
-
 constexpr int kRowScales = 14336, kUnitScales = 2048;   // bytes of LDS for them: what the ring leaves
 
 // A wavefront has 32 RT rows x 32 CT columns of a tile.  OUT: kPlanesOut, or kBf16Out, kGluOut or

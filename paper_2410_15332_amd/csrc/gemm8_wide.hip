@@ -12,9 +12,9 @@
 // 40.6; 20 560 rows the same).
 //
 // What bounds it: many tiles run at the chip's power limit.  SwiGLU of 20 560 rows, N 28 672,
-// K 4096 to e4m3, 256-row tiles: 1.82-1.92 ms, 2.52-2.65 PFLOP/s, at 1.75 GHz with the
+// K 4096 to e4m3, 256-row tiles: 1.82-1.93 ms, 2.50-2.66 PFLOP/s, at 1.75 GHz with the
 // matrix cores busy for 68% of the cycles (a large library product without the epilogue: 2.97).
-// Few tiles wait for memory: 736 rows, 192-row tiles, two each on 224 CUs: 84-87 us, 2.1 GHz,
+// Few tiles wait for memory: 736 rows, 192-row tiles, two each on 224 CUs: 84-89 us, 2.1 GHz,
 // busy for 44%, 19% of the wavefronts' time waiting.
 // Tile heights, the same two, before W had the longer way: 736 rows 107 us (128), 89 (192), 93 (256);
 // 20 560 rows 2109, 1984, 1887.
@@ -58,8 +58,6 @@ struct WidePlan8 {
   int G;                       // workgroups, a multiple of 8
   int parts;                   // kPlanesOut: equal parts of K per tile, a workgroup each
 };
-
-__device__ __forceinline__ float silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(-x * kLog2e)); }
 
 template <class F, int... M>
 __device__ __forceinline__ void for_each_index(const F& f, std::integer_sequence<int, M...>) {
