@@ -458,6 +458,16 @@ def _expect(name: str, t, shape, dtypes, device: int) -> int:
     return t.data_ptr()
 
 
+def _scratch(t, device: int):
+    """Address and bytes of a workspace.  A missing or short one is the library's to refuse; it cannot see
+    memory of the host or another device, nor that a view has less memory behind it than elements."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"workspace: contiguous memory of device {device} expected, got strides {t.stride()} on {t.device}")
+    return t.data_ptr(), t.nbytes
+
+
 def _raw_stream(stream, device: int) -> int:
     """_stream() for calls of a few us: the current stream's handle without an object around it."""
     if stream is not None:
@@ -510,13 +520,13 @@ def epic_gemm_fp8(epilogue: int, a, a_scale, w, w_scale, out, out_scale=None, wo
     (m, k), n = a.shape, w.shape[0]
     quant = epilogue == FP8_SWIGLU_FP8
     cols = n if epilogue == FP8_BF16 else n // 2
+    ws, ws_bytes = _scratch(workspace, dev)
     _check(_gemm_fp8(epilogue, _expect("a", a, (m, k), e4m3, dev),
                      _expect("a_scale", a_scale, fp8_row_scale_shape(m, k), e8m0, dev), _expect("w", w, (n, k), e4m3, dev),
                      _expect("w_scale", w_scale, fp8_block_scale_shape(n, k), e8m0, dev), m, n, k,
                      _expect("out", out, (m, cols), e4m3 if quant else bf16, dev),
                      _expect("out_scale", out_scale, fp8_row_scale_shape(m, cols), e8m0, dev) if quant else None,
-                     _ptr(workspace), 0 if workspace is None else workspace.nbytes, _raw_stream(stream, dev)),
-           "epic_gemm_fp8")
+                     ws, ws_bytes, _raw_stream(stream, dev)), "epic_gemm_fp8")
 
 
 def epic_model_fp8_workspace_bytes(cfg: epic_model_cfg, sizes: epic_plan_sizes) -> int:

@@ -129,6 +129,51 @@ def test_binding_refuses_what_the_kernels_cannot_read():
                          torch.zeros(4, 128, dtype=torch.bfloat16))
 
 
+class _Elsewhere:
+    """A workspace of 64 MB of another device, aligned: everything that the library itself looks at is right."""
+
+    device, nbytes = "another device", 64 << 20
+
+    def get_device(self):
+        return 7
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return P
+
+    def stride(self):
+        return (1,)
+
+    def numel(self):
+        return self.nbytes
+
+    def element_size(self):
+        return 1
+
+
+def _workspaces():
+    """What may not reach a kernel: memory of another device, and a view with one byte behind its 64 MB."""
+    return [_Elsewhere(), torch.zeros(1, dtype=torch.uint8).expand(64 << 20)]
+
+
+@pytest.mark.parametrize("bad", [0, 1])
+def test_gemm_refuses_workspaces_of_other_memory(bad, monkeypatch):
+    """With host tensors in the place of the GPU's, and no call past the binding."""
+    calls = []
+    monkeypatch.setattr(el, "_device_of", lambda name, t: t.get_device())
+    monkeypatch.setattr(el, "_raw_stream", lambda stream, device: None)
+    monkeypatch.setattr(el, "_gemm_fp8", lambda *args: calls.append(args) or 0)
+    u8 = lambda *s: torch.zeros(s, dtype=torch.uint8)  # noqa: E731
+    args = (el.FP8_BF16, u8(4, 256), u8(2, 4), u8(128, 256), u8(1, 2), torch.zeros(4, 128, dtype=torch.bfloat16))
+    el.epic_gemm_fp8(*args, workspace=u8(64 << 20))
+    assert len(calls) == 1
+    with pytest.raises(ValueError, match="workspace"):
+        el.epic_gemm_fp8(*args, workspace=_workspaces()[bad])
+    assert len(calls) == 1
+
+
 # ---------------------------------------------------------------- the kernel chosen by sizes
 
 def route(epi, m, n, k):

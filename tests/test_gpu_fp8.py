@@ -656,3 +656,14 @@ def test_binding_refuses_what_the_kernels_cannot_read():
         with pytest.raises(el.EpicError):
             el.epic_gemm_fp8(**{**gemm, **bad})
     torch.cuda.synchronize()
+
+
+def test_binding_refuses_workspaces_of_other_memory():
+    """A workspace of the host, or a view of one byte: ValueError before any launch (test_fp8.py has them without a GPU)."""
+    el = _el()
+    u8 = lambda *s, **kw: torch.zeros(s, dtype=torch.uint8, **{"device": "cuda", **kw})  # noqa: E731
+    n = el.epic_gemm_fp8_workspace_bytes()
+    out = torch.zeros(4, 256, dtype=torch.bfloat16, device="cuda")
+    for bad in (u8(n, device="cpu"), u8(1).expand(n)):
+        with pytest.raises(ValueError, match="workspace"):
+            el.epic_gemm_fp8(el.FP8_BF16, u8(4, 256), u8(2, 4), u8(256, 256), u8(2, 2), out, workspace=bad)
