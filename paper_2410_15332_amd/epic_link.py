@@ -533,25 +533,41 @@ def epic_model_fp8_workspace_bytes(cfg: epic_model_cfg, sizes: epic_plan_sizes) 
     return int(_model_fp8_ws(C.byref(cfg), C.byref(sizes)))
 
 
+def _current_device() -> int:
+    import torch
+
+    return torch.cuda.current_device()
+
+
+def _packed(name: str, t, device: int) -> Optional[int]:
+    """The address of a layer's or model's tensor: contiguous, of the call's device.  A missing one is the library's to refuse."""
+    if t is not None and (t.get_device() != device or not t.is_contiguous()):
+        raise ValueError(f"{name}: contiguous memory of device {device} expected, got strides {t.stride()} on {t.device}")
+    return _ptr(t)
+
+
 def epic_link_layer_fp8(cfg: epic_model_cfg, weights: epic_layer_weights_fp8, dplan: DevicePlan, hidden_s, k_cache,
                         v_cache, workspace, stream=None):
     """epic_link_layer with its projections on 8-bit operands."""
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_link_layer_fp8(C.byref(cfg), C.byref(weights), C.byref(dplan.sizes), C.byref(dplan.plan), _ptr(hidden_s),
-                           _ptr(k_cache), _ptr(v_cache), _ptr(workspace), ws_bytes, _stream(stream)),
+    dev = _current_device()
+    ws, ws_bytes = _scratch(workspace, dev)
+    _check(_link_layer_fp8(C.byref(cfg), C.byref(weights), C.byref(dplan.sizes), C.byref(dplan.plan),
+                           _packed("hidden_s", hidden_s, dev), _packed("k_cache", k_cache, dev),
+                           _packed("v_cache", v_cache, dev), ws, ws_bytes, _raw_stream(stream, dev)),
            "epic_link_layer_fp8")
 
 
 def epic_link_model_fp8(cfg: epic_model_cfg, layers: Sequence[epic_layer_weights_fp8], final_norm, dplan: DevicePlan,
                         hidden_s, k_caches: Sequence, v_caches: Sequence, out_hidden, workspace, stream=None):
     """epic_link_model with its projections on 8-bit operands."""
-    n = len(layers)
+    n, dev = len(layers), _current_device()
     warr = (epic_layer_weights_fp8 * n)(*layers)
-    karr = (C.c_void_p * n)(*[t.data_ptr() for t in k_caches])
-    varr = (C.c_void_p * n)(*[t.data_ptr() for t in v_caches])
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_link_model_fp8(C.byref(cfg), warr, _ptr(final_norm), C.byref(dplan.sizes), C.byref(dplan.plan),
-                           _ptr(hidden_s), karr, varr, _ptr(out_hidden), _ptr(workspace), ws_bytes, _stream(stream)),
+    karr = (C.c_void_p * n)(*[_packed("k_caches", t, dev) for t in k_caches])
+    varr = (C.c_void_p * n)(*[_packed("v_caches", t, dev) for t in v_caches])
+    ws, ws_bytes = _scratch(workspace, dev)
+    _check(_link_model_fp8(C.byref(cfg), warr, _packed("final_norm", final_norm, dev), C.byref(dplan.sizes),
+                           C.byref(dplan.plan), _packed("hidden_s", hidden_s, dev), karr, varr,
+                           _packed("out_hidden", out_hidden, dev), ws, ws_bytes, _raw_stream(stream, dev)),
            "epic_link_model_fp8")
 
 

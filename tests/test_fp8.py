@@ -174,6 +174,58 @@ def test_gemm_refuses_workspaces_of_other_memory(bad, monkeypatch):
     assert len(calls) == 1
 
 
+class _Plan:
+    sizes, plan = el.epic_plan_sizes(), el.epic_plan()
+
+
+def _model_args(n=2):
+    """Arguments of a model call on host tensors; a layer call's are the first of each list."""
+    t = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype)  # noqa: E731
+    bf16 = torch.bfloat16
+    return dict(cfg=el.epic_model_cfg(el.attn_cfg(2, 1, 64), 128, 128, n, 1e4, 1e-5),
+                layers=[el.epic_layer_weights_fp8() for _ in range(n)], final_norm=t(128, dtype=bf16), dplan=_Plan(),
+                hidden_s=t(3, 128), k_caches=[t(4, 1, 16, 64, dtype=bf16) for _ in range(n)],
+                v_caches=[t(4, 1, 64, 16, dtype=bf16) for _ in range(n)], out_hidden=t(3, 128),
+                workspace=t(512, dtype=torch.uint8))
+
+
+def _layer_args(**kw):
+    a = {**_model_args(1), **kw}
+    return dict(cfg=a["cfg"], weights=a["layers"][0], dplan=a["dplan"], hidden_s=a["hidden_s"], k_cache=a["k_caches"][0],
+                v_cache=a["v_caches"][0], workspace=a["workspace"])
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    """Layer and model calls on host tensors, up to the library; returns the calls that got there."""
+    calls = []
+    monkeypatch.setattr(el, "_current_device", lambda: -1, raising=False)
+    for name in ("_stream", "_raw_stream"):
+        monkeypatch.setattr(el, name, lambda *args: None)
+    for name in ("_link_layer_fp8", "_link_model_fp8"):
+        monkeypatch.setattr(el, name, lambda *args: calls.append(args) or 0)
+    return calls
+
+
+def test_layer_and_model_refuse_tensors_of_other_memory(on_host):
+    """A workspace of another device or with nothing behind it, and tensors whose rows lie apart."""
+    el.epic_link_layer_fp8(**_layer_args())
+    el.epic_link_model_fp8(**_model_args())
+    assert len(on_host) == 2
+    wide = torch.zeros(3, 256)[:, :128]
+    k = torch.zeros(4, 16, 1, 64, dtype=torch.bfloat16)[:, ::2]
+    for bad in [dict(workspace=w) for w in _workspaces()] + [dict(hidden_s=wide), dict(hidden_s=_Elsewhere()),
+                                                             dict(k_caches=[k, k]), dict(v_caches=[_Elsewhere()] * 2)]:
+        with pytest.raises(ValueError, match=next(iter(bad))[:7]):
+            el.epic_link_layer_fp8(**_layer_args(**bad))
+        with pytest.raises(ValueError, match=next(iter(bad))[:7]):
+            el.epic_link_model_fp8(**{**_model_args(), **bad})
+    for bad in (dict(out_hidden=wide), dict(final_norm=_Elsewhere())):
+        with pytest.raises(ValueError):
+            el.epic_link_model_fp8(**{**_model_args(), **bad})
+    assert len(on_host) == 2
+
+
 # ---------------------------------------------------------------- the kernel chosen by sizes
 
 def route(epi, m, n, k):
