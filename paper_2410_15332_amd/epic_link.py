@@ -561,6 +561,9 @@ def epic_link_model_fp8(cfg: epic_model_cfg, layers: Sequence[epic_layer_weights
                         hidden_s, k_caches: Sequence, v_caches: Sequence, out_hidden, workspace, stream=None):
     """epic_link_model with its projections on 8-bit operands."""
     n, dev = len(layers), _current_device()
+    if n != cfg.n_layers or len(k_caches) != n or len(v_caches) != n:
+        raise ValueError(f"{cfg.n_layers} layers, as many caches of K and of V expected, got {n}, {len(k_caches)} and "
+                         f"{len(v_caches)}")
     warr = (epic_layer_weights_fp8 * n)(*layers)
     karr = (C.c_void_p * n)(*[_packed("k_caches", t, dev) for t in k_caches])
     varr = (C.c_void_p * n)(*[_packed("v_caches", t, dev) for t in v_caches])

@@ -226,6 +226,18 @@ def test_layer_and_model_refuse_tensors_of_other_memory(on_host):
     assert len(on_host) == 2
 
 
+def test_model_refuses_other_numbers_of_layers(on_host):
+    """The library reads cfg.n_layers entries of each list."""
+    good = _model_args()
+    for name in ("layers", "k_caches", "v_caches"):
+        for n in (0, 1, 3):
+            with pytest.raises(ValueError, match="2 layers"):
+                el.epic_link_model_fp8(**{**good, name: (good[name] * 2)[:n]})
+    with pytest.raises(ValueError, match="3 layers"):
+        el.epic_link_model_fp8(**{**good, "cfg": _model_args(3)["cfg"]})
+    assert not on_host
+
+
 # ---------------------------------------------------------------- the kernel chosen by sizes
 
 def route(epi, m, n, k):
