@@ -2,6 +2,7 @@
 // launches on the caller's stream.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "gemm8.h"
@@ -17,6 +18,19 @@ bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 epic_status hip_status(const char* what) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(EPIC_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+  return EPIC_OK;
+}
+
+// The sizes of a product (epilogue: Gemm8Epilogue).
+epic_status check_gemm_sizes(int epilogue, int32_t m, int32_t n, int32_t k) {
+  EPIC_CHECK_ARG(m >= 0 && n > 0 && k > 0, "m, n, k = %d, %d, %d", m, n, k);
+  const int per = epilogue == kGluOut || epilogue == kGluQuantOut ? 2 * kGroup : kGroup;
+  if (k % kGroup != 0 || n % per != 0)
+    return fail(EPIC_ERR_UNSUPPORTED, "k %% %d == 0 and n %% %d == 0 required (k = %d, n = %d)", kGroup, per, k, n);
+  // 31-bit byte offsets, of the fp32 partial sums of short row sets too (they fit the workspace)
+  const int64_t rows = int64_t(m) + 256, lim = int64_t(1) << 31;
+  if (rows * k >= lim || int64_t(n) * k >= lim || rows * n * 2 >= lim)
+    return fail(EPIC_ERR_UNSUPPORTED, "operands of %d x %d x %d exceed the 2^31-byte limit", m, n, k);
   return EPIC_OK;
 }
 
@@ -69,14 +83,8 @@ extern "C" epic_status epic_gemm_fp8(int32_t epilogue, const uint8_t* a, const u
                                      uint8_t* out_scale, void* workspace, size_t workspace_bytes, void* stream) {
   clear_error();
   EPIC_CHECK_ARG(epilogue >= EPIC_FP8_BF16 && epilogue <= EPIC_FP8_SWIGLU_FP8, "unknown epilogue %d", epilogue);
-  EPIC_CHECK_ARG(m >= 0 && n > 0 && k > 0, "m, n, k = %d, %d, %d", m, n, k);
-  const int per = epilogue == EPIC_FP8_BF16 ? kGroup : 2 * kGroup;
-  if (k % kGroup != 0 || n % per != 0)
-    return fail(EPIC_ERR_UNSUPPORTED, "k %% %d == 0 and n %% %d == 0 required (k = %d, n = %d)", kGroup, per, k, n);
-  // 31-bit byte offsets, of the fp32 partial sums of short row sets too (they fit the workspace)
-  const int64_t rows = int64_t(m) + 256, lim = int64_t(1) << 31;
-  if (rows * k >= lim || int64_t(n) * k >= lim || rows * n * 2 >= lim)
-    return fail(EPIC_ERR_UNSUPPORTED, "operands of %d x %d x %d exceed the 2^31-byte limit", m, n, k);
+  epic_status st = check_gemm_sizes(epilogue, m, n, k);
+  if (st != EPIC_OK) return st;
   if (m == 0) return EPIC_OK;
   EPIC_CHECK_ARG(a && a_scale && w && w_scale && aligned(a, 16) && aligned(w, 16),
                  "operands must be non-NULL, a and w 16-byte aligned");
@@ -96,8 +104,9 @@ extern "C" epic_status epic_gemm_fp8(int32_t epilogue, const uint8_t* a, const u
   return hip_status("8-bit GEMM launch");
 }
 
-// The kernel that a product of these sizes runs (epilogue: Gemm8Epilogue, kRopeOut too), or "" for sizes that are refused.  Host only and
-// not in the public header: it is for tests, each of which is about one kernel.
+// The kernel that the plan has for a product of these sizes (epilogue: Gemm8Epilogue, kRopeOut too), or "" where they are
+// not whole groups of 128.  It plans also what the entry points refuse for other reasons (SwiGLU of an odd number of
+// blocks, operands of 2^31 bytes).  Host only and not in the public header: it is for tests, each of which is about one kernel.
 extern "C" const char* epic_gemm_fp8_route_name(int32_t epilogue, int32_t m, int32_t n, int32_t k) {
   if (epilogue < kBf16Out || epilogue > kRopeOut || m <= 0 || n <= 0 || k <= 0 || n % kGroup != 0 || k % kGroup != 0)
     return "";
@@ -108,4 +117,19 @@ extern "C" const char* epic_gemm_fp8_route_name(int32_t epilogue, int32_t m, int
     return p.tm == 128 ? "narrow128x128" : p.tn == 256 ? "narrow64x256" : p.tn == 128 ? "narrow64x128" : "narrow64x64";
   if (p.kind == Gemm8Kind::kSplit) return p.tm == 256 ? "split256" : p.tm == 192 ? "split192" : "split128";
   return p.tm == 256 ? "whole256" : p.tm == 192 ? "whole192" : "whole128";
+}
+
+// The fp32 planes [m][n] of partial sums that such a product has at most (few rows: one, where its consumer adds it), or -1
+// for sizes that are refused.  For tests too.
+extern "C" int32_t epic_gemm_fp8_planes(int32_t epilogue, int32_t m, int32_t n, int32_t k) {
+  clear_error();
+  if (epilogue < kBf16Out || epilogue > kRopeOut || m == 0 || check_gemm_sizes(epilogue, m, n, k) != EPIC_OK) return -1;
+  const Gemm8Plan p = gemm8_plan(m, n, k, epilogue);
+  if (p.kind == Gemm8Kind::kFew) return 1;
+  if (p.kind == Gemm8Kind::kSplit) return p.parts;
+  if (p.kind != Gemm8Kind::kStream) return 0;
+  const StreamSum s = gemm8_stream_sum(m, n, k);
+  int planes = 0;
+  for (int tile = 0; tile < s.units / s.ks; ++tile) planes = std::max(planes, s.planes(tile));
+  return planes;
 }

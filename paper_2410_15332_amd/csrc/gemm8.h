@@ -64,6 +64,7 @@ StreamSum launch_gemm8_stream(const Gemm8Args& g, hipStream_t stream);
 bool gemm8_narrow_fits(int N, int K, int epi, int tm, int tn);
 void launch_gemm8_narrow(const Gemm8Args& g, int epi, int tm, int tn, hipStream_t stream);
 bool gemm8_stream_fits(int M, int N, int K);
+StreamSum gemm8_stream_sum(int M, int N, int K);   // how its tiles are dealt, without the planes' address
 StreamSum launch_gemm8_split(const Gemm8Args& g, int tm, int parts, hipStream_t stream);
 void launch_gemm8_wide(const Gemm8Args& g, int epi, int tm, hipStream_t stream);
 

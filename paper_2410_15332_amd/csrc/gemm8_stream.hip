@@ -317,18 +317,12 @@ __global__ __launch_bounds__(512, 1) void gemm8_stream_kernel(Gemm8Args g, Strea
 
 int cdiv(int a, int b) { return (a + b - 1) / b; }
 
-template <int TM, int TN, int NS>
-StreamSum launch_tm(const Gemm8Args& g, hipStream_t stream) {
-  StreamSum s{};
-  s.partial = g.partial;
-  s.M = g.M, s.N = g.N;
-  s.tm = TM, s.tn = TN;
-  s.m_tiles = cdiv(g.M, TM);
-  s.ks = g.K / kBK;
-  s.units = s.m_tiles * (g.N / TN) * s.ks;
-  s.G = s.units < kWorkers * kMinUnits ? cdiv(s.units, kMinUnits) : kWorkers;
-  gemm8_stream_kernel<kPlanesOut, TM, TN, 1, 1, 1, NS><<<s.G, (TM / 32) * (TN / 32) * 64, 0, stream>>>(g, s);
-  return s;
+constexpr int kStreamTN = 64;                           // columns of a streamed tile
+int stream_tm(int M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }   // ... and its rows
+
+template <int TM, int NS>
+void launch_stream_tm(const Gemm8Args& g, const StreamSum& s, hipStream_t stream) {
+  gemm8_stream_kernel<kPlanesOut, TM, kStreamTN, 1, 1, 1, NS><<<s.G, (TM / 32) * (kStreamTN / 32) * 64, 0, stream>>>(g, s);
 }
 
 template <int OUT, int TM, int TN, int RT, int CT, int KS, int NS>
@@ -346,8 +340,7 @@ void launch_whole(const Gemm8Args& g, hipStream_t stream) {
 }  // namespace
 
 bool gemm8_stream_fits(int M, int N, int K) {
-  const int tm = M <= 32 ? 32 : M <= 64 ? 64 : 128;
-  const int64_t units = int64_t(cdiv(M, tm)) * (N / 64) * (K / kBK);
+  const int64_t units = int64_t(cdiv(M, stream_tm(M))) * (N / kStreamTN) * (K / kBK);
   if (units >= (1 << 23)) return false;                 // 32-bit arithmetic of StreamSum::owner
   const int64_t per = std::max<int64_t>(units / kWorkers, 1);
   const int64_t planes = (K / kBK + per - 1) / per + 1;
@@ -376,10 +369,24 @@ void launch_gemm8_narrow(const Gemm8Args& g, int epi, int tm, int tn, hipStream_
   }
 }
 
+StreamSum gemm8_stream_sum(int M, int N, int K) {
+  StreamSum s{};
+  s.M = M, s.N = N;
+  s.tm = stream_tm(M), s.tn = kStreamTN;
+  s.m_tiles = cdiv(M, s.tm);
+  s.ks = K / kBK;
+  s.units = s.m_tiles * (N / s.tn) * s.ks;
+  s.G = s.units < kWorkers * kMinUnits ? cdiv(s.units, kMinUnits) : kWorkers;
+  return s;
+}
+
 StreamSum launch_gemm8_stream(const Gemm8Args& g, hipStream_t stream) {
-  if (g.M <= 32) return launch_tm<32, 64, 11>(g, stream);
-  if (g.M <= 64) return launch_tm<64, 64, 9>(g, stream);
-  return launch_tm<128, 64, 6>(g, stream);
+  StreamSum s = gemm8_stream_sum(g.M, g.N, g.K);
+  s.partial = g.partial;
+  if (s.tm == 32) launch_stream_tm<32, 11>(g, s, stream);
+  else if (s.tm == 64) launch_stream_tm<64, 9>(g, s, stream);
+  else launch_stream_tm<128, 6>(g, s, stream);
+  return s;
 }
 
 }  // namespace epic

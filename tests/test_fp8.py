@@ -285,3 +285,40 @@ def test_plans_keep_within_what_they_need():
                 name = route(e, m, n, 128)
                 planes = {"few": 1, "stream": 2}.get(name, 2 if name.startswith("split") else 0)
                 assert planes * 4 * m * n <= 64 << 20, (m, n, name)
+
+
+def planes(epi, m, n, k):
+    return el._lib.epic_gemm_fp8_planes(epi, m, n, k)
+
+
+@pytest.mark.parametrize("epi,m,n,k", [(1, 100, 384, 256), (2, 4, 128, 128), (0, 1 << 24, 1024, 128), (0, 4, 128, 64), (0, 4, 64, 128),
+                                       (0, 1, 1 << 24, 128), (0, (1 << 19) - 256, 128, 4096), (1, -1, 256, 128)])
+def test_refused_sizes_have_no_planes(epi, m, n, k):
+    """The query about partial sums and the entry point have one opinion on sizes."""
+    assert planes(epi, m, n, k) == -1
+    assert _gemm(epi=epi, m=m, n=n, k=k) in (INVALID, UNSUPPORTED)
+
+
+def test_largest_row_count():
+    """With 256 rows more the operands are below 2^31 bytes; of one row more they are not."""
+    m = (1 << 19) - 257
+    assert planes(0, m, 128, 4096) == 0 and planes(0, m + 1, 128, 4096) == -1
+
+
+def test_partial_sums_fit_the_workspace():
+    """Every plan's planes, whatever the sizes: many parts of a long k, many columns, all row counts of the kernels that
+    leave planes."""
+    rng = np.random.default_rng(10)
+    most, size = {}, el.epic_gemm_fp8_workspace_bytes()
+    for i in range(20000):
+        m = int(np.exp(rng.uniform(0, np.log(150 if i % 2 else 5000))))
+        n = 256 * int(np.exp(rng.uniform(0, np.log(1 << 14))))
+        k = 128 * int(np.exp(rng.uniform(0, np.log(2000))))
+        for e in range(4):
+            p = planes(e, m, n, k)
+            if p >= 0:
+                kind = route(e, m, n, k).rstrip("0123456789x")
+                assert p * 4 * m * n <= size, (e, m, n, k, kind, p)
+                assert (p == 0) == (kind in ("whole", "narrow")) and (kind != "split" or 2 <= p <= 16)
+                most[kind] = max(most.get(kind, 0), p)
+    assert most["few"] == 1 and most["split"] == 16 and most["stream"] > 2
