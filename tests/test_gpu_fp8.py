@@ -667,3 +667,45 @@ def test_binding_refuses_workspaces_of_other_memory():
     for bad in (u8(n, device="cpu"), u8(1).expand(n)):
         with pytest.raises(ValueError, match="workspace"):
             el.epic_gemm_fp8(el.FP8_BF16, u8(4, 256), u8(2, 4), u8(256, 256), u8(2, 2), out, workspace=bad)
+
+
+# ---------------------------------------------------------------- infinities, tiny results and sums that cancel, in every route
+
+def _overflowing(m, n, k):
+    """Operands whose first block of K is zero but for columns that some rows make overflow: those columns have +-1 at t = 0
+    and nothing else, and the rows 2^100 there (the product of gate and up overflows) or 448 * 2^127 (the sums themselves
+    do).  The first group of 128 consists of such columns.  Returns the operands, those rows and those columns."""
+    rng = np.random.default_rng([m, n, k])
+    f = n // 2
+    qa, ta, qw, tw = _operands(rng, m, n, k)
+    qa[:, :128], qw[:, :128], tw[:, 0] = 0, 0, 0
+    cols = np.unique(np.r_[np.arange(128), (128 * np.arange(f // 128)[:, None] + rng.integers(0, 128, (f // 128, 3))).ravel(), f - 1])
+    qw[cols], qw[f + cols] = 0, 0
+    qw[cols, 0], qw[f + cols, 0] = 0x38, np.where(rng.random(len(cols)) < 0.5, 0x38, 0xB8)   # +1, +-1
+    rows = np.unique(np.r_[rng.integers(0, m, max(1, m // 3)), m - 1])
+    most = rng.random(len(rows)) < 0.5
+    ta[:, 0] = 0
+    qa[rows, 0], ta[rows, 0] = np.where(most, 0x7E, 0x38), np.where(most, 127, 100)
+    return (qa, ta, qw, tw), rows, cols
+
+
+@pytest.mark.parametrize("m,n,k", BORDERS, ids=lambda x: str(x))
+def test_infinities_in_a_group_keep_its_scale(m, n, k):
+    """A group's infinities become NaN codes; its scale and its finite values are those that it has where the same
+    results are 0 (the finite columns' products with the overflowing block are exact zeros), and those are float64's."""
+    _say("gemm infinities", m, n, k)
+    (qa, ta, qw, tw), rows, cols = _overflowing(m, n, k)
+    none = qa.copy()
+    none[:, :128] = 0
+    clean, clean_t = _run_gemm("swiglu_fp8", none, ta, qw, tw)
+    at = np.unique(np.r_[rows[:40], 0, m - 1])
+    y, e = _products(fp8.dequantise(none[at], ta[at]), fp8.dequantise(qw, tw, 128))
+    gate, up, eg, eu = y[:, :n // 2], y[:, n // 2:], e[:, :n // 2], e[:, n // 2:]
+    y = _silu(gate) * up
+    _check_rounded(clean[at], clean_t[at], y, 1.1 * eg * (np.abs(up) + eu) + np.abs(_silu(gate)) * eu + 2.0 ** -19 * np.abs(y))
+    codes, t = _run_gemm("swiglu_fp8", qa, ta, qw, tw)
+    assert np.array_equal(t, clean_t) and np.all(t[:, 0] == 0)
+    bad = np.zeros(codes.shape, bool)
+    bad[np.ix_(rows, cols)] = True
+    assert np.all((codes[bad] & 0x7F) == 0x7F)
+    assert np.array_equal(codes[~bad], clean[~bad])
