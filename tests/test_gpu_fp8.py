@@ -709,3 +709,23 @@ def test_infinities_in_a_group_keep_its_scale(m, n, k):
     bad[np.ix_(rows, cols)] = True
     assert np.all((codes[bad] & 0x7F) == 0x7F)
     assert np.array_equal(codes[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("m,n,k", BORDERS, ids=lambda x: str(x))
+def test_groups_of_the_smallest_scales(m, n, k):
+    """Results from 2^-149 up to some 2^-100: scale bytes from 0 on, values below the smallest normal fp32 among
+    them.  Sums of small integers times powers of two are exact, silu(x) = x / 2 to 2^-60; the product of gate and up has
+    2^-19 like elsewhere and, below the normal range, half of fp32's smallest step."""
+    _say("gemm smallest scales", m, n, k)
+    rng = np.random.default_rng([n, m, k])
+    ia, iw = rng.integers(-2, 3, (m, k)), rng.integers(-2, 3, (n, k))
+    shift = rng.integers(-46, -20, m)
+    shift[0] = -44
+    ta, tw = np.repeat(shift[:, None], k // 128, 1), np.full((n // 128, k // 128), -32)
+    codes, t = _run_gemm("swiglu_fp8", fp8.e4m3_encode(ia.astype(float)), ta, fp8.e4m3_encode(iw.astype(float)), tw)
+    at = np.unique(np.r_[0, m - 1, rng.integers(0, m, 300)])
+    s = torch.from_numpy(ia[at]).cuda().double() @ torch.from_numpy(iw).cuda().double().t().contiguous()
+    s = s.cpu().numpy()
+    y = np.ldexp(s[:, :n // 2] * s[:, n // 2:], 2 * (shift[at] - 32)[:, None] - 1)
+    assert np.any(t[at] == -127) and (m < 30 or np.any(t[at] > -120))
+    _check_rounded(codes[at], t[at], y, 2.0 ** -19 * np.abs(y) + 2.0 ** -150)
