@@ -33,7 +33,9 @@ __device__ __forceinline__ i32x8 read32(const char* p, int c0, int c1) {
 // neighbouring scale, and another one by another route.  So where the largest, with bits
 // top, is within 2^-12 of a border (one group in 1400), that one result is computed again in
 // 64 bits, by all wavefronts of the workgroup, and decides.  Of 1.5 million groups none then
-// differs from float64's (87 before).  A result costs some 4 us where it holds up its
+// differs from float64's (87 before).  This is no guarantee: sums whose large products cancel
+// are farther off than the window is wide, and a result that is not the largest before it is
+// computed again, but would be after, is not looked at.  A result costs some 4 us where it holds up its
 // workgroup: 20560 x 28672 x 4096 1817 -> 1883 us, 736 rows 92 -> 95, 100 rows 33.5 -> 35.2.
 // In one tile some 1 us each: 736 times the same row, next to a border, 274 where others take 91.
 __device__ __forceinline__ bool near_border(uint32_t top) {

@@ -729,3 +729,27 @@ def test_groups_of_the_smallest_scales(m, n, k):
     y = np.ldexp(s[:, :n // 2] * s[:, n // 2:], 2 * (shift[at] - 32)[:, None] - 1)
     assert np.any(t[at] == -127) and (m < 30 or np.any(t[at] > -120))
     _check_rounded(codes[at], t[at], y, 2.0 ** -19 * np.abs(y) + 2.0 ** -150)
+
+
+@pytest.mark.parametrize("epi", list(EPI))
+@pytest.mark.parametrize("m,n,k", [(5, 512, 640), (100, 2048, 4096), (257, 768, 1152), (520, 8192, 1152)])
+def test_gemm_of_sums_that_cancel(m, n, k, epi):
+    """Two large products of each eight cancel and leave small ones: what the matrix cores drop is bounded by the largest
+    product, not by the result (which is then off by some 1e-2 of its norm, where other operands' are by 4e-5 at most)."""
+    _say("gemm cancelling", m, n, k, epi)
+    rng = np.random.default_rng([k, m, n])
+    qa, ta = fp8.e4m3_encode(rng.normal(size=(m, k))), rng.integers(-2, 3, (m, k // 128))
+    qw, tw = fp8.e4m3_encode(rng.normal(size=(n, k))), rng.integers(-7, -4, (n // 128, k // 128))
+    qa[:, ::8], qa[:, 1::8], qw[:, 1::8] = 0x7E, 0xFE, qw[:, ::8]        # 448 w - 448 w
+    y, e = _products(fp8.dequantise(qa, ta), fp8.dequantise(qw, tw, 128))
+    got = _run_gemm(epi, qa, ta, qw, tw)
+    if epi != "bf16":
+        gate, up, eg, eu = y[:, :n // 2], y[:, n // 2:], e[:, :n // 2], e[:, n // 2:]
+        y = _silu(gate) * up
+        e = 1.1 * eg * (np.abs(up) + eu) + np.abs(_silu(gate)) * eu + 2.0 ** -19 * np.abs(y)
+    if epi == "swiglu_fp8":
+        _check_rounded(got[0], got[1], y, e)
+    else:
+        assert np.all(np.abs(got - y) <= 2.0 ** -8 * np.abs(y) + (1 + 2.0 ** -8) * e)
+        print(f"[gpu-test] off by {np.linalg.norm(got - y) / np.linalg.norm(y):.1e} of the norm, {np.max(np.abs(got - y) / e):.2f} of e",
+              flush=True)
