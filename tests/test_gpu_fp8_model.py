@@ -162,3 +162,50 @@ def test_refusals():
     w.wo_scale = None
     with pytest.raises(el.EpicError):
         el.epic_link_layer_fp8(st.cfg, w, st.dplan, st.hidden, st.k_caches[0], st.v_caches[0], st.workspace)
+
+
+# ---------------------------------------------------------------- the other plans: re-rotated chunks, none to recompute, decode
+
+def _against_the_oracle(call, h_in, s_pos, w, cached_k, cached_v, n_total, wl, read):
+    """A layer call on the stream h_in (fp32, in place) against the oracle's, by the bars above.  read() returns the
+    recomputed K and V from the cache."""
+    hq, hkv, d = wl.num_q_heads, wl.num_kv_heads, wl.head_dim
+    before = h_in.double().cpu().numpy()
+    call()
+    torch.cuda.synchronize()
+    h, k, v, added = fp8.decoder_layer(before, s_pos, w, cached_k, cached_v, n_total, wl.ffn, hq, hkv, d, wl.rope_theta, wl.rms_eps)
+    gk, gv = read()
+    ek, ev = _norm(gk - k) / _norm(k), _norm(gv - v) / _norm(v)
+    eh = _norm(h_in.double().cpu().numpy() - h) / _norm(added[0] + added[1])
+    print(f"[gpu-test] k {ek:.2e} v {ev:.2e} added {eh:.2e}", flush=True)
+    assert ek <= 2.0 ** -8 and ev <= 2.0 ** -8 and eh <= 0.06
+
+
+RE_ROTATED = [(CASES[0], "stream"), (CASES[1], "stream"), (_wl("rr_one_row", [37, 20, 50], 1, 0, hidden=256, ffn=512, hq=4, hkv=4), "few"),
+              (_wl("rr_split_d128", [200, 150], 150, 100, hidden=4096, ffn=1024, hq=8, hkv=2, d=128, layers=1), "split128"), (CASES[4], "whole128"), (CASES[5], "whole128")]
+
+
+@pytest.mark.parametrize("wl,kernel", RE_ROTATED, ids=[w.name for w, _ in RE_ROTATED])
+def test_re_rotated_layers_against_the_oracle(wl, kernel):
+    """Re-rotated plans rotate and write in two launches where others take one: the recomputed K and V, what a layer adds
+    to the stream, and the rows that are only moved (within a bf16 step), of every layer."""
+    from paper_2410_15332_amd import epic_link as el
+    import ctypes as C
+    route = el._lib.epic_gemm_fp8_route_name
+    route.restype = C.c_char_p
+    hq, hkv, d = wl.num_q_heads, wl.num_kv_heads, wl.head_dim
+    st = _stage(wl, caches="synthetic", rerotate=True)
+    assert st.sizes.n_rerotated > 0 and route(3, st.sizes.n_s, (hq + 2 * hkv) * d, wl.hidden).decode() == kernel
+    s_pos = oracle.legolink_positions(wl.chunk_lens, wl.suffix_len, wl.k)
+    st.hidden.copy_(st.emb)
+    for layer in range(wl.n_layers):
+        caches = [synth.chunk_cache(wl.seed, j, n, hkv, d, 0.5, layer=layer) for j, n in enumerate(wl.chunk_lens)]
+        moved = oracle.rerotate_cached([_f64(c[0]) for c in caches], wl.chunk_lens, wl.rope_theta, True)
+        w = fp8.weights(synth.model_weights(wl.seed, layer, wl.hidden, wl.ffn, hq, hkv, d))
+        _against_the_oracle(lambda: _layer_call(st, layer, st.hidden), st.hidden, s_pos, w, moved, [_f64(c[1]) for c in caches],
+                            wl.linked_len, wl, lambda: _linked_rows(st, layer, s_pos))
+        K, V = el.read_linked_kv(_bits(st.k_caches[layer]), _bits(st.v_caches[layer]), st.views, 0)
+        keep = np.setdiff1d(np.arange(sum(wl.chunk_lens)), s_pos)
+        moved, v = np.concatenate(moved), np.concatenate([c[1] for c in caches])
+        assert np.abs(_f64(K[keep]) - moved[keep]).max() <= 2.0 ** -7 * np.abs(moved).max()
+        assert np.array_equal(V[keep], v[keep])
