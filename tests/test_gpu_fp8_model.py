@@ -209,3 +209,33 @@ def test_re_rotated_layers_against_the_oracle(wl, kernel):
         moved, v = np.concatenate(moved), np.concatenate([c[1] for c in caches])
         assert np.abs(_f64(K[keep]) - moved[keep]).max() <= 2.0 ** -7 * np.abs(moved).max()
         assert np.array_equal(V[keep], v[keep])
+
+
+def test_plans_without_rows():
+    """n_s = 0: the re-rotated copies are all that a call writes, by the layer, by the model, and as the bf16 entry
+    points write them; without re-rotation, nothing."""
+    from paper_2410_15332_amd import epic_link as el, harness
+    wl = _wl("no_rows", [37, 100, 16], 0, 0)
+    ref = harness.stage_model(wl, caches="synthetic", rerotate=True)
+    st = _stage(wl, caches="synthetic", rerotate=True)
+    assert st.sizes.n_s == 0 and st.sizes.n_rerotated > 0
+    fresh = [[_bits(t).copy() for t in c] for c in (st.k_caches, st.v_caches)]
+    ref.run()
+    for call in ("model", "layers"):
+        if call == "model":
+            st.run()
+        else:
+            for layer in range(wl.n_layers):
+                for t, bits in zip((st.k_caches[layer], st.v_caches[layer]), (fresh[0][layer], fresh[1][layer])):
+                    t.view(torch.int16).copy_(torch.from_numpy(bits.view(np.int16)))
+                el.epic_link_layer_fp8(st.cfg, st.layers[layer], st.dplan, None, st.k_caches[layer], st.v_caches[layer], None)
+        torch.cuda.synchronize()
+        for layer in range(wl.n_layers):
+            k, v = _bits(st.k_caches[layer]), _bits(st.v_caches[layer])
+            assert not np.array_equal(k, fresh[0][layer])
+            assert np.array_equal(k, _bits(ref.k_caches[layer])) and np.array_equal(v, _bits(ref.v_caches[layer]))
+    plain = _stage(wl, caches="synthetic")
+    before = [_bits(t).copy() for t in plain.k_caches + plain.v_caches]
+    plain.run()
+    torch.cuda.synchronize()
+    assert all(np.array_equal(a, _bits(t)) for a, t in zip(before, plain.k_caches + plain.v_caches))
