@@ -239,3 +239,62 @@ def test_plans_without_rows():
     plain.run()
     torch.cuda.synchronize()
     assert all(np.array_equal(a, _bits(t)) for a, t in zip(before, plain.k_caches + plain.v_caches))
+
+
+DECODE = [_wl("decode_d64", [37, 100, 16], 25, 5, layers=1), _wl("decode_d128", [40, 21], 18, 3, ffn=512, hq=4, hkv=2, d=128, layers=1)]
+
+
+@pytest.mark.parametrize("wl", DECODE, ids=[w.name for w in DECODE])
+def test_decode_of_two_requests(wl):
+    """Decode plans through the 8-bit layer after a link of two requests that share chunks: single tokens, then 3 and
+    10 at once.  Each request's new K and V and what the layer adds, against the oracle; all other rows keep their bits."""
+    from paper_2410_15332_amd import epic_link as el, harness
+    print(f"[gpu-test] fp8 decode {wl.name}", flush=True)
+    hq, hkv, d, H = wl.num_q_heads, wl.num_kv_heads, wl.head_dim, wl.hidden
+    bits = synth.model_weights(wl.seed, 0, H, wl.ffn, hq, hkv, d)
+    tw, layer = harness.quantise_layer({k: harness._bf16_tensor(v, "cuda") for k, v in bits.items()})
+    w = fp8.weights(bits)
+    cfg = harness.model_cfg(wl, 1)
+    chunks, pool, at = [], 80, 0
+    for n in wl.chunk_lens:
+        chunks.append(list(range(at, at + -(-n // 16))))
+        at += len(chunks[-1])
+    pick = [list(range(len(wl.chunk_lens))), [1, 0]]
+    reqs = [el.Request([wl.chunk_lens[j] for j in p], [chunks[j] for j in p], wl.suffix_len + 7 * i, wl.k) for i, p in enumerate(pick)]
+    gen = torch.Generator(device="cuda").manual_seed(wl.seed)
+    kc = torch.empty((pool, hkv, 16, d), dtype=torch.bfloat16, device="cuda").normal_(0, 0.5, generator=gen)
+    vc = torch.empty((pool, hkv, d, 16), dtype=torch.bfloat16, device="cuda").normal_(0, 0.5, generator=gen)
+
+    def step(sizes, host, views, cached):
+        """One layer call on a plan; per request checked where cached (its K and V before the new rows) is given."""
+        h = torch.randn(sizes.n_s, H, device="cuda", generator=gen)
+        before = h.double().cpu().numpy()
+        ws = torch.empty(max(256, el.epic_model_fp8_workspace_bytes(cfg, sizes)), dtype=torch.uint8, device="cuda")
+        el.epic_link_layer_fp8(cfg, layer, el.DevicePlan(sizes, host), h, kc, vc, ws)
+        torch.cuda.synchronize()
+        out, linked = h.double().cpu().numpy(), []
+        for b in range(2):
+            K, V = el.read_linked_kv(_bits(kc), _bits(vc), views, b)
+            linked.append((K, V))
+            if cached is None:
+                continue
+            rows = slice(int(views["s_off"][b]), int(views["s_off"][b + 1]))
+            pos, n = views["s_pos"][rows].astype(np.int64), len(cached[b][0])
+            assert np.array_equal(pos, np.arange(n, n + rows.stop - rows.start)) and len(K) == pos[-1] + 1
+            ref, k, v, added = fp8.decoder_layer(before[rows], pos, w, [_f64(cached[b][0])], [_f64(cached[b][1])], len(K), wl.ffn,
+                                                 hq, hkv, d, wl.rope_theta, wl.rms_eps)
+            ek, ev = _norm(_f64(K[pos]) - k) / _norm(k), _norm(_f64(V[pos]) - v) / _norm(v)
+            eh = _norm(out[rows] - ref) / _norm(added[0] + added[1])
+            print(f"[gpu-test] request {b}, {len(pos)} tokens: k {ek:.2e} v {ev:.2e} added {eh:.2e}", flush=True)
+            assert ek <= 2.0 ** -8 and ev <= 2.0 ** -8 and eh <= 0.06
+            assert np.array_equal(K[:n], cached[b][0]) and np.array_equal(V[:n], cached[b][1])
+        return linked
+
+    sizes, host, views = el.epic_plan_link(reqs, cfg.attn, list(range(at, 60)), pool)
+    linked = step(sizes, host, views, None)
+    free = [i for i in range(60, pool)]
+    for new in ([1, 1], [3, 10], [1, 1]):
+        sizes, host, views = el.epic_plan_decode(sizes, host, new, cfg.attn, free, pool)
+        assert sizes.n_s == sum(new) and (sum(new) > 2 or sizes.tile_rows == 16)
+        free = [i for i in free if i not in set(views["linked_blocks"].tolist())]
+        linked = step(sizes, host, views, linked)
