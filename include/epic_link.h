@@ -354,8 +354,8 @@ epic_status epic_link_model(const epic_model_cfg* cfg, const epic_layer_weights*
  *          EPIC_GEMM_RESIDUAL: c[i][j] += C[i][j]                      c: fp32 [m][n], in place
  *          EPIC_GEMM_SWIGLU:   act[i][j] = bf16(silu(C[i][j]) C[i][j + n/2]), j < n/2
  *                              (rows [0, n/2) of w: gate; [n/2, n): up)   act: bf16 [m][n/2]
- * Shapes: m >= 0, k % 64 == 0, n % 128 == 0, and with m rounded up to a multiple
- * of 256 every operand and output below 2^31 bytes; else EPIC_ERR_UNSUPPORTED.
+ * Shapes: m >= 0, k % 64 == 0, n % 128 == 0, and with 256 rows more than m every
+ * operand and output below 2^31 bytes; else EPIC_ERR_UNSUPPORTED.
  * Device pointers, 16-byte aligned.  workspace: at least epic_gemm_workspace_bytes()
  * bytes of device memory, 256-byte aligned, owned by the caller; it holds the
  * partial sums of products that are divided along k and the arrival counters of tiles
@@ -424,9 +424,8 @@ epic_status epic_rmsnorm_fp8(const float* x, const uint16_t* delta, const uint16
  * Where the largest value of a group of the quantised result, summed like that, is within 2^-12 of
  * where its scale changes, its 64-bit sum decides.  The scale is that of the exact sums then,
  * unless the group's sums cancel as above, or another of its values is as near to the same place.
- * Shapes: m >= 0, k % 128 == 0, n % 128 == 0 (SwiGLU: n % 256 == 0), and with m rounded up
- * to a multiple of 256 every operand and a bf16 [m][n] below 2^31 bytes; else
- * EPIC_ERR_UNSUPPORTED.  workspace: epic_gemm_fp8_workspace_bytes() bytes, 256-byte
+ * Shapes: m >= 0, k % 128 == 0, n % 128 == 0 (SwiGLU: n % 256 == 0), and with 256 rows more
+ * than m every operand and a bf16 [m][n] below 2^31 bytes; else EPIC_ERR_UNSUPPORTED.  workspace: epic_gemm_fp8_workspace_bytes() bytes, 256-byte
  * aligned, for partial sums; calls in flight at the same time need separate ones. */
 typedef enum { EPIC_FP8_BF16 = 0, EPIC_FP8_SWIGLU = 1, EPIC_FP8_SWIGLU_FP8 = 2 } epic_fp8_epilogue;
 size_t epic_gemm_fp8_workspace_bytes(void);
