@@ -35,9 +35,10 @@ __device__ __forceinline__ i32x8 read32(const char* p, int c0, int c1) {
 // 64 bits, by all wavefronts of the workgroup, and decides.  Of 1.5 million groups none then
 // differs from float64's (87 before).  This is no guarantee: sums whose large products cancel
 // are farther off than the window is wide, and a result that is not the largest before it is
-// computed again, but would be after, is not looked at.  A result costs some 4 us where it holds up its
-// workgroup: 20560 x 28672 x 4096 1817 -> 1883 us, 736 rows 92 -> 95, 100 rows 33.5 -> 35.2.
-// In one tile some 1 us each: 736 times the same row, next to a border, 274 where others take 91.
+// computed again, but would be after, is not looked at.  A result costs some
+// 4 us where it holds up its workgroup, with and without: 20560 x 28672 x 4096 1884 us and 1803, 100 rows 32.7
+// and 32.1, 32 rows 30.9 and 30.1; 736 rows 96-101 and 93-96.  In one tile some 1 us each: 736 times the
+// same row, next to a border, 272 where others take 89.
 __device__ __forceinline__ bool near_border(uint32_t top) {
   return abs(int(top & 0x7FFFFFu) - 0x600000) <= 3584;   // 1.75 * 2^23 * 2^-12
 }

@@ -7,9 +7,10 @@
 // to a plane of its own (stream_sum.h), LDS a ring of NS stages.  32 rows, N 4096, K 14 336:
 // 14.2 us (59 MB, 4.2 TB/s) and 1.9 to add the planes.
 //
-// Whole tiles have no second launch.  What bounds them is what a CU can load, some 90 GB/s: one
+// Whole tiles have no second launch.  What bounds them is mostly what a CU can load: one
 // tile alone takes 0.18, 0.29 and 0.44 us a stage for the 16, 24 and 32 KB of 64 x 64, 64 x 128
-// and 128 x 128, and a third less read from LDS per product changes nothing.  So larger
+// and 128 x 128 (91 to 74 GB/s, where loads alone of this shape reach 100), and a third less read from
+// LDS per product changes nothing.  So larger
 // tiles cost less per product, and smaller ones use more CUs.  501 rows, N = K = 4096: 64 x 64
 // tiles 22.9 us, 64 x 128 16.4, 128 x 128 21.2, 256-column tiles 22 at best.  SwiGLU of 100 rows,
 // N 28 672, K 4096: 128 x 128 29 us (121 MB, 4.1 TB/s), 64 x 128 37, planes 41; to e4m3, where
