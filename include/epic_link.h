@@ -425,7 +425,8 @@ epic_status epic_rmsnorm_fp8(const float* x, const uint16_t* delta, const uint16
  * where its scale changes, its 64-bit sum decides.  The scale is that of the exact sums then,
  * unless the group's sums cancel as above, or another of its values is as near to the same place.
  * Shapes: m >= 0, k % 128 == 0, n % 128 == 0 (SwiGLU: n % 256 == 0), and with 256 rows more
- * than m every operand and a bf16 [m][n] below 2^31 bytes; else EPIC_ERR_UNSUPPORTED.  workspace: epic_gemm_fp8_workspace_bytes() bytes, 256-byte
+ * than m every operand and a bf16 [m][n] below 2^31 bytes; else EPIC_ERR_UNSUPPORTED.
+ * workspace: epic_gemm_fp8_workspace_bytes() bytes, 256-byte
  * aligned, for partial sums; calls in flight at the same time need separate ones. */
 typedef enum { EPIC_FP8_BF16 = 0, EPIC_FP8_SWIGLU = 1, EPIC_FP8_SWIGLU_FP8 = 2 } epic_fp8_epilogue;
 size_t epic_gemm_fp8_workspace_bytes(void);
