@@ -753,3 +753,17 @@ def test_gemm_of_sums_that_cancel(m, n, k, epi):
         assert np.all(np.abs(got - y) <= 2.0 ** -8 * np.abs(y) + (1 + 2.0 ** -8) * e)
         print(f"[gpu-test] off by {np.linalg.norm(got - y) / np.linalg.norm(y):.1e} of the norm, {np.max(np.abs(got - y) / e):.2f} of e",
               flush=True)
+
+
+@pytest.mark.parametrize("m", [5, 40, 100, 300])
+def test_gemm_below_the_normal_range(m):
+    """Integers of up to 2^13 times 2^-140: every sum is a multiple of fp32's smallest step, so exact; what is left is bf16's rounding,
+    whose steps are 2^-133 there."""
+    _say("gemm below the normal range", m)
+    rng = np.random.default_rng(m)
+    n, k = 512, 640
+    ia, iw = rng.integers(-4, 5, (m, k)), rng.integers(-4, 5, (n, k))
+    t = lambda r: np.full((r, k // 128), -70, np.int64)  # noqa: E731
+    got = _run_gemm("bf16", fp8.e4m3_encode(ia.astype(float)), t(m), fp8.e4m3_encode(iw.astype(float)), t(n // 128))
+    ref = np.ldexp((ia @ iw.T).astype(np.float64), -140)
+    assert np.all(np.abs(got - ref) <= np.maximum(2.0 ** -8 * np.abs(ref), 2.0 ** -134))

@@ -298,3 +298,39 @@ def test_decode_of_two_requests(wl):
         assert sizes.n_s == sum(new) and (sum(new) > 2 or sizes.tile_rows == 16)
         free = [i for i in free if i not in set(views["linked_blocks"].tolist())]
         linked = step(sizes, host, views, linked)
+
+
+# streams longer than the norm's 4096 in registers at a time, with planes pending; and Q|K|V whose last column tile is half
+# past the end, after each kind of 256-column tiles
+WIDE = [
+    (_wl("long_8320", [40, 33], 9, 4, hidden=8320, ffn=256, hq=4, hkv=2), "stream"),
+    (_wl("long_20480", [40], 5, 0, hidden=20480, ffn=256, hq=2, hkv=1), "stream"),
+    (_wl("half_tile_d128", [700, 300], 250, 250, hidden=256, ffn=768, hq=3, hkv=3, d=128), "whole128"),
+    (_wl("half_tile_d64", [700, 300], 250, 250, hidden=256, ffn=512, hq=2, hkv=2), "whole128"),
+    (_wl("half_tile192", [64], 2049, 0, hidden=384, ffn=512, hq=11, hkv=11, d=128, layers=1), "whole192"),
+    (_wl("half_tile256", [64], 2049, 0, hidden=384, ffn=512, hq=17, hkv=17, d=128, layers=1), "whole256"),
+    (_wl("half_tile_split", [200, 100], 150, 100, hidden=4096, ffn=1024, hq=3, hkv=3, d=128, layers=1), "split128"),
+]
+
+
+@pytest.mark.parametrize("wl,kernel", WIDE, ids=[w.name for w, _ in WIDE])
+def test_wide_layers_against_the_oracle(wl, kernel):
+    from paper_2410_15332_amd import epic_link as el
+    import ctypes as C
+    route = el._lib.epic_gemm_fp8_route_name
+    route.restype = C.c_char_p
+    hq, hkv, d = wl.num_q_heads, wl.num_kv_heads, wl.head_dim
+    st = _stage(wl, caches="synthetic")
+    assert route(3, st.sizes.n_s, (hq + 2 * hkv) * d, wl.hidden).decode() == kernel
+    s_pos = oracle.legolink_positions(wl.chunk_lens, wl.suffix_len, wl.k)
+    st.hidden.copy_(st.emb)
+    for layer in range(wl.n_layers):
+        caches = [synth.chunk_cache(wl.seed, j, n, hkv, d, 0.5, layer=layer) for j, n in enumerate(wl.chunk_lens)]
+        w = fp8.weights(synth.model_weights(wl.seed, layer, wl.hidden, wl.ffn, hq, hkv, d))
+        _against_the_oracle(lambda: _layer_call(st, layer, st.hidden), st.hidden, s_pos, w, [_f64(c[0]) for c in caches],
+                            [_f64(c[1]) for c in caches], wl.linked_len, wl, lambda: _linked_rows(st, layer, s_pos))
+    alone = st.hidden.double()
+    st.run()
+    torch.cuda.synchronize()
+    ref = alone * torch.rsqrt(alone.square().mean(-1, keepdim=True) + wl.rms_eps) * st.final_norm.double()
+    assert bool(((st.out - ref).abs() <= 2.0 ** -20 * ref.abs()).all())
