@@ -397,7 +397,8 @@ epic_status epic_gemm(int32_t epilogue, const uint16_t* a, const uint16_t* w, in
 size_t epic_fp8_scale_bytes(int32_t m, int32_t k);
 
 /* Round x (bf16 [m][k]) to q and scale: as rows (block_rows == 1), or as weights
- * (block_rows == 128; the last block may have fewer rows). */
+ * (block_rows == 128; the last block may have fewer rows).  Up to 2^35 - 2^13 values, and 65535
+ * blocks of rows; more are EPIC_ERR_UNSUPPORTED (a launch has fewer than 2^32 threads). */
 epic_status epic_quant_fp8(const uint16_t* x, int32_t m, int32_t k, int32_t block_rows, uint8_t* q, uint8_t* scale,
                            void* stream);
 
@@ -406,7 +407,7 @@ epic_status epic_quant_fp8(const uint16_t* x, int32_t m, int32_t k, int32_t bloc
  * x, x_out: fp32 [m][hidden]; delta: bf16 [m][hidden] (a product of epic_gemm_fp8, say), or
  * NULL for none; weight: bf16 [hidden].  x_out receives s unless it is NULL; it may be x,
  * and else overlaps nothing.  Sums and statistics are fp32.  hidden % 128 == 0, at most
- * 32768. */
+ * 32768; up to 2^22 - 1 rows at any such width (2^23 - 2 up to 16384 wide), for the same reason. */
 epic_status epic_rmsnorm_fp8(const float* x, const uint16_t* delta, const uint16_t* weight, int32_t m, int32_t hidden,
                              float eps, float* x_out, uint8_t* q, uint8_t* scale, void* stream);
 
