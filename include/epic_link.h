@@ -467,6 +467,93 @@ epic_status epic_link_model_fp8(const epic_model_cfg* cfg, const epic_layer_weig
                                 float* out_hidden, void* workspace, size_t workspace_bytes,
                                 void* stream);
 
+/* ---------------------------------------------------------------- head norm and rotation */
+
+/* Rotary positions.  The first rot_dim dims of a head (a multiple of 16, at most head_dim; 0: none)
+ * are rot_dim / 2 pairs j: dims (j, j + rot_dim / 2), or (2 j, 2 j + 1) where interleaved == 1.
+ * Pair j turns by pos * f_j:
+ *   f_j = theta^(-2 j / rot_dim) * (keep_j + (1 - keep_j) / factor)
+ * keep_j = 0 where original_context == 0 (every frequency divided by factor), else, with
+ * turns_j = original_context * theta^(-2 j / rot_dim) / 2 pi the turns that pair j makes over the
+ * context the model was trained on, 0 up to low_turns, 1 from high_turns, and linear between.
+ * amplitude multiplies the rotated pairs.  factor == 0 and amplitude == 0 stand for 1. */
+typedef struct {
+  int32_t rot_dim;
+  int32_t interleaved;
+  float theta;
+  float factor;
+  int32_t original_context;
+  float low_turns;
+  float high_turns;
+  float amplitude;
+} epic_rope_cfg;
+
+/* Host only: freqs[rot_dim / 2] = f_j (float64, radians a position).  A caller uploads them once. */
+epic_status epic_rope_freqs(const epic_rope_cfg* rope, double* freqs);
+
+/* What stands between the Q|K|V product and the attention, in one pass: of every row, each query
+ * and key head is normed (y = x / sqrt(mean(x^2) + eps) * w, where its weight is given) and its
+ * first rot_dim dims are rotated at the row's position; V passes.  In fp32, from float64 angles,
+ * rounded to bf16 once.
+ * qkv: rows of q | k | v heads, (Hq + 2 Hkv) D values, ld values apart (a multiple of 16 bytes),
+ * in_type EPIC_QKV_BF16 (as epic_gemm_fp8 leaves them) or EPIC_QKV_FP32 (as epic_gemm does);
+ * pos [rows] (a plan's s_pos, say); freqs [rot_dim / 2] of epic_rope_freqs, in device memory (may
+ * be NULL where rot_dim == 0); q_norm, k_norm: bf16 [D] or NULL for no norm; q [rows][Hq][D], k, v
+ * [rows][Hkv][D] bf16, as epic_link_attention and epic_link_attention_kv8 take them.  Device
+ * pointers, 16-byte aligned (freqs 8); no two of input and outputs overlap.  Up to 2^24 - 4 rows. */
+typedef enum { EPIC_QKV_BF16 = 0, EPIC_QKV_FP32 = 1 } epic_qkv_type;
+epic_status epic_qk_norm_rope(const epic_attn_cfg* cfg, const epic_rope_cfg* rope, int32_t in_type, const void* qkv,
+                              int64_t ld, int32_t rows, const int32_t* pos, const double* freqs,
+                              const uint16_t* q_norm, const uint16_t* k_norm, float eps, uint16_t* q, uint16_t* k,
+                              uint16_t* v, void* stream);
+
+/* ---------------------------------------------------------------- cache in 8 bits */
+
+/* A paged cache of one layer in 8 bits, 0.51 of the bf16 one: blocks of 16 tokens; a row (the D
+ * values of K, or of V, of a token and KV head) is e4m3 values and one e8m0 byte by the rule of
+ * the 8-bit projections, t the smallest integer in [-127, 127] with max |y| <= 448 * 2^t.  A token
+ * of which a value of K or V is not finite is NaN: both bytes 255.
+ *   k      [num_blocks][Hkv][D / 64][4][16][16]     dim 64 j + 16 a + e of token s at [j][a][s][e]
+ *   v      [num_blocks][Hkv][D / 64][4][16][4][4]   dim 64 j + 16 t + r of token 4 a + c at [j][a][r][t][c]
+ *   scale  [num_blocks][Hkv][2][16]                 bytes of K, of V
+ * (the order in which the matrix cores take the values).  Device memory, 16-byte aligned.  In a
+ * cache that is written other than by this library, NaN tokens hold K all 0x7F and V all 0, and
+ * other tokens no NaN codes. */
+typedef struct {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* scale;
+  int32_t num_blocks;
+} epic_kv8_cache;
+
+/* Blocks of a bf16 cache (k_cache, v_cache: the layouts above, num_blocks blocks) to blocks of an
+ * 8-bit one, and back: src_blocks[i] into dst_blocks[i], i < n, whole blocks.  Lists in device
+ * memory; NULL stands for 0 .. n - 1.  The blocks of dst_blocks are distinct.  An entry with an id
+ * outside its pool moves nothing.  Back is exact, but for results outside bf16's range; NaN tokens
+ * are NaN in K and V. */
+epic_status epic_kv8_pack(const epic_attn_cfg* cfg, int32_t n, const int32_t* src_blocks, const uint16_t* k_cache,
+                          const uint16_t* v_cache, int32_t num_blocks, const int32_t* dst_blocks,
+                          const epic_kv8_cache* cache, void* stream);
+epic_status epic_kv8_unpack(const epic_attn_cfg* cfg, int32_t n, const int32_t* src_blocks, const epic_kv8_cache* cache,
+                            const int32_t* dst_blocks, uint16_t* k_cache, uint16_t* v_cache, int32_t num_blocks,
+                            void* stream);
+
+/* epic_link_attention over an 8-bit cache, with any plan (link, decode, compile):
+ *   1. every private block takes its source's bytes (K of re-rotated blocks: turned in fp32 and
+ *      rounded to 8 bits again), then the S rows k_s / v_s, rounded; a slot with neither holds zeros;
+ *   2. attention as there, over the values that the cache now holds, with fp32 sums, P rounded to
+ *      bf16.  A row that attends to a NaN token has NaN in out, and its lse means nothing; NaN in
+ *      tokens after a row, or in slots past a block's tokens, does not reach it.
+ * q_s, k_s, v_s, out, lse as there.  workspace: epic_link_kv8_workspace_bytes() bytes (0 without
+ * split-KV partials and wide tiles), 16-byte aligned; calls in flight at the same time need separate
+ * ones.  Plans of wide tiles (128 or 256 rows) keep their linked blocks in it in bf16, 64 D Hkv
+ * bytes each, for the time of the call. */
+size_t epic_link_kv8_workspace_bytes(const epic_attn_cfg* cfg, const epic_plan_sizes* sizes);
+epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const epic_plan_sizes* sizes, const epic_plan* plan_dev,
+                                    const uint16_t* q_s, const uint16_t* k_s, const uint16_t* v_s,
+                                    const epic_kv8_cache* cache, uint16_t* out, float* lse, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ Contents
                projections on their own.
   fp8.py    -- the 8-bit operands: rounding to e4m3 with power-of-two scales, and
                the decoder layer with its projections on them.
+  kv8.py    -- the 8-bit cache: its rows, their order, the link write, attention over it.
 
 Pins (tests/test_oracle_pins.py) tie each function to something other than
 itself: library causal attention (FR = full prefill, Sec. 2.3), the Naive

@@ -43,9 +43,7 @@ epic_status check_plan(const epic_plan_sizes* s, const epic_plan* p) {
 // Optional profiling events of the calling thread (see epic_set_profile_events).
 thread_local hipEvent_t g_prof_events[4] = {nullptr, nullptr, nullptr, nullptr};
 
-void record_event(int i, hipStream_t stream) {
-  if (g_prof_events[i]) (void)hipEventRecord(g_prof_events[i], stream);
-}
+void record_event(int i, hipStream_t stream) { record_profile_event(i, stream); }
 
 epic_status hip_status(const char* what) {
   hipError_t e = hipGetLastError();
@@ -68,22 +66,22 @@ extern "C" size_t epic_link_workspace_bytes(const epic_attn_cfg* cfg, const epic
 
 namespace epic {
 
-// Shared by epic_link_attention and the layer driver: link write, attention, combine.
-epic_status run_link_attention(const epic_attn_cfg* cfg, const epic_plan_sizes* s, const epic_plan* p,
-                               const uint16_t* q_s, const uint16_t* k_s, const uint16_t* v_s,
-                               uint16_t* k_cache, uint16_t* v_cache, uint16_t* out, float* lse,
-                               void* workspace, void* stream_ptr) {
-  hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
-  const bool written = k_s == nullptr && s->n_s > 0;
-  record_event(0, stream);
-  if (!written) {
-    if (s->n_rerotated > 0)
-      launch_link_write_rotated(p, s->n_private, cfg->num_kv_heads, cfg->head_dim, cfg->rope_theta, k_s, v_s, k_cache,
-                                v_cache, stream);
-    else
-      launch_link_write(p, s->n_private, cfg->num_kv_heads, cfg->head_dim, k_s, v_s, k_cache, v_cache, stream);
-  }
-  if (s->n_s == 0) return hip_status("link write launch");   // re-rotated copies only
+void record_profile_event(int i, hipStream_t stream) {
+  if (g_prof_events[i]) (void)hipEventRecord(g_prof_events[i], stream);
+}
+
+epic_status check_attention(const epic_attn_cfg* cfg, const epic_plan_sizes* sizes, const epic_plan* plan_dev) {
+  epic_status st = validate_attn_cfg(cfg);
+  if (st != EPIC_OK) return st;
+  st = check_plan(sizes, plan_dev);
+  if (st != EPIC_OK) return st;
+  if (sizes->n_rerotated > 0 && !(cfg->rope_theta > 1.0f))
+    return fail(EPIC_ERR_INVALID_ARG, "plan re-rotates cached K: rope_theta %g must be > 1", cfg->rope_theta);
+  return EPIC_OK;
+}
+
+AttnArgs attention_args(const epic_attn_cfg* cfg, const epic_plan_sizes* s, const epic_plan* p, const uint16_t* q_s,
+                        const uint16_t* k_cache, const uint16_t* v_cache, uint16_t* out, float* lse, void* workspace) {
   AttnArgs a{};
   a.s_pos = p->s_pos;
   a.linked_blocks = p->linked_blocks;
@@ -107,6 +105,26 @@ epic_status run_link_attention(const epic_attn_cfg* cfg, const epic_plan_sizes* 
   a.rows_per_tile = s->tile_rows / a.G;
   const float scale = cfg->softmax_scale > 0.0f ? cfg->softmax_scale : 1.0f / std::sqrt(float(cfg->head_dim));
   a.scale_log2 = scale * kLog2eHost;
+  return a;
+}
+
+// Shared by epic_link_attention and the layer driver: link write, attention, combine.
+epic_status run_link_attention(const epic_attn_cfg* cfg, const epic_plan_sizes* s, const epic_plan* p,
+                               const uint16_t* q_s, const uint16_t* k_s, const uint16_t* v_s,
+                               uint16_t* k_cache, uint16_t* v_cache, uint16_t* out, float* lse,
+                               void* workspace, void* stream_ptr) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
+  const bool written = k_s == nullptr && s->n_s > 0;
+  record_event(0, stream);
+  if (!written) {
+    if (s->n_rerotated > 0)
+      launch_link_write_rotated(p, s->n_private, cfg->num_kv_heads, cfg->head_dim, cfg->rope_theta, k_s, v_s, k_cache,
+                                v_cache, stream);
+    else
+      launch_link_write(p, s->n_private, cfg->num_kv_heads, cfg->head_dim, k_s, v_s, k_cache, v_cache, stream);
+  }
+  if (s->n_s == 0) return hip_status("link write launch");   // re-rotated copies only
+  const AttnArgs a = attention_args(cfg, s, p, q_s, k_cache, v_cache, out, lse, workspace);
   record_event(1, stream);
   if (s->tile_rows == kTileRowsTiny)
     launch_link_decode(a, cfg->head_dim, s->n_work, stream);
@@ -126,12 +144,8 @@ extern "C" epic_status epic_link_attention(const epic_attn_cfg* cfg, const epic_
                                            uint16_t* out, float* lse, void* workspace, size_t workspace_bytes,
                                            void* stream) {
   clear_error();
-  epic_status st = validate_attn_cfg(cfg);
+  epic_status st = check_attention(cfg, sizes, plan_dev);
   if (st != EPIC_OK) return st;
-  st = check_plan(sizes, plan_dev);
-  if (st != EPIC_OK) return st;
-  if (sizes->n_rerotated > 0 && !(cfg->rope_theta > 1.0f))
-    return fail(EPIC_ERR_INVALID_ARG, "plan re-rotates cached K: rope_theta %g must be > 1", cfg->rope_theta);
   if (sizes->n_s == 0 && sizes->n_private == 0) return EPIC_OK;
   EPIC_CHECK_ARG(k_cache && v_cache && aligned16(k_cache) && aligned16(v_cache), "KV caches NULL or unaligned");
   if (sizes->n_s == 0)

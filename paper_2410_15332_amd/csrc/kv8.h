@@ -1,0 +1,42 @@
+// Cache blocks in 8 bits: e4m3 values and, for each token and KV head, one power-of-two scale
+// (an e8m0 byte) for its K and one for its V.  Host side of kv8.hip and kv8_attention.hip;
+// arguments are validated by the callers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.h"
+
+namespace epic {
+
+// Bytes of a (block, KV head): values of K, as many of V, and 16 + 16 scales.
+constexpr int kKv8Scales = 32;
+constexpr int kKv8Nan = 255;                  // scale byte of a token whose K or V is not finite
+
+// Launches stay below 2^31 workgroups of 4 (block, KV head) pairs.
+inline int64_t kv8_groups(int64_t n, int hkv) { return n * ((hkv + 3) / 4); }
+constexpr int64_t kKv8MaxGroups = (int64_t(1) << 24) - 1;        // x 256 threads < 2^32
+
+struct Kv8Move {
+  const int32_t* src;                         // block ids, or null for 0 .. n - 1
+  const int32_t* dst;
+  int n, src_blocks, dst_blocks;              // ids outside their pool are passed over
+  int hkv;
+};
+
+void launch_kv8_pack(const Kv8Move& mv, int head_dim, const uint16_t* k, const uint16_t* v, const epic_kv8_cache& c,
+                     hipStream_t stream);
+void launch_kv8_unpack(const Kv8Move& mv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
+                       hipStream_t stream);
+// The linked blocks of a plan as a bf16 cache of their own, [n_linked_blocks], for the attention kernel of
+// wide tiles, and the table 0 .. n_linked_blocks - 1 that it reads them by.  Tokens that are NaN get K = NaN, V = 0.
+void launch_kv8_expand(const int32_t* linked_blocks, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k,
+                       uint16_t* v, int32_t* table, hipStream_t stream);
+// As launch_link_write and launch_link_write_rotated (rope_theta is read where blocks move).
+void launch_kv8_write(const epic_plan* plan, int n_private, bool rotated, int hkv, int head_dim, float rope_theta,
+                      const uint16_t* k_s, const uint16_t* v_s, const epic_kv8_cache& c, hipStream_t stream);
+// As launch_link_decode; a.k_cache and a.v_cache are not read.
+void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, int head_dim, int n_work, hipStream_t stream);
+
+}  // namespace epic

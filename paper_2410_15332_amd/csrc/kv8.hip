@@ -1,0 +1,342 @@
+// The 8-bit cache: blocks from a bf16 cache and back, and the link write of an 8-bit cache.
+//
+// A row y (the D values of K or of V of a token and KV head) is stored as q = e4m3(y / 2^t),
+// rounded once, to nearest even, with t the smallest integer such that max |y| <= 448 2^t.  A
+// power of two costs no relative precision against a finer scale (e4m3 has an exponent of its
+// own), and attention applies it after the products: K's to the scores, V's to the
+// probabilities, where it is exact.  A token of which a value of K or V is not finite is
+// stored as NaN, both rows: byte 255, K all NaN, V all 0.  Whatever attends to it gets NaN
+// from the score; whatever does not meets only the zeros, since a weight of 0 times a NaN in
+// V would be NaN.
+//
+// One wavefront per (block, KV head), the slab in registers (kv8_device.h); all four kernels
+// read and write their bytes once and are bound by that.
+#include <cmath>
+
+#include "kv8_device.h"
+
+namespace epic {
+
+namespace {
+
+constexpr int kWaves = 4;                     // KV heads per workgroup
+constexpr int kThreads = 64 * kWaves;
+
+// The (list entry, KV head) of this wavefront.
+struct Place {
+  int i, g;
+  __device__ __forceinline__ explicit Place(int hkv) {
+    const int ng = (hkv + kWaves - 1) / kWaves;
+    i = int(blockIdx.x) / ng;
+    g = (int(blockIdx.x) % ng) * kWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  }
+};
+
+// Four bf16 (two pairs), each over its own 2^(byte - 127), as e4m3.  NaN rows (255) hold zeros in V.
+__device__ __forceinline__ uint32_t round4_each(uint32_t lo, uint32_t hi, const int (&b)[4]) {
+  auto in = [&](uint32_t bits, int byte) {
+    return byte == kKv8Nan ? 0.0f : __builtin_amdgcn_ldexpf(__uint_as_float(bits), 127 - byte);
+  };
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(in(lo << 16, b[0]), in(lo & 0xFFFF0000u, b[1]), 0, false);
+  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(in(hi << 16, b[2]), in(hi & 0xFFFF0000u, b[3]), r, true));
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const uint16_t* __restrict__ k,
+                                                            const uint16_t* __restrict__ v, epic_kv8_cache c) {
+  constexpr int J = D / 64;
+  const Place at(mv.hkv);
+  if (at.g >= mv.hkv) return;
+  const int src = mv.src ? mv.src[at.i] : at.i, dst = mv.dst ? mv.dst[at.i] : at.i;
+  if (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks)) return;
+  const int lane = threadIdx.x & 63, r = lane & 15, a = lane >> 4;
+  const size_t from = (size_t(src) * mv.hkv + at.g) * 16 * D, to = (size_t(dst) * mv.hkv + at.g) * 16 * D;
+  uint4 x[2 * J];
+  uint2 y[4 * J];                              // tokens 4 a .. of dims 16 i + r
+#pragma unroll
+  for (int i = 0; i < 2 * J; ++i)
+    x[i] = *reinterpret_cast<const uint4*>(k + from + r * D + 64 * (i >> 1) + 16 * a + 8 * (i & 1));
+#pragma unroll
+  for (int i = 0; i < 4 * J; ++i) y[i] = *reinterpret_cast<const uint2*>(v + from + (16 * i + r) * 16 + 4 * a);
+  int kb = kv8_byte(row_top<J>(x));
+  uint32_t m0 = 0, m1 = 0;
+#pragma unroll
+  for (int i = 0; i < 4 * J; ++i) {
+    m0 = pair_max(m0, pair_abs(y[i].x));
+    m1 = pair_max(m1, pair_abs(y[i].y));
+  }
+  m0 = row16_pair_max(m0);
+  m1 = row16_pair_max(m1);
+  int vb[4] = {kv8_byte(m0 & 0xFFFFu), kv8_byte(m0 >> 16), kv8_byte(m1 & 0xFFFFu), kv8_byte(m1 >> 16)};
+  const bool bad = kb == kKv8Nan || vb[0] == kKv8Nan || vb[1] == kKv8Nan || vb[2] == kKv8Nan || vb[3] == kKv8Nan;
+  if (__ballot(bad)) {                         // a token that is NaN in K or V is so in both
+    uint32_t tokens = uint32_t(__ballot(kb == kKv8Nan)) & 0xFFFFu;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t b = __ballot(vb[i] == kKv8Nan);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tokens |= uint32_t(b >> (16 * q) & 1) << (4 * q + i);
+    }
+    if (tokens >> r & 1) kb = kKv8Nan;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (tokens >> (4 * a + i) & 1) vb[i] = kKv8Nan;
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    uint4 q = round16(x[2 * j], x[2 * j + 1], kb);
+    if (kb == kKv8Nan) q = make_uint4(kNanBytes, kNanBytes, kNanBytes, kNanBytes);
+    *reinterpret_cast<uint4*>(c.k + to + 1024 * j + 16 * lane) = q;
+    *reinterpret_cast<uint4*>(c.v + to + 1024 * j + 16 * lane) =
+        make_uint4(round4_each(y[4 * j].x, y[4 * j].y, vb), round4_each(y[4 * j + 1].x, y[4 * j + 1].y, vb),
+                   round4_each(y[4 * j + 2].x, y[4 * j + 2].y, vb), round4_each(y[4 * j + 3].x, y[4 * j + 3].y, vb));
+  }
+  uint8_t* s = c.scale + (size_t(dst) * mv.hkv + at.g) * kKv8Scales;
+  if (lane < 16) s[lane] = uint8_t(kb);
+  if (r == 0) *reinterpret_cast<uint32_t*>(s + 16 + 4 * a) = vb[0] | vb[1] << 8 | vb[2] << 16 | uint32_t(vb[3]) << 24;
+}
+
+// The values of 8-bit blocks in bf16, as a cache of the other kind.  Exact, but for results
+// outside bf16's range.  EXPAND: for the attention kernel, block i of the list into block i;
+// K = NaN, V = 0 for NaN tokens (that kernel multiplies masked V by 0).  Else NaN in both.
+template <int D, bool EXPAND>
+__global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_kv8_cache c, uint16_t* __restrict__ k,
+                                                              uint16_t* __restrict__ v, int32_t* __restrict__ table) {
+  constexpr int J = D / 64;
+  const Place at(mv.hkv);
+  if (at.g >= mv.hkv) return;
+  const int src = mv.src ? mv.src[at.i] : at.i, dst = EXPAND || !mv.dst ? at.i : mv.dst[at.i];
+  if (!EXPAND && (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks))) return;
+  const int lane = threadIdx.x & 63, r = lane & 15, a = lane >> 4;
+  const size_t from = (size_t(src) * mv.hkv + at.g) * 16 * D, to = (size_t(dst) * mv.hkv + at.g) * 16 * D;
+  uint4 x[J], y[J];
+  const uint8_t* s = c.scale + (size_t(src) * mv.hkv + at.g) * kKv8Scales;
+  const int kb = s[r];
+  const uint32_t vw = *reinterpret_cast<const uint32_t*>(s + 16 + 4 * a);
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    x[j] = *reinterpret_cast<const uint4*>(c.k + from + 1024 * j + 16 * lane);
+    y[j] = *reinterpret_cast<const uint4*>(c.v + from + 1024 * j + 16 * lane);
+  }
+  // over the scale and then times it, in fp32: both exact, and no scale of 2^-127 as a float
+  auto wide = [&](uint32_t w, int b0, int b1, int b2, int b3) {
+    auto one = [&](float f, int b) {
+      const float z = __builtin_amdgcn_ldexpf(f, b - 127);
+      return b == kKv8Nan ? (EXPAND ? 0.0f : __uint_as_float(0x7FC00000u)) : z;
+    };
+    return make_uint2(pack_bf16x2(one(__builtin_amdgcn_cvt_f32_fp8(int(w), 0), b0), one(__builtin_amdgcn_cvt_f32_fp8(int(w), 1), b1)),
+                      pack_bf16x2(one(__builtin_amdgcn_cvt_f32_fp8(int(w), 2), b2), one(__builtin_amdgcn_cvt_f32_fp8(int(w), 3), b3)));
+  };
+  constexpr uint32_t kNanPair = 0x7FC07FC0u;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w}, u[4] = {y[j].x, y[j].y, y[j].z, y[j].w};
+    uint2 q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      q[i] = wide(w[i], kb, kb, kb, kb);
+      if (EXPAND && kb == kKv8Nan) q[i] = make_uint2(kNanPair, kNanPair);
+    }
+    uint4* kp = reinterpret_cast<uint4*>(k + to + r * D + 64 * j + 16 * a);
+    kp[0] = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
+    kp[1] = make_uint4(q[2].x, q[2].y, q[3].x, q[3].y);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      *reinterpret_cast<uint2*>(v + to + (64 * j + 16 * t + r) * 16 + 4 * a) =
+          wide(u[t], vw & 255, vw >> 8 & 255, vw >> 16 & 255, vw >> 24);
+  }
+  if (EXPAND && at.g == 0 && lane == 0) table[at.i] = at.i;
+}
+
+// The link write: every private block takes what its source block holds (ROTATE: K turned by
+// priv_rot, from its 8-bit values to 8 bits again), then the rows of S, rounded to 8 bits, in
+// their slots.  A slot that neither fills holds a row of zeros.  A block that is its own
+// source is read whole before it is written, by one wavefront.
+//
+// V rows come like K's, 16 dims of a token a lane; their e4m3 bytes change places through
+// LDS, a row of 64 + 4 bytes per token and 64 dims.
+template <int D, bool ROTATE>
+__global__ __launch_bounds__(kThreads) void kv8_write_kernel(const int32_t* __restrict__ priv_block,
+                                                             const int32_t* __restrict__ priv_src,
+                                                             const int32_t* __restrict__ priv_rows,
+                                                             const int32_t* __restrict__ priv_rot,
+                                                             const uint16_t* __restrict__ k_s,
+                                                             const uint16_t* __restrict__ v_s, epic_kv8_cache c, int hkv,
+                                                             double log2_theta) {
+  constexpr int J = D / 64, LD = 68;
+  __shared__ uint32_t turn[kWaves][J][16 * LD / 4];
+  __shared__ float2 cs[ROTATE ? D / 2 : 1];
+  const Place at(hkv);
+  const int g = min(at.g, hkv - 1);            // all wavefronts meet at the barriers
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, a = lane >> 4;
+  const int dst = priv_block[at.i], src = priv_src[at.i];
+  const int rot = ROTATE && src >= 0 ? priv_rot[at.i] : 0;
+  const int row = priv_rows[at.i * 16 + r];
+  const int32_t* rows4 = priv_rows + at.i * 16 + 4 * a;
+  const bool fresh = row >= 0;
+
+  uint4 x[2 * J], y[2 * J], kq[J], vq[J];
+  int kb = 127;                                // a row of zeros
+  uint32_t vw = 0x7F7F7F7Fu;
+#pragma unroll
+  for (int i = 0; i < 2 * J; ++i) {
+    x[i] = y[i] = make_uint4(0, 0, 0, 0);
+    if (fresh) {
+      const size_t from = (size_t(row) * hkv + g) * D + 64 * (i >> 1) + 16 * a + 8 * (i & 1);
+      x[i] = *reinterpret_cast<const uint4*>(k_s + from);
+      y[i] = *reinterpret_cast<const uint4*>(v_s + from);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) kq[j] = vq[j] = make_uint4(0, 0, 0, 0);
+  if (src >= 0) {
+    const size_t from = (size_t(src) * hkv + g) * 16 * D;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      kq[j] = *reinterpret_cast<const uint4*>(c.k + from + 1024 * j + 16 * lane);
+      vq[j] = *reinterpret_cast<const uint4*>(c.v + from + 1024 * j + 16 * lane);
+    }
+    const uint8_t* s = c.scale + (size_t(src) * hkv + g) * kKv8Scales;
+    kb = s[r];
+    vw = *reinterpret_cast<const uint32_t*>(s + 16 + 4 * a);
+  }
+  if constexpr (ROTATE) {
+    if (rot != 0) {                            // one block per workgroup: all of its wavefronts or none
+      if (threadIdx.x < D / 2) {
+        double sn, cn;
+        sincos(double(rot) * exp2(-double(2 * int(threadIdx.x)) / double(D) * log2_theta), &sn, &cn);
+        cs[threadIdx.x] = make_float2(float(cn), float(sn));
+      }
+      __syncthreads();
+      float f[16 * J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const uint32_t w[4] = {kq[j].x, kq[j].y, kq[j].z, kq[j].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f[16 * j + 4 * i] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 0);
+          f[16 * j + 4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 1);
+          f[16 * j + 4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 2);
+          f[16 * j + 4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 3);
+        }
+      }
+      // the values over their scale: turning commutes with it, and nothing overflows
+      uint32_t top = 0;
+      float z[16 * J];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if constexpr (J == 2) {                // dims 16 a + e and 64 more
+          const float2 t = cs[16 * a + e];
+          z[e] = f[e] * t.x - f[16 + e] * t.y;
+          z[16 + e] = f[16 + e] * t.x + f[e] * t.y;
+          top = max(top, max(finite_abs(z[e]), finite_abs(z[16 + e])));
+        } else {                               // the partner is 32 dims, 32 lanes away
+          const float2 t = cs[16 * (a & 1) + e];
+          const float o = __shfl_xor(f[e], 32);
+          z[e] = a < 2 ? f[e] * t.x - o * t.y : f[e] * t.x + o * t.y;
+          top = max(top, finite_abs(z[e]));
+        }
+      }
+      top = max(top, uint32_t(__shfl_xor(int(top), 16)));
+      top = max(top, uint32_t(__shfl_xor(int(top), 32)));
+      if (kb != kKv8Nan) {
+        // z is over 2^(kb - 127), and so is its scale; rows of bf16 leave bytes far below 254
+        const int byte = top == 0 ? 127 : min(max(scale_byte(top) + kb - 127, 0), kKv8Nan - 1), t = byte - kb + 127;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+          kq[j] = make_uint4(pack_e4m3x4(z[16 * j], z[16 * j + 1], z[16 * j + 2], z[16 * j + 3], t),
+                             pack_e4m3x4(z[16 * j + 4], z[16 * j + 5], z[16 * j + 6], z[16 * j + 7], t),
+                             pack_e4m3x4(z[16 * j + 8], z[16 * j + 9], z[16 * j + 10], z[16 * j + 11], t),
+                             pack_e4m3x4(z[16 * j + 12], z[16 * j + 13], z[16 * j + 14], z[16 * j + 15], t));
+        kb = byte;
+      }
+    }
+  }
+  // the rows of S
+  int nk = kv8_byte(row_top<J>(x)), nv = kv8_byte(row_top<J>(y));
+  if (nk == kKv8Nan || nv == kKv8Nan) nk = nv = kKv8Nan;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    uint4 q = round16(x[2 * j], x[2 * j + 1], nk), p = round16(y[2 * j], y[2 * j + 1], nv);
+    if (nk == kKv8Nan) {
+      q = make_uint4(kNanBytes, kNanBytes, kNanBytes, kNanBytes);
+      p = make_uint4(0, 0, 0, 0);
+    }
+    if (fresh) kq[j] = q;
+    uint32_t* to = &turn[wave][j][(r * LD + 16 * a) / 4];
+    to[0] = p.x, to[1] = p.y, to[2] = p.z, to[3] = p.w;
+  }
+  if (fresh) kb = nk;
+  __syncthreads();
+  // this lane's tokens 4 a ..: their bytes and their scale
+  const uint32_t mask = (rows4[0] >= 0 ? 0xFFu : 0u) | (rows4[1] >= 0 ? 0xFF00u : 0u) |
+                        (rows4[2] >= 0 ? 0xFF0000u : 0u) | (rows4[3] >= 0 ? 0xFF000000u : 0u);
+  uint32_t nvw = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) nvw |= uint32_t(__shfl(nv, 4 * a + i)) << (8 * i);
+  vw = (vw & ~mask) | (nvw & mask);
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(turn[wave][j]);
+    uint32_t w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      w[t] = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[t] |= uint32_t(from[(4 * a + i) * LD + 16 * t + r]) << (8 * i);
+    }
+    vq[j] = make_uint4((vq[j].x & ~mask) | (w[0] & mask), (vq[j].y & ~mask) | (w[1] & mask),
+                       (vq[j].z & ~mask) | (w[2] & mask), (vq[j].w & ~mask) | (w[3] & mask));
+  }
+  if (at.g >= hkv) return;
+  const size_t to = (size_t(dst) * hkv + g) * 16 * D;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    *reinterpret_cast<uint4*>(c.k + to + 1024 * j + 16 * lane) = kq[j];
+    *reinterpret_cast<uint4*>(c.v + to + 1024 * j + 16 * lane) = vq[j];
+  }
+  uint8_t* s = c.scale + (size_t(dst) * hkv + g) * kKv8Scales;
+  if (lane < 16) s[lane] = uint8_t(kb);
+  if (r == 0) *reinterpret_cast<uint32_t*>(s + 16 + 4 * a) = vw;
+}
+
+unsigned grid_of(int n, int hkv) { return unsigned(kv8_groups(n, hkv)); }
+
+}  // namespace
+
+void launch_kv8_pack(const Kv8Move& mv, int head_dim, const uint16_t* k, const uint16_t* v, const epic_kv8_cache& c,
+                     hipStream_t stream) {
+  auto go = [&](auto kernel) { kernel<<<grid_of(mv.n, mv.hkv), kThreads, 0, stream>>>(mv, k, v, c); };
+  if (head_dim == 128) go(kv8_pack_kernel<128>);
+  else go(kv8_pack_kernel<64>);
+}
+
+void launch_kv8_unpack(const Kv8Move& mv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
+                       hipStream_t stream) {
+  auto go = [&](auto kernel) { kernel<<<grid_of(mv.n, mv.hkv), kThreads, 0, stream>>>(mv, c, k, v, nullptr); };
+  if (head_dim == 128) go(kv8_unpack_kernel<128, false>);
+  else go(kv8_unpack_kernel<64, false>);
+}
+
+void launch_kv8_expand(const int32_t* linked_blocks, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k,
+                       uint16_t* v, int32_t* table, hipStream_t stream) {
+  Kv8Move mv{};
+  mv.src = linked_blocks, mv.n = n, mv.hkv = hkv;
+  auto go = [&](auto kernel) { kernel<<<grid_of(n, hkv), kThreads, 0, stream>>>(mv, c, k, v, table); };
+  if (head_dim == 128) go(kv8_unpack_kernel<128, true>);
+  else go(kv8_unpack_kernel<64, true>);
+}
+
+void launch_kv8_write(const epic_plan* plan, int n_private, bool rotated, int hkv, int head_dim, float rope_theta,
+                      const uint16_t* k_s, const uint16_t* v_s, const epic_kv8_cache& c, hipStream_t stream) {
+  if (n_private == 0) return;
+  const double l2t = rotated ? std::log2(double(rope_theta)) : 0.0;
+  auto go = [&](auto kernel) {
+    kernel<<<grid_of(n_private, hkv), kThreads, 0, stream>>>(plan->priv_block, plan->priv_src, plan->priv_rows, plan->priv_rot,
+                                                             k_s, v_s, c, hkv, l2t);
+  };
+  if (rotated) head_dim == 128 ? go(kv8_write_kernel<128, true>) : go(kv8_write_kernel<64, true>);
+  else head_dim == 128 ? go(kv8_write_kernel<128, false>) : go(kv8_write_kernel<64, false>);
+}
+
+}  // namespace epic

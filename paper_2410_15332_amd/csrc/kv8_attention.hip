@@ -1,0 +1,295 @@
+// Causal attention (Eq. 1) over the 8-bit linked cache for tiles of 16 query rows: decode.
+//
+// Workgroup = (work item, KV head), 4 wavefronts, tile rows and items as in the bf16 kernel of
+// such tiles.  A wavefront takes pairs of the item's linked blocks, 32 keys, through a ring of
+// registers:
+//   S^T (16 keys x 16 rows) = K Q^T per block by v_mfma_f32_16x16x32_bf16, K's bytes widened in
+//     registers (exact); lane l = r + 16 a holds the scores of row r for keys 4 a + i, which
+//     are scaled by their keys' 2^t;
+//   online softmax per row in the scaled log2 domain; the running maximum lags by up to kLag,
+//     so that rows are merged over lanes and the output is rescaled only when one grows past it;
+//   O^T (D x 16) += V^T P^T by v_mfma_f32_16x16x32_bf16 over both blocks' keys: the P operand of
+//     a lane is its own 8 probabilities times their keys' 2^t (exact), rounded to bf16, and V's
+//     is the dword of 4 keys of its dim that the cache's order keeps together, for each block.
+// What bounds it is the read of K and V, once per item.
+#include <cmath>
+
+#include "kv8_device.h"
+#include "plan_internal.h"
+
+namespace epic {
+
+namespace {
+
+constexpr int kDecRows = 16;
+constexpr int kDecWaves = 4;
+constexpr float kLag = 8.0f;
+
+template <int D>
+struct Kv8DecodeLds {
+  float m[kDecWaves][kDecRows];
+  float l[kDecWaves][kDecRows];
+  float o[kDecWaves][D][kDecRows];
+};
+
+// What a wavefront holds of a block in flight.
+template <int J>
+struct Kv8Block {
+  uint4 k[J], v[J];
+  uint32_t ks, vs;                            // scales of keys 4 a ..
+};
+
+template <int D, int RING>
+__global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs a, epic_kv8_cache c) {
+  constexpr int J = D / 64;
+  constexpr int NDT = D / 16;                 // 16-dim tiles of O^T
+  __shared__ Kv8DecodeLds<D> lds;
+
+  const int hkv = a.hkv;
+  const int g = blockIdx.x % hkv;
+  const int item = blockIdx.x / hkv;
+  const int32_t* wk = a.work + kWorkInts * item;
+  const int tile = wk[0], b0 = wk[1], b1 = wk[2], kind = wk[7];
+  if (tile < 0) return;                       // list entries of other items
+  const int row0 = a.tiles[4 * tile + 0];
+  const int32_t* list = a.work + kWorkInts * wk[6] + 2;   // kItemShared, kItemList: entry i at i / 6 * 8 + i % 6
+  auto listed = [&](int i) __attribute__((always_inline)) { return list[i / kExtInts * kWorkInts + i % kExtInts]; };
+  const int nrows = kind == kItemShared ? wk[5] : a.tiles[4 * tile + 1];
+  // S row, partial (-1: the output) and row within its request's tile of row s
+  auto slot = [&](int s, int& srow, int& part, int& lr) __attribute__((always_inline)) {
+    if (kind == kItemShared) {
+      srow = listed(2 * s);
+      const int to = listed(2 * s + 1);
+      part = to < 0 ? -1 : to / kDecRows;
+      lr = to < 0 ? 0 : to % kDecRows;
+    } else {
+      srow = row0 + s;
+      part = wk[3];
+      lr = s;
+    }
+  };
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15;                    // tile row of this lane
+  const int qd = lane >> 4;                   // its quarter: keys 4 qd ..
+  const int R = a.rows_per_tile;
+  const int srl = r % R;
+  const int h = g * a.G + r / R;
+  const bool row_ok = srl < nrows;
+  int srow, part_, lr_;
+  slot(row_ok ? srl : nrows - 1, srow, part_, lr_);
+  // shared blocks precede every row of the item; a row that is none sees nothing
+  const int qpos = !row_ok ? -1 : kind == kItemShared ? 0x7fffffff : a.s_pos[srow];
+
+  bf16x8 qf[2 * J];                           // Q^T operand: row r, dims 64 j + 16 qd + 8 e ..
+  {
+    const uint16_t* qp = a.q + (size_t(srow) * a.hq + h) * D + qd * 16;
+#pragma unroll
+    for (int i = 0; i < 2 * J; ++i) {
+      bf16x8 x = *reinterpret_cast<const bf16x8*>(qp + 64 * (i >> 1) + 8 * (i & 1));
+      qf[i] = row_ok ? x : bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+  }
+
+  const float sl2 = a.scale_log2;
+  const size_t blk_bytes = size_t(hkv) * 16 * D, blk_scales = size_t(hkv) * kKv8Scales;
+  const uint8_t* kbase = c.k + size_t(g) * 16 * D + 16 * lane;
+  const uint8_t* vbase = c.v + size_t(g) * 16 * D + 16 * lane;
+  const uint8_t* sbase = c.scale + size_t(g) * kKv8Scales + 4 * qd;
+  auto load = [&](int phys, Kv8Block<J>& x) __attribute__((always_inline)) {
+    const size_t at = size_t(phys) * blk_bytes;
+    const uint8_t* sp = sbase + size_t(phys) * blk_scales;
+    x.ks = *reinterpret_cast<const uint32_t*>(sp);
+    x.vs = *reinterpret_cast<const uint32_t*>(sp + 16);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      x.k[j] = *reinterpret_cast<const uint4*>(kbase + at + 1024 * j);
+      x.v[j] = *reinterpret_cast<const uint4*>(vbase + at + 1024 * j);
+    }
+  };
+
+  f32x4 o[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = -INFINITY, lsum = 0.0f;           // lsum: of this lane's keys
+
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  // one block's scores, in the log2 domain: masked past the block's end, after the row
+  auto scores = [&](const Kv8Block<J>& x, int pos0, int len, float (&s)[4]) __attribute__((always_inline)) {
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const uint4 w = x.k[j];
+      const u32x4 lo = {e4m3_pair<false>(w.x, 1.0f), e4m3_pair<true>(w.x, 1.0f), e4m3_pair<false>(w.y, 1.0f),
+                        e4m3_pair<true>(w.y, 1.0f)};
+      const u32x4 hi = {e4m3_pair<false>(w.z, 1.0f), e4m3_pair<true>(w.z, 1.0f), e4m3_pair<false>(w.w, 1.0f),
+                        e4m3_pair<true>(w.w, 1.0f)};
+      acc = mfma_16x16x32(__builtin_bit_cast(bf16x8, lo), qf[2 * j], acc);
+      acc = mfma_16x16x32(__builtin_bit_cast(bf16x8, hi), qf[2 * j + 1], acc);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = qd * 4 + i;
+      const bool ok = key < len && pos0 + key <= qpos;
+      s[i] = ok ? __builtin_amdgcn_ldexpf(acc[i] * sl2, int(x.ks >> (8 * i) & 255u) - 127) : -INFINITY;
+    }
+  };
+
+  // The wavefront's blocks, in pairs: block i of its own (i = 2 p + e) is b0 + 2 (wave + 4 p) + e.
+  // Their ids, positions and lengths come 64 at a time, one per lane, so that no load of a block
+  // waits for a chain of loads; past the item's end stands its last block, with no keys.
+  const int n_pairs = (b1 - b0 + 1) / 2;
+  const int mine = n_pairs > wave ? 2 * ((n_pairs - wave + kDecWaves - 1) / kDecWaves) : 0;
+  for (int first = 0; first < mine; first += 64) {
+    int phys_l, pos_l, len_l;
+    {
+      const int i = first + lane;
+      const int b = b0 + 2 * (wave + kDecWaves * (i >> 1)) + (i & 1);
+      const bool in = i < mine && b < b1;
+      const int bc = in ? b : b1 - 1;
+      const int lb = kind == kItemList ? listed(bc) : bc;
+      phys_l = a.linked_blocks[lb];
+      pos_l = a.block_pos0[lb];
+      len_l = in ? a.block_len[lb] : 0;
+    }
+    const int n = min(64, mine - first) / 2;  // pairs of this batch
+    Kv8Block<J> ring[RING][2];
+#pragma unroll
+    for (int j = 0; j < RING; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) load(__builtin_amdgcn_readlane(phys_l, 2 * min(j, n - 1) + e), ring[j][e]);
+    for (int base = 0; base < n; base += RING) {
+#pragma unroll
+      for (int j = 0; j < RING; ++j) {
+        const int p = base + j;
+        if (p < n) {
+          float s[8];
+          const int len0 = __builtin_amdgcn_readlane(len_l, 2 * p), len1 = __builtin_amdgcn_readlane(len_l, 2 * p + 1);
+          {
+            float t0[4], t1[4];
+            scores(ring[j][0], __builtin_amdgcn_readlane(pos_l, 2 * p), len0, t0);
+            scores(ring[j][1], __builtin_amdgcn_readlane(pos_l, 2 * p + 1), len1, t1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = t0[i], s[4 + i] = t1[i];
+          }
+          float mb = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+          if (__ballot(mb > m + kLag)) {      // a row's maximum grew past the lag (at first: from nothing)
+            mb = fmaxf(mb, __shfl_xor(mb, 16));
+            mb = fmaxf(mb, __shfl_xor(mb, 32));
+            const bool grow = mb > m + kLag;  // row by row: a row's result depends on no other row
+            const float alpha = grow ? fast_exp2(m - mb) : 1.0f;
+            m = grow ? mb : m;
+            lsum *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[dt][i] *= alpha;
+          }
+          const float m_use = m == -INFINITY ? 0.0f : m;
+          float pv[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float q = fast_exp2(s[i] - m_use);
+            lsum += q;
+            pv[i] = __builtin_amdgcn_ldexpf(q, int((i < 4 ? ring[j][0].vs : ring[j][1].vs) >> (8 * (i & 3)) & 255u) - 127);
+          }
+          const u32x4 pw = {pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
+                            pack_bf16x2(pv[6], pv[7])};
+          const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
+          // slots past a block's end may hold any bits, and a weight of 0 would not hide NaN
+          uint32_t keep0 = 0xFFFFFFFFu, keep1 = 0xFFFFFFFFu;
+          if (len0 < 16 || len1 < 16) {
+            auto mask = [&](int len) {
+              const int k = len - 4 * qd;
+              return k >= 4 ? 0xFFFFFFFFu : k <= 0 ? 0u : 0xFFFFFFFFu >> (32 - 8 * k);
+            };
+            keep0 = mask(len0);
+            keep1 = mask(len1);
+          }
+#pragma unroll
+          for (int q = 0; q < J; ++q) {
+            const uint4 v0 = ring[j][0].v[q], v1 = ring[j][1].v[q];
+            const uint32_t w0[4] = {v0.x & keep0, v0.y & keep0, v0.z & keep0, v0.w & keep0};
+            const uint32_t w1[4] = {v1.x & keep1, v1.y & keep1, v1.z & keep1, v1.w & keep1};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const u32x4 vv = {e4m3_pair<false>(w0[t], 1.0f), e4m3_pair<true>(w0[t], 1.0f), e4m3_pair<false>(w1[t], 1.0f),
+                                e4m3_pair<true>(w1[t], 1.0f)};
+              o[4 * q + t] = mfma_16x16x32(__builtin_bit_cast(bf16x8, vv), pb, o[4 * q + t]);
+            }
+          }
+        }
+        // refill, past the batch's end with its last pair: every slot always has the same loads in flight
+        if (n > RING)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) load(__builtin_amdgcn_readlane(phys_l, 2 * min(p + RING, n - 1) + e), ring[j][e]);
+      }
+    }
+  }
+
+  __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): the ring's last loads land before the exit
+
+  lsum += __shfl_xor(lsum, 16);
+  lsum += __shfl_xor(lsum, 32);
+  // merge the wavefronts: O^T of lane l holds dims 16 dt + 4 qd + i of row r
+  if (qd == 0) {
+    lds.m[wave][r] = m;
+    lds.l[wave][r] = lsum;
+  }
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lds.o[wave][dt * 16 + qd * 4 + i][r] = o[dt][i];
+  __syncthreads();
+  // thread -> (row rr, dims dd, dd + 16, ...): 16 rows x 16 dim groups
+  const int rr = tid & 15, d0 = tid >> 4;
+  float mw[kDecWaves], M = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kDecWaves; ++w) {
+    mw[w] = lds.m[w][rr];
+    M = fmaxf(M, mw[w]);
+  }
+  const float Mu = M == -INFINITY ? 0.0f : M;
+  float wt[kDecWaves], L = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kDecWaves; ++w) {
+    wt[w] = fast_exp2(mw[w] - Mu);
+    L += lds.l[w][rr] * wt[w];
+  }
+  const int s2 = rr % R;
+  if (s2 >= nrows) return;
+  int srow2, part, lr2;
+  slot(s2, srow2, part, lr2);
+  const int hh = rr / R, h2 = g * a.G + hh, rp = hh * R + lr2;   // rp: its row in its request's tile
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  for (int d = d0; d < D; d += 16) {
+    float acc = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kDecWaves; ++w) acc += lds.o[w][d][rr] * wt[w];
+    acc *= inv;
+    if (part < 0)
+      a.out[(size_t(srow2) * a.hq + h2) * D + d] = uint16_t(pack_bf16x2(acc, 0.0f) & 0xFFFFu);
+    else
+      a.part_o[((size_t(part) * hkv + g) * kDecRows + rp) * D + d] = acc;
+  }
+  if (d0 == 0) {
+    if (part < 0) {
+      if (a.lse) a.lse[size_t(srow2) * a.hq + h2] = (M + fast_log2(L)) * kLn2;
+    } else {
+      a.part_lse[(size_t(part) * hkv + g) * kDecRows + rp] = L == 0.0f ? -INFINITY : M + fast_log2(L);
+    }
+  }
+}
+
+}  // namespace
+
+void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, int head_dim, int n_work, hipStream_t stream) {
+  if (n_work == 0) return;
+  const dim3 grid{unsigned(n_work) * unsigned(a.hkv)};
+  if (head_dim == 128) kv8_decode_kernel<128, 2><<<grid, 64 * kDecWaves, 0, stream>>>(a, c);
+  else kv8_decode_kernel<64, 3><<<grid, 64 * kDecWaves, 0, stream>>>(a, c);
+}
+
+}  // namespace epic

@@ -90,6 +90,16 @@ class epic_layer_weights_fp8(C.Structure):
                                           "w_gate_up_scale", "w_down", "w_down_scale")]
 
 
+class epic_rope_cfg(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("theta", C.c_float), ("factor", C.c_float),
+                ("original_context", C.c_int32), ("low_turns", C.c_float), ("high_turns", C.c_float),
+                ("amplitude", C.c_float)]
+
+
+class epic_kv8_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("scale", C.c_void_p), ("num_blocks", C.c_int32)]
+
+
 def _proto(name, restype, argtypes):
     f = getattr(_lib, name)
     f.restype = restype
@@ -161,19 +171,36 @@ _link_model_fp8 = _proto("epic_link_model_fp8", C.c_int,
                           _P(epic_plan), C.c_void_p, _P(C.c_void_p), _P(C.c_void_p), C.c_void_p, C.c_void_p,
                           C.c_size_t, C.c_void_p])
 
+_rope_freqs = _proto("epic_rope_freqs", C.c_int, [_P(epic_rope_cfg), C.c_void_p])
+_qk_norm_rope = _proto("epic_qk_norm_rope", C.c_int,
+                       [_P(epic_attn_cfg), _P(epic_rope_cfg), C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
+                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p])
+_kv8_pack = _proto("epic_kv8_pack", C.c_int,
+                   [_P(epic_attn_cfg), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                    _P(epic_kv8_cache), C.c_void_p])
+_kv8_unpack = _proto("epic_kv8_unpack", C.c_int,
+                     [_P(epic_attn_cfg), C.c_int32, C.c_void_p, _P(epic_kv8_cache), C.c_void_p, C.c_void_p, C.c_void_p,
+                      C.c_int32, C.c_void_p])
+_link_kv8_ws = _proto("epic_link_kv8_workspace_bytes", C.c_size_t, [_P(epic_attn_cfg), _P(epic_plan_sizes)])
+_link_attention_kv8 = _proto("epic_link_attention_kv8", C.c_int,
+                             [_P(epic_attn_cfg), _P(epic_plan_sizes), _P(epic_plan), C.c_void_p, C.c_void_p, C.c_void_p,
+                              _P(epic_kv8_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p])
+
 EXPORTED = ["epic_status_string", "epic_last_error", "epic_version", "epic_plan_sizes_get", "epic_plan_layout",
             "epic_plan_link", "epic_link_workspace_bytes", "epic_link_attention", "epic_set_profile_events",
             "epic_model_workspace_bytes", "epic_link_layer", "epic_link_model", "epic_gemm_workspace_bytes",
             "epic_gemm", "epic_plan_decode_sizes", "epic_plan_decode", "epic_plan_compile_sizes",
             "epic_plan_compile", "epic_link_attention_noalloc", "epic_fp8_scale_bytes", "epic_quant_fp8",
             "epic_rmsnorm_fp8", "epic_gemm_fp8_workspace_bytes", "epic_gemm_fp8", "epic_model_fp8_workspace_bytes",
-            "epic_link_layer_fp8", "epic_link_model_fp8"]
+            "epic_link_layer_fp8", "epic_link_model_fp8", "epic_rope_freqs", "epic_qk_norm_rope", "epic_kv8_pack",
+            "epic_kv8_unpack", "epic_link_kv8_workspace_bytes", "epic_link_attention_kv8"]
 
 NOALLOC_SCRATCH_BYTES = 96 << 20      # EPIC_NOALLOC_SCRATCH_BYTES
 
 GEMM_STORE, GEMM_RESIDUAL, GEMM_SWIGLU = 0, 1, 2
 FP8_BF16, FP8_SWIGLU, FP8_SWIGLU_FP8 = 0, 1, 2      # epilogues of epic_gemm_fp8
 FP8_GROUP = 128                       # values that share a scale
+QKV_BF16, QKV_FP32 = 0, 1             # input types of epic_qk_norm_rope
 
 
 def _check(st: int, where: str):
@@ -572,6 +599,138 @@ def epic_link_model_fp8(cfg: epic_model_cfg, layers: Sequence[epic_layer_weights
                            C.byref(dplan.plan), _packed("hidden_s", hidden_s, dev), karr, varr,
                            _packed("out_hidden", out_hidden, dev), ws, ws_bytes, _raw_stream(stream, dev)),
            "epic_link_model_fp8")
+
+
+# ---------------------------------------------------------------- head norm and rotation
+
+def rope_cfg(rot_dim: int, theta: float, interleaved: bool = False, factor: float = 1.0, original_context: int = 0,
+             low_turns: float = 0.0, high_turns: float = 0.0, amplitude: float = 1.0) -> epic_rope_cfg:
+    return epic_rope_cfg(rot_dim, int(interleaved), theta, factor, original_context, low_turns, high_turns, amplitude)
+
+
+def epic_rope_freqs(rope: epic_rope_cfg) -> np.ndarray:
+    """Frequencies of the rotated pairs, float64 [rot_dim / 2], for the caller to upload once."""
+    out = np.zeros(max(0, rope.rot_dim // 2), np.float64)
+    _check(_rope_freqs(C.byref(rope), out.ctypes.data), "epic_rope_freqs")
+    return out
+
+
+def epic_qk_norm_rope(cfg: epic_attn_cfg, rope: epic_rope_cfg, qkv, pos, freqs, q, k, v, q_norm=None, k_norm=None,
+                      eps: float = 1e-6, stream=None):
+    """Enqueue the norm and rotation of Q|K|V rows (see include/epic_link.h): qkv [n, (Hq + 2 Hkv) D] in
+    bf16 or fp32, whose rows may be apart; pos int32 [n]; freqs float64 [rot_dim / 2]; q [n, Hq, D], k, v
+    [n, Hkv, D] bf16; q_norm, k_norm bf16 [D] or None."""
+    import torch
+
+    bf16, f32 = _dtypes()[:2]
+    dev = _device_of("qkv", qkv)
+    hq, hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
+    if qkv.dim() != 2 or qkv.shape[1] != (hq + 2 * hkv) * d or qkv.stride(1) != 1:
+        raise ValueError(f"qkv: rows of {(hq + 2 * hkv) * d} values expected, got {tuple(qkv.shape)} with strides {qkv.stride()}")
+    if qkv.dtype not in bf16 + f32:
+        raise ValueError(f"qkv: {bf16[0]} or {f32[0]} expected, got {qkv.dtype}")
+    n = qkv.shape[0]
+    ld = qkv.stride(0) if n > 1 else qkv.shape[1]     # a single row's stride says nothing
+    if rope.rot_dim:
+        _expect("freqs", freqs, (rope.rot_dim // 2,), (torch.float64,), dev)
+    _check(_qk_norm_rope(C.byref(cfg), C.byref(rope), QKV_FP32 if qkv.dtype in f32 else QKV_BF16, qkv.data_ptr(), ld, n,
+                         _expect("pos", pos, (n,), (torch.int32,), dev), _ptr(freqs) if rope.rot_dim else None,
+                         None if q_norm is None else _expect("q_norm", q_norm, (d,), bf16, dev),
+                         None if k_norm is None else _expect("k_norm", k_norm, (d,), bf16, dev), eps,
+                         _expect("q", q, (n, hq, d), bf16, dev), _expect("k", k, (n, hkv, d), bf16, dev),
+                         _expect("v", v, (n, hkv, d), bf16, dev), _raw_stream(stream, dev)), "epic_qk_norm_rope")
+
+
+# ---------------------------------------------------------------- cache in 8 bits
+
+def kv8_shapes(num_blocks: int, hkv: int, d: int):
+    """Shapes of the three parts of an 8-bit cache: k, v and scale."""
+    return ((num_blocks, hkv, d // 64, 4, 16, 16), (num_blocks, hkv, d // 64, 4, 16, 4, 4), (num_blocks, hkv, 2, 16))
+
+
+class Kv8Cache:
+    """An 8-bit cache of one layer (see include/epic_link.h): three tensors of kv8_shapes(), uint8 or torch's
+    8-bit float types, which stay the caller's."""
+
+    def __init__(self, k, v, scale):
+        if k.dim() != 6 or k.shape[2] not in (1, 2):
+            raise ValueError(f"k: [blocks, Hkv, D / 64, 4, 16, 16] expected, got {tuple(k.shape)}")
+        _, _, e4m3, e8m0 = _dtypes()
+        self.num_blocks, self.hkv, self.d = k.shape[0], k.shape[1], 64 * k.shape[2]
+        self.device = k.get_device()
+        shapes = kv8_shapes(self.num_blocks, self.hkv, self.d)
+        at = [_expect(name, t, shape, dtypes, self.device) for name, t, shape, dtypes in
+              zip(("k", "v", "scale"), (k, v, scale), shapes, (e4m3, e4m3, e8m0))]
+        self.k, self.v, self.scale = k, v, scale
+        self.c = epic_kv8_cache(*at, self.num_blocks)
+
+    @classmethod
+    def zeros(cls, num_blocks: int, hkv: int, d: int, device="cuda"):
+        import torch
+
+        return cls(*(torch.zeros(s, dtype=torch.uint8, device=device) for s in kv8_shapes(num_blocks, hkv, d)))
+
+    def of(self, hkv: int, d: int, device: int):
+        """Its C form, for a call with these heads on this device."""
+        if (self.hkv, self.d) != (hkv, d):
+            raise ValueError(f"8-bit cache: {hkv} KV heads of {d} expected, got {self.hkv} of {self.d}")
+        if self.device != device:
+            raise ValueError(f"8-bit cache: expected on device {device}, got one of {self.device}")
+        return C.byref(self.c)
+
+
+def _kv8_move(k_cache, v_cache, cache: Kv8Cache, src_blocks, dst_blocks, pools):
+    """What the moves between a bf16 and an 8-bit cache share: device, config, number of blocks and addresses."""
+    import torch
+
+    bf16 = _dtypes()[0]
+    dev = _device_of("k_cache", k_cache)
+    blocks, (hkv, d) = k_cache.shape[0], (cache.hkv, cache.d)
+    lists = [t for t in (src_blocks, dst_blocks) if t is not None]
+    n = len(lists[0]) if lists else min(pools)
+    if not lists and pools[0] != pools[1]:
+        raise ValueError(f"lists of blocks are needed between pools of {pools[0]} and {pools[1]} blocks")
+    at = [None if t is None else _expect(name, t, (n,), (torch.int32,), dev) for name, t in
+          (("src_blocks", src_blocks), ("dst_blocks", dst_blocks))]
+    return (dev, attn_cfg(hkv, hkv, d), n, at[0], at[1], _expect("k_cache", k_cache, (blocks, hkv, 16, d), bf16, dev),
+            _expect("v_cache", v_cache, (blocks, hkv, d, 16), bf16, dev), cache.of(hkv, d, dev))
+
+
+def epic_kv8_pack(k_cache, v_cache, cache: Kv8Cache, src_blocks=None, dst_blocks=None, stream=None):
+    """Enqueue blocks src_blocks of a bf16 cache -> blocks dst_blocks of an 8-bit one (int32 lists in device
+    memory; None: 0 .. n - 1)."""
+    dev, cfg, n, src, dst, k, v, c = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks,
+                                               (k_cache.shape[0], cache.num_blocks))
+    _check(_kv8_pack(C.byref(cfg), n, src, k, v, k_cache.shape[0], dst, c, _raw_stream(stream, dev)), "epic_kv8_pack")
+
+
+def epic_kv8_unpack(cache: Kv8Cache, k_cache, v_cache, src_blocks=None, dst_blocks=None, stream=None):
+    """Enqueue blocks src_blocks of an 8-bit cache -> blocks dst_blocks of a bf16 one."""
+    dev, cfg, n, src, dst, k, v, c = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks,
+                                               (cache.num_blocks, k_cache.shape[0]))
+    _check(_kv8_unpack(C.byref(cfg), n, src, c, dst, k, v, k_cache.shape[0], _raw_stream(stream, dev)), "epic_kv8_unpack")
+
+
+def epic_link_kv8_workspace_bytes(cfg: epic_attn_cfg, sizes: epic_plan_sizes) -> int:
+    return int(_link_kv8_ws(C.byref(cfg), C.byref(sizes)))
+
+
+def epic_link_attention_kv8(cfg: epic_attn_cfg, dplan: DevicePlan, q_s, k_s, v_s, cache: Kv8Cache, out, lse, workspace,
+                            stream=None):
+    """Enqueue one attention layer of the link step, of decode or of the compile step over an 8-bit cache."""
+    bf16, f32 = _dtypes()[:2]
+    dev, n = _current_device(), dplan.sizes.n_s
+    hq, hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
+    at = [None] * 5
+    if n:
+        at = [_expect("q_s", q_s, (n, hq, d), bf16, dev), _expect("k_s", k_s, (n, hkv, d), bf16, dev),
+              _expect("v_s", v_s, (n, hkv, d), bf16, dev), _expect("out", out, (n, hq, d), bf16, dev),
+              None if lse is None else _expect("lse", lse, (n, hq), f32, dev)]
+    if dplan.dev.get_device() != dev:
+        raise ValueError(f"plan: expected on device {dev}, got {dplan.dev.device}")
+    ws, ws_bytes = _scratch(workspace, dev)
+    _check(_link_attention_kv8(C.byref(cfg), C.byref(dplan.sizes), C.byref(dplan.plan), *at[:3], cache.of(hkv, d, dev),
+                               *at[3:], ws, ws_bytes, _raw_stream(stream, dev)), "epic_link_attention_kv8")
 
 
 # ---------------------------------------------------------------- cache layout helpers
