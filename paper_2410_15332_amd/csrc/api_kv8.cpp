@@ -125,7 +125,7 @@ extern "C" epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const e
   AttnArgs a = attention_args(cfg, sizes, plan_dev, q_s, nullptr, nullptr, out, lse, workspace);
   if (sizes->tile_rows == kTileRowsTiny) {
     record_profile_event(1, stream);
-    launch_kv8_decode(a, *cache, d, sizes->n_work, stream);
+    launch_kv8_decode(a, *cache, d, sizes->n_work, sizes->n_tiles == 1, stream);
   } else {
     // The matrix cores bound wide tiles, and every tile would widen the same keys again: the
     // linked blocks are widened once, for the bf16 kernel.

@@ -36,7 +36,8 @@ void launch_kv8_expand(const int32_t* linked_blocks, int n, int hkv, int head_di
 // As launch_link_write and launch_link_write_rotated (rope_theta is read where blocks move).
 void launch_kv8_write(const epic_plan* plan, int n_private, bool rotated, int hkv, int head_dim, float rope_theta,
                       const uint16_t* k_s, const uint16_t* v_s, const epic_kv8_cache& c, hipStream_t stream);
-// As launch_link_decode; a.k_cache and a.v_cache are not read.
-void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, int head_dim, int n_work, hipStream_t stream);
+// As launch_link_decode; a.k_cache and a.v_cache are not read.  once: no two work items read the same block.
+void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, int head_dim, int n_work, bool once,
+                       hipStream_t stream);
 
 }  // namespace epic

@@ -55,9 +55,9 @@ __global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const ui
   uint2 y[4 * J];                              // tokens 4 a .. of dims 16 i + r
 #pragma unroll
   for (int i = 0; i < 2 * J; ++i)
-    x[i] = *reinterpret_cast<const uint4*>(k + from + r * D + 64 * (i >> 1) + 16 * a + 8 * (i & 1));
+    x[i] = load16(k + from + r * D + 64 * (i >> 1) + 16 * a + 8 * (i & 1));
 #pragma unroll
-  for (int i = 0; i < 4 * J; ++i) y[i] = *reinterpret_cast<const uint2*>(v + from + (16 * i + r) * 16 + 4 * a);
+  for (int i = 0; i < 4 * J; ++i) y[i] = load8(v + from + (16 * i + r) * 16 + 4 * a);
   int kb = kv8_byte(row_top<J>(x));
   uint32_t m0 = 0, m1 = 0;
 #pragma unroll
@@ -86,10 +86,10 @@ __global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const ui
   for (int j = 0; j < J; ++j) {
     uint4 q = round16(x[2 * j], x[2 * j + 1], kb);
     if (kb == kKv8Nan) q = make_uint4(kNanBytes, kNanBytes, kNanBytes, kNanBytes);
-    *reinterpret_cast<uint4*>(c.k + to + 1024 * j + 16 * lane) = q;
-    *reinterpret_cast<uint4*>(c.v + to + 1024 * j + 16 * lane) =
-        make_uint4(round4_each(y[4 * j].x, y[4 * j].y, vb), round4_each(y[4 * j + 1].x, y[4 * j + 1].y, vb),
-                   round4_each(y[4 * j + 2].x, y[4 * j + 2].y, vb), round4_each(y[4 * j + 3].x, y[4 * j + 3].y, vb));
+    store16(c.k + to + 1024 * j + 16 * lane, q);
+    store16(c.v + to + 1024 * j + 16 * lane,
+            make_uint4(round4_each(y[4 * j].x, y[4 * j].y, vb), round4_each(y[4 * j + 1].x, y[4 * j + 1].y, vb),
+                   round4_each(y[4 * j + 2].x, y[4 * j + 2].y, vb), round4_each(y[4 * j + 3].x, y[4 * j + 3].y, vb)));
   }
   uint8_t* s = c.scale + (size_t(dst) * mv.hkv + at.g) * kKv8Scales;
   if (lane < 16) s[lane] = uint8_t(kb);

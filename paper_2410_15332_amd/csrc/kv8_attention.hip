@@ -39,8 +39,9 @@ struct Kv8Block {
   uint32_t ks, vs;                            // scales of keys 4 a ..
 };
 
-template <int D, int RING>
-__global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs a, epic_kv8_cache c) {
+// NT: K and V are read past the caches, which hold nothing of them that is read again.
+template <int D, int RING, bool NT>
+__global__ __launch_bounds__(64 * kDecWaves, 3) void kv8_decode_kernel(AttnArgs a, epic_kv8_cache c) {
   constexpr int J = D / 64;
   constexpr int NDT = D / 16;                 // 16-dim tiles of O^T
   __shared__ Kv8DecodeLds<D> lds;
@@ -72,6 +73,25 @@ __global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // The wavefront's blocks, in pairs: block i of its own (i = 2 p + e) is b0 + 2 (wave + 4 p) + e.
+  // Their ids, positions and lengths come 64 at a time, one per lane, so that no load of a block
+  // waits for a chain of loads; past the item's end stands its last block, with no keys.
+  const int n_pairs = (b1 - b0 + 1) / 2;
+  const int mine = n_pairs > wave ? 2 * ((n_pairs - wave + kDecWaves - 1) / kDecWaves) : 0;
+  int phys_l, pos_l, len_l;
+  auto fetch = [&](int first) __attribute__((always_inline)) {
+    const int i = first + lane;
+    const int b = b0 + 2 * (wave + kDecWaves * (i >> 1)) + (i & 1);
+    const bool in = i < mine && b < b1;
+    const int bc = in ? b : b1 - 1;
+    const int lb = kind == kItemList ? listed(bc) : bc;
+    phys_l = a.linked_blocks[lb];
+    pos_l = a.block_pos0[lb];
+    len_l = in ? a.block_len[lb] : 0;
+  };
+  fetch(0);
+
   const int r = lane & 15;                    // tile row of this lane
   const int qd = lane >> 4;                   // its quarter: keys 4 qd ..
   const int R = a.rows_per_tile;
@@ -80,8 +100,12 @@ __global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs 
   const bool row_ok = srl < nrows;
   int srow, part_, lr_;
   slot(row_ok ? srl : nrows - 1, srow, part_, lr_);
-  // shared blocks precede every row of the item; a row that is none sees nothing
-  const int qpos = !row_ok ? -1 : kind == kItemShared ? 0x7fffffff : a.s_pos[srow];
+  // shared blocks precede every row of the item; lanes without a row see what the last row sees, for nothing
+  const int qpos = kind == kItemShared ? 0x7fffff00 : a.s_pos[srow];
+  int first_row = qpos;                       // the first position of the tile's rows
+#pragma unroll
+  for (int off = 1; off < 16; off *= 2) first_row = min(first_row, __shfl_xor(first_row, off));
+  first_row = __builtin_amdgcn_readfirstlane(first_row);
 
   bf16x8 qf[2 * J];                           // Q^T operand: row r, dims 64 j + 16 qd + 8 e ..
   {
@@ -98,16 +122,18 @@ __global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs 
   const uint8_t* kbase = c.k + size_t(g) * 16 * D + 16 * lane;
   const uint8_t* vbase = c.v + size_t(g) * 16 * D + 16 * lane;
   const uint8_t* sbase = c.scale + size_t(g) * kKv8Scales + 4 * qd;
-  auto load = [&](int phys, Kv8Block<J>& x) __attribute__((always_inline)) {
-    const size_t at = size_t(phys) * blk_bytes;
-    const uint8_t* sp = sbase + size_t(phys) * blk_scales;
-    x.ks = *reinterpret_cast<const uint32_t*>(sp);
-    x.vs = *reinterpret_cast<const uint32_t*>(sp + 16);
+  auto piece = [&](const uint8_t* p) __attribute__((always_inline)) {
+    return NT ? load16(p) : *reinterpret_cast<const uint4*>(p);
+  };
+  auto load_k = [&](int phys, Kv8Block<J>& x) __attribute__((always_inline)) {
+    x.ks = *reinterpret_cast<const uint32_t*>(sbase + size_t(phys) * blk_scales);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      x.k[j] = *reinterpret_cast<const uint4*>(kbase + at + 1024 * j);
-      x.v[j] = *reinterpret_cast<const uint4*>(vbase + at + 1024 * j);
-    }
+    for (int j = 0; j < J; ++j) x.k[j] = piece(kbase + size_t(phys) * blk_bytes + 1024 * j);
+  };
+  auto load_v = [&](int phys, Kv8Block<J>& x) __attribute__((always_inline)) {
+    x.vs = *reinterpret_cast<const uint32_t*>(sbase + size_t(phys) * blk_scales + 16);
+#pragma unroll
+    for (int j = 0; j < J; ++j) x.v[j] = piece(vbase + size_t(phys) * blk_bytes + 1024 * j);
   };
 
   f32x4 o[NDT];
@@ -115,9 +141,8 @@ __global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs 
   for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, lsum = 0.0f;           // lsum: of this lane's keys
 
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  // one block's scores, in the log2 domain: masked past the block's end, after the row
-  auto scores = [&](const Kv8Block<J>& x, int pos0, int len, float (&s)[4]) __attribute__((always_inline)) {
+  // one block's scores, in the log2 domain
+  auto scores = [&](const Kv8Block<J>& x, float (&s)[4]) __attribute__((always_inline)) {
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -130,49 +155,53 @@ __global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs 
       acc = mfma_16x16x32(__builtin_bit_cast(bf16x8, hi), qf[2 * j + 1], acc);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = qd * 4 + i;
-      const bool ok = key < len && pos0 + key <= qpos;
-      s[i] = ok ? __builtin_amdgcn_ldexpf(acc[i] * sl2, int(x.ks >> (8 * i) & 255u) - 127) : -INFINITY;
-    }
+    for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_ldexpf(acc[i] * sl2, int(x.ks >> (8 * i) & 255u) - 127);
+  };
+  // V's bytes of keys past a block's end may hold any bits, and a weight of 0 would not hide NaN
+  auto cut = [&](uint4 (&v)[J], int len) __attribute__((always_inline)) {
+    const int k = len - 4 * qd;
+    const uint32_t keep = k >= 4 ? 0xFFFFFFFFu : k <= 0 ? 0u : 0xFFFFFFFFu >> (32 - 8 * k);
+#pragma unroll
+    for (int j = 0; j < J; ++j) v[j] = make_uint4(v[j].x & keep, v[j].y & keep, v[j].z & keep, v[j].w & keep);
   };
 
-  // The wavefront's blocks, in pairs: block i of its own (i = 2 p + e) is b0 + 2 (wave + 4 p) + e.
-  // Their ids, positions and lengths come 64 at a time, one per lane, so that no load of a block
-  // waits for a chain of loads; past the item's end stands its last block, with no keys.
-  const int n_pairs = (b1 - b0 + 1) / 2;
-  const int mine = n_pairs > wave ? 2 * ((n_pairs - wave + kDecWaves - 1) / kDecWaves) : 0;
   for (int first = 0; first < mine; first += 64) {
-    int phys_l, pos_l, len_l;
-    {
-      const int i = first + lane;
-      const int b = b0 + 2 * (wave + kDecWaves * (i >> 1)) + (i & 1);
-      const bool in = i < mine && b < b1;
-      const int bc = in ? b : b1 - 1;
-      const int lb = kind == kItemList ? listed(bc) : bc;
-      phys_l = a.linked_blocks[lb];
-      pos_l = a.block_pos0[lb];
-      len_l = in ? a.block_len[lb] : 0;
-    }
+    if (first > 0) fetch(first);
     const int n = min(64, mine - first) / 2;  // pairs of this batch
     Kv8Block<J> ring[RING][2];
 #pragma unroll
     for (int j = 0; j < RING; ++j)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) load(__builtin_amdgcn_readlane(phys_l, 2 * min(j, n - 1) + e), ring[j][e]);
+      for (int e = 0; e < 2; ++e) {
+        const int phys = __builtin_amdgcn_readlane(phys_l, 2 * min(j, n - 1) + e);
+        load_k(phys, ring[j][e]);
+        load_v(phys, ring[j][e]);
+      }
     for (int base = 0; base < n; base += RING) {
 #pragma unroll
       for (int j = 0; j < RING; ++j) {
         const int p = base + j;
         if (p < n) {
-          float s[8];
+          // what this slot holds next; past the batch's end its last pair again, so that the same loads
+          // are in flight behind every wait
+          const int next = 2 * min(p + RING, n - 1);
+          const int phys0 = __builtin_amdgcn_readlane(phys_l, next), phys1 = __builtin_amdgcn_readlane(phys_l, next + 1);
+          const int pos0 = __builtin_amdgcn_readlane(pos_l, 2 * p), pos1 = __builtin_amdgcn_readlane(pos_l, 2 * p + 1);
           const int len0 = __builtin_amdgcn_readlane(len_l, 2 * p), len1 = __builtin_amdgcn_readlane(len_l, 2 * p + 1);
-          {
-            float t0[4], t1[4];
-            scores(ring[j][0], __builtin_amdgcn_readlane(pos_l, 2 * p), len0, t0);
-            scores(ring[j][1], __builtin_amdgcn_readlane(pos_l, 2 * p + 1), len1, t1);
+          float t0[4], t1[4];
+          scores(ring[j][0], t0);
+          scores(ring[j][1], t1);
+          float s[8] = {t0[0], t0[1], t0[2], t0[3], t1[0], t1[1], t1[2], t1[3]};
+          load_k(phys0, ring[j][0]);
+          load_k(phys1, ring[j][1]);
+          // masked: keys past the block's end, after the row (whole blocks before every row need nothing)
+          if (len0 + len1 < 32 || max(pos0, pos1) + 15 > first_row) {
+            const int k0 = min(len0, qpos - pos0 + 1) - 4 * qd, k1 = min(len1, qpos - pos1 + 1) - 4 * qd;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = t0[i], s[4 + i] = t1[i];
+            for (int i = 0; i < 4; ++i) {
+              s[i] = i < k0 ? s[i] : -INFINITY;
+              s[4 + i] = i < k1 ? s[4 + i] : -INFINITY;
+            }
           }
           float mb = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
           if (__ballot(mb > m + kLag)) {      // a row's maximum grew past the lag (at first: from nothing)
@@ -198,21 +227,12 @@ __global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs 
           const u32x4 pw = {pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
                             pack_bf16x2(pv[6], pv[7])};
           const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
-          // slots past a block's end may hold any bits, and a weight of 0 would not hide NaN
-          uint32_t keep0 = 0xFFFFFFFFu, keep1 = 0xFFFFFFFFu;
-          if (len0 < 16 || len1 < 16) {
-            auto mask = [&](int len) {
-              const int k = len - 4 * qd;
-              return k >= 4 ? 0xFFFFFFFFu : k <= 0 ? 0u : 0xFFFFFFFFu >> (32 - 8 * k);
-            };
-            keep0 = mask(len0);
-            keep1 = mask(len1);
-          }
+          if (len0 < 16) cut(ring[j][0].v, len0);
+          if (len1 < 16) cut(ring[j][1].v, len1);
 #pragma unroll
           for (int q = 0; q < J; ++q) {
             const uint4 v0 = ring[j][0].v[q], v1 = ring[j][1].v[q];
-            const uint32_t w0[4] = {v0.x & keep0, v0.y & keep0, v0.z & keep0, v0.w & keep0};
-            const uint32_t w1[4] = {v1.x & keep1, v1.y & keep1, v1.z & keep1, v1.w & keep1};
+            const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
               const u32x4 vv = {e4m3_pair<false>(w0[t], 1.0f), e4m3_pair<true>(w0[t], 1.0f), e4m3_pair<false>(w1[t], 1.0f),
@@ -220,15 +240,12 @@ __global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs 
               o[4 * q + t] = mfma_16x16x32(__builtin_bit_cast(bf16x8, vv), pb, o[4 * q + t]);
             }
           }
+          load_v(phys0, ring[j][0]);
+          load_v(phys1, ring[j][1]);
         }
-        // refill, past the batch's end with its last pair: every slot always has the same loads in flight
-        if (n > RING)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) load(__builtin_amdgcn_readlane(phys_l, 2 * min(p + RING, n - 1) + e), ring[j][e]);
       }
     }
   }
-
   __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): the ring's last loads land before the exit
 
   lsum += __shfl_xor(lsum, 16);
@@ -285,11 +302,13 @@ __global__ __launch_bounds__(64 * kDecWaves, 2) void kv8_decode_kernel(AttnArgs 
 
 }  // namespace
 
-void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, int head_dim, int n_work, hipStream_t stream) {
+void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, int head_dim, int n_work, bool once,
+                       hipStream_t stream) {
   if (n_work == 0) return;
   const dim3 grid{unsigned(n_work) * unsigned(a.hkv)};
-  if (head_dim == 128) kv8_decode_kernel<128, 2><<<grid, 64 * kDecWaves, 0, stream>>>(a, c);
-  else kv8_decode_kernel<64, 3><<<grid, 64 * kDecWaves, 0, stream>>>(a, c);
+  auto go = [&](auto kernel) { kernel<<<grid, 64 * kDecWaves, 0, stream>>>(a, c); };
+  if (head_dim == 128) once ? go(kv8_decode_kernel<128, 1, true>) : go(kv8_decode_kernel<128, 1, false>);
+  else once ? go(kv8_decode_kernel<64, 2, true>) : go(kv8_decode_kernel<64, 2, false>);
 }
 
 }  // namespace epic

@@ -20,6 +20,13 @@ __device__ __forceinline__ uint32_t e4m3_pair(uint32_t w, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(w), scale, HI));
 }
 
+// Loads and stores of bytes that nothing reads again soon.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load16(const void* p) { return __builtin_bit_cast(uint4, __builtin_nontemporal_load(static_cast<const u32x4*>(p))); }
+__device__ __forceinline__ uint2 load8(const void* p) { return __builtin_bit_cast(uint2, __builtin_nontemporal_load(static_cast<const u32x2*>(p))); }
+__device__ __forceinline__ void store16(void* p, const uint4& x) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), static_cast<u32x4*>(p)); }
+
 // |bits| of the pairs of a dword, and the larger of two such dwords, half by half.
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pair_abs(uint32_t w) { return w & 0x7FFF7FFFu; }

@@ -19,8 +19,7 @@ struct QkRopeArgs {
   float eps, amplitude;
 };
 
-// Rows of one workgroup, and threads of a launch: fewer than 2^32.
-constexpr int kQkRows = 4;
+// A workgroup of 256 threads a row: fewer than 2^32 threads.
 constexpr int64_t kQkMaxRows = (int64_t(1) << 24) - 4;
 
 void launch_qk_rope(const QkRopeArgs& p, int head_dim, bool fp32, bool interleaved, hipStream_t stream);

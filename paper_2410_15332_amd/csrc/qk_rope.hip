@@ -10,8 +10,8 @@
 //
 // What bounds it is reading and writing the rows once.  A head is D / 16 lanes of 16 values,
 // two pieces of 8 each: both pieces of a lane's pairs, so a rotation stays in the lane.  A workgroup
-// takes up to kQkRows rows, whose angles (one per thread) are computed once, into LDS, while the
-// first loads are in flight; few rows are dealt to a workgroup per 32 or 64 heads instead.
+// takes a row in passes of 256 threads, the next pass's loads ahead of this one's work; the row's
+// angles (one per thread) are computed once, into LDS, while the first loads are in flight.
 #include "device_common.h"
 #include "qk_rope.h"
 
@@ -74,28 +74,24 @@ struct Piece<true> {
 };
 
 template <int D, bool F32, bool INTER>
-__global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p, int rows_per_wg, int passes) {
+__global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p) {
   constexpr int L = D / 16;                   // lanes per head
-  constexpr int HPW = kThreads / L;           // heads of a pass
-  __shared__ float2 cs[kQkRows][kMaxPairs];
-  const int heads = p.hq + 2 * p.hkv, half = p.rot / 2;
-  const int row0 = blockIdx.x * rows_per_wg, nr = min(rows_per_wg, p.rows - row0);
+  __shared__ float2 cs[kMaxPairs];
+  const int heads = p.hq + 2 * p.hkv, row = blockIdx.x, step = kThreads / L * gridDim.y;
   const int l = threadIdx.x % L;
   // this lane's two pieces of 8 dims: the two sides of its pairs (half layout), or neighbours
   const int R = p.rot / 8;                    // rotated pieces, an even number
   const bool turned = l < R / 2;
   const int c0 = INTER || !turned ? 2 * l : l, c1 = INTER || !turned ? 2 * l + 1 : l + R / 2;
 
-  const int total = nr * heads;
-  int hr = blockIdx.y * passes * HPW + threadIdx.x / L;
+  int head = blockIdx.y * (kThreads / L) + threadIdx.x / L;
   Piece<F32> x[2];
   auto fetch = [&](int at) __attribute__((always_inline)) {
-    at = min(at, total - 1);
-    const size_t from = size_t(row0 + at / heads) * p.ld + size_t(at % heads) * D;
+    const size_t from = size_t(row) * p.ld + size_t(min(at, heads - 1)) * D;
     x[0].load(p.qkv, from + 8 * c0);
     x[1].load(p.qkv, from + 8 * c1);
   };
-  fetch(hr);
+  fetch(head);
   uint4 wq[2] = {}, wk[2] = {};
   if (p.q_norm) {
     wq[0] = *reinterpret_cast<const uint4*>(p.q_norm + 8 * c0);
@@ -105,16 +101,14 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p, int row
     wk[0] = *reinterpret_cast<const uint4*>(p.k_norm + 8 * c0);
     wk[1] = *reinterpret_cast<const uint4*>(p.k_norm + 8 * c1);
   }
-  for (int i = threadIdx.x; i < nr * half; i += kThreads) {
-    const int row = i / half, j = i - row * half;
-    const float2 t = turn_of(p.pos[row0 + row], p.freqs[j]);
-    cs[row][j] = make_float2(p.amplitude * t.x, p.amplitude * t.y);
+  if (int(threadIdx.x) < p.rot / 2) {
+    const float2 t = turn_of(p.pos[row], p.freqs[threadIdx.x]);
+    cs[threadIdx.x] = make_float2(p.amplitude * t.x, p.amplitude * t.y);
   }
   __syncthreads();
-  for (int pass = 0; pass < passes; ++pass, hr += HPW) {
+  for (;; head += step) {
     const Piece<F32> y0 = x[0], y1 = x[1];
-    if (pass + 1 < passes) fetch(hr + HPW);
-    const int row = hr / heads, head = hr - row * heads;
+    if (head + step < heads) fetch(head + step);
     const bool is_q = head < p.hq, is_v = head >= p.hq + p.hkv;
     float u[8], v[8];
     y0.get(u);
@@ -124,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p, int row
     for (int i = 0; i < 8; ++i) ss += u[i] * u[i] + v[i] * v[i];
 #pragma unroll
     for (int off = L / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
-    if (hr >= total) continue;
+    if (head >= heads) break;                 // after the exchange: all lanes of a head together
     uint4 r0 = y0.bf16(), r1 = y1.bf16();
     if (!is_v) {
       if ((is_q ? p.q_norm : p.k_norm) != nullptr) {
@@ -139,17 +133,16 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p, int row
         }
       }
       if (turned) {
-        const float2* t = cs[row];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if constexpr (INTER) {              // pairs 8 l + i: u holds four of them, then v
             float* e = i < 4 ? u + 2 * i : v + 2 * (i - 4);
-            const float2 k = t[8 * l + i];
+            const float2 k = cs[8 * l + i];
             const float a = e[0], b = e[1];
             e[0] = a * k.x - b * k.y;
             e[1] = b * k.x + a * k.y;
           } else {
-            const float2 k = t[8 * l + i];
+            const float2 k = cs[8 * l + i];
             const float a = u[i], b = v[i];
             u[i] = a * k.x - b * k.y;
             v[i] = b * k.x + a * k.y;
@@ -159,7 +152,7 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p, int row
       r0 = pack8(u);
       r1 = pack8(v);
     }
-    const size_t at = size_t(row0 + row);
+    const size_t at = row;
     uint16_t* to = is_q ? p.q + (at * p.hq + head) * D
                         : is_v ? p.v + (at * p.hkv + (head - p.hq - p.hkv)) * D : p.k + (at * p.hkv + (head - p.hq)) * D;
     *reinterpret_cast<uint4*>(to + 8 * c0) = r0;
@@ -170,12 +163,12 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p, int row
 }  // namespace
 
 void launch_qk_rope(const QkRopeArgs& p, int head_dim, bool fp32, bool interleaved, hipStream_t stream) {
-  const int heads = p.hq + 2 * p.hkv, hpw = kThreads / (head_dim / 16);
-  // few rows: a workgroup per row and pass, so that they spread over the chip
-  const bool few = p.rows < 512;
-  const int per = few ? 1 : kQkRows, passes = (per * heads + hpw - 1) / hpw;
-  const dim3 grid((p.rows + per - 1) / per, few ? passes : 1);
-  auto go = [&](auto kernel) { kernel<<<grid, kThreads, 0, stream>>>(p, per, few ? 1 : passes); };
+  // Passes of 32 heads (64 of 64 dims) over a row; each a workgroup of its own where rows are fewer
+  // than CUs.  32 + 8 + 8 heads of 128: 1 row 2.8 us (3.5 undivided), 736 rows of fp32 7.5 (8.4 divided), 20 560 rows
+  // 85 (505 MB, 5.9 TB/s; 96 to 99 divided, with 4 rows a workgroup, or in one pass of 384 threads).
+  const int per_pass = kThreads / (head_dim / 16);
+  const int passes = p.rows < 256 ? (p.hq + 2 * p.hkv + per_pass - 1) / per_pass : 1;
+  auto go = [&](auto kernel) { kernel<<<dim3(p.rows, passes), kThreads, 0, stream>>>(p); };
   if (head_dim == 128) {
     if (fp32) interleaved ? go(qk_rope_kernel<128, true, true>) : go(qk_rope_kernel<128, true, false>);
     else interleaved ? go(qk_rope_kernel<128, false, true>) : go(qk_rope_kernel<128, false, false>);

@@ -452,37 +452,35 @@ _fp8_types = None
 
 
 def _dtypes():
-    """(bf16, fp32, what e4m3 values come in, what e8m0 scales come in); torch is imported late."""
+    """(bf16, fp32, what e4m3 values come in, what e8m0 scales come in, int32, float64); torch is imported late."""
     global _fp8_types
     if _fp8_types is None:
         import torch
 
         _fp8_types = ((torch.bfloat16,), (torch.float32,), (torch.uint8, torch.float8_e4m3fn),
-                      (torch.uint8, torch.float8_e8m0fnu))
+                      (torch.uint8, torch.float8_e8m0fnu), (torch.int32,), (torch.float64,))
     return _fp8_types
 
 
 def _device_of(name: str, t) -> int:
     """The device of a call's first tensor, which has to be the current one."""
-    import torch
-
     device = t.get_device()
-    if device < 0 or device != torch.cuda.current_device():
+    if device < 0 or device != _current_device():
         raise ValueError(f"{name}: a tensor of the current GPU expected, got one of {t.device}")
     return device
 
 
 def _expect(name: str, t, shape, dtypes, device: int) -> int:
     """The address of an argument of the 8-bit operators, which take packed tensors of one device."""
+    if t is not None and t.shape == shape and t.dtype in dtypes and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
     if t is None:
         raise ValueError(f"{name} is missing")
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous {tuple(shape)} expected, got {tuple(t.shape)} with strides {t.stride()}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: {' or '.join(map(str, dtypes))} expected, got {t.dtype}")
-    if t.get_device() != device:
-        raise ValueError(f"{name}: expected on device {device}, got {t.device}")
-    return t.data_ptr()
+    raise ValueError(f"{name}: expected on device {device}, got {t.device}")
 
 
 def _scratch(t, device: int):
@@ -495,13 +493,27 @@ def _scratch(t, device: int):
     return t.data_ptr(), t.nbytes
 
 
+_torch_c = None
+
+
+def _c():
+    """torch's C module, imported late: calls of a few us ask it for the device and the stream without objects around them."""
+    global _torch_c
+    if _torch_c is None:
+        import torch
+
+        torch.cuda.current_device()                   # initialises the GPU
+        _torch_c = torch._C
+    return _torch_c
+
+
+def _current_device() -> int:
+    return _c()._cuda_getDevice()
+
+
 def _raw_stream(stream, device: int) -> int:
     """_stream() for calls of a few us: the current stream's handle without an object around it."""
-    if stream is not None:
-        return stream.cuda_stream
-    import torch
-
-    return torch._C._cuda_getCurrentRawStream(device)
+    return stream.cuda_stream if stream is not None else _c()._cuda_getCurrentRawStream(device)
 
 
 def epic_fp8_scale_bytes(m: int, k: int) -> int:
@@ -512,7 +524,7 @@ def epic_quant_fp8(x, q, scale, block_rows: int = 1, stream=None):
     """Enqueue x bf16 [m, k] -> e4m3 values q [m, k] and e8m0 scales (see include/epic_link.h):
     rows (block_rows 1, scale fp8_row_scale_shape(m, k)) or weights (128,
     fp8_block_scale_shape(m, k)).  q and scale: uint8 or torch's 8-bit float types."""
-    bf16, _, e4m3, e8m0 = _dtypes()
+    bf16, _, e4m3, e8m0 = _dtypes()[:4]
     dev = _device_of("x", x)
     m, k = x.shape
     shape = fp8_row_scale_shape(m, k) if block_rows == 1 else fp8_block_scale_shape(m, k)
@@ -523,7 +535,7 @@ def epic_quant_fp8(x, q, scale, block_rows: int = 1, stream=None):
 def epic_rmsnorm_fp8(x, weight, eps: float, q, scale, delta=None, x_out=None, stream=None):
     """Enqueue s = x + delta, x_out = s (x itself or None are fine) and RMSNorm(s) weight -> q, scale
     as rows (see include/epic_link.h); x, x_out fp32, delta bf16 or None."""
-    bf16, f32, e4m3, e8m0 = _dtypes()
+    bf16, f32, e4m3, e8m0 = _dtypes()[:4]
     dev = _device_of("x", x)
     m, hidden = rows = x.shape
     _check(_rmsnorm_fp8(_expect("x", x, rows, f32, dev), None if delta is None else _expect("delta", delta, rows, bf16, dev),
@@ -542,7 +554,7 @@ def epic_gemm_fp8(epilogue: int, a, a_scale, w, w_scale, out, out_scale=None, wo
     """Enqueue the 8-bit projection GEMM (see include/epic_link.h): a [m, k] with row scales, w
     [n, k] with block scales; out bf16 [m, n] (FP8_BF16) or [m, n/2] (FP8_SWIGLU), or e4m3
     [m, n/2] with out_scale (FP8_SWIGLU_FP8)."""
-    bf16, _, e4m3, e8m0 = _dtypes()
+    bf16, _, e4m3, e8m0 = _dtypes()[:4]
     dev = _device_of("a", a)
     (m, k), n = a.shape, w.shape[0]
     quant = epilogue == FP8_SWIGLU_FP8
@@ -558,12 +570,6 @@ def epic_gemm_fp8(epilogue: int, a, a_scale, w, w_scale, out, out_scale=None, wo
 
 def epic_model_fp8_workspace_bytes(cfg: epic_model_cfg, sizes: epic_plan_sizes) -> int:
     return int(_model_fp8_ws(C.byref(cfg), C.byref(sizes)))
-
-
-def _current_device() -> int:
-    import torch
-
-    return torch.cuda.current_device()
 
 
 def _packed(name: str, t, device: int) -> Optional[int]:
@@ -620,25 +626,29 @@ def epic_qk_norm_rope(cfg: epic_attn_cfg, rope: epic_rope_cfg, qkv, pos, freqs, 
     """Enqueue the norm and rotation of Q|K|V rows (see include/epic_link.h): qkv [n, (Hq + 2 Hkv) D] in
     bf16 or fp32, whose rows may be apart; pos int32 [n]; freqs float64 [rot_dim / 2]; q [n, Hq, D], k, v
     [n, Hkv, D] bf16; q_norm, k_norm bf16 [D] or None."""
-    import torch
-
-    bf16, f32 = _dtypes()[:2]
+    bf16, f32, _, _, i32, f64 = _dtypes()
     dev = _device_of("qkv", qkv)
-    hq, hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
-    if qkv.dim() != 2 or qkv.shape[1] != (hq + 2 * hkv) * d or qkv.stride(1) != 1:
-        raise ValueError(f"qkv: rows of {(hq + 2 * hkv) * d} values expected, got {tuple(qkv.shape)} with strides {qkv.stride()}")
-    if qkv.dtype not in bf16 + f32:
-        raise ValueError(f"qkv: {bf16[0]} or {f32[0]} expected, got {qkv.dtype}")
-    n = qkv.shape[0]
-    ld = qkv.stride(0) if n > 1 else qkv.shape[1]     # a single row's stride says nothing
-    if rope.rot_dim:
-        _expect("freqs", freqs, (rope.rot_dim // 2,), (torch.float64,), dev)
-    _check(_qk_norm_rope(C.byref(cfg), C.byref(rope), QKV_FP32 if qkv.dtype in f32 else QKV_BF16, qkv.data_ptr(), ld, n,
-                         _expect("pos", pos, (n,), (torch.int32,), dev), _ptr(freqs) if rope.rot_dim else None,
+    hq, hkv, d, rot = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim, rope.rot_dim
+    shape, (ld, step), dtype = qkv.shape, _strides2(qkv), qkv.dtype
+    if len(shape) != 2 or shape[1] != (hq + 2 * hkv) * d or step != 1:
+        raise ValueError(f"qkv: rows of {(hq + 2 * hkv) * d} values expected, got {tuple(shape)} with strides {qkv.stride()}")
+    if dtype not in bf16 and dtype not in f32:
+        raise ValueError(f"qkv: {bf16[0]} or {f32[0]} expected, got {dtype}")
+    n = shape[0]
+    if n < 2:
+        ld = shape[1]                                 # a single row's stride says nothing
+    _check(_qk_norm_rope(C.byref(cfg), C.byref(rope), QKV_FP32 if dtype in f32 else QKV_BF16, qkv.data_ptr(), ld, n,
+                         _expect("pos", pos, (n,), i32, dev),
+                         _expect("freqs", freqs, (rot // 2,), f64, dev) if rot else None,
                          None if q_norm is None else _expect("q_norm", q_norm, (d,), bf16, dev),
                          None if k_norm is None else _expect("k_norm", k_norm, (d,), bf16, dev), eps,
                          _expect("q", q, (n, hq, d), bf16, dev), _expect("k", k, (n, hkv, d), bf16, dev),
                          _expect("v", v, (n, hkv, d), bf16, dev), _raw_stream(stream, dev)), "epic_qk_norm_rope")
+
+
+def _strides2(t):
+    s = t.stride()
+    return s if len(s) == 2 else (0, 0)
 
 
 # ---------------------------------------------------------------- cache in 8 bits
@@ -655,7 +665,7 @@ class Kv8Cache:
     def __init__(self, k, v, scale):
         if k.dim() != 6 or k.shape[2] not in (1, 2):
             raise ValueError(f"k: [blocks, Hkv, D / 64, 4, 16, 16] expected, got {tuple(k.shape)}")
-        _, _, e4m3, e8m0 = _dtypes()
+        _, _, e4m3, e8m0 = _dtypes()[:4]
         self.num_blocks, self.hkv, self.d = k.shape[0], k.shape[1], 64 * k.shape[2]
         self.device = k.get_device()
         shapes = kv8_shapes(self.num_blocks, self.hkv, self.d)
@@ -663,6 +673,7 @@ class Kv8Cache:
               zip(("k", "v", "scale"), (k, v, scale), shapes, (e4m3, e4m3, e8m0))]
         self.k, self.v, self.scale = k, v, scale
         self.c = epic_kv8_cache(*at, self.num_blocks)
+        self.cfg = attn_cfg(self.hkv, self.hkv, self.d)   # what the moves need of an attention config
 
     @classmethod
     def zeros(cls, num_blocks: int, hkv: int, d: int, device="cuda"):
@@ -672,43 +683,45 @@ class Kv8Cache:
 
     def of(self, hkv: int, d: int, device: int):
         """Its C form, for a call with these heads on this device."""
-        if (self.hkv, self.d) != (hkv, d):
+        if self.hkv != hkv or self.d != d:
             raise ValueError(f"8-bit cache: {hkv} KV heads of {d} expected, got {self.hkv} of {self.d}")
         if self.device != device:
             raise ValueError(f"8-bit cache: expected on device {device}, got one of {self.device}")
         return C.byref(self.c)
 
 
-def _kv8_move(k_cache, v_cache, cache: Kv8Cache, src_blocks, dst_blocks, pools):
-    """What the moves between a bf16 and an 8-bit cache share: device, config, number of blocks and addresses."""
-    import torch
-
-    bf16 = _dtypes()[0]
+def _kv8_move(k_cache, v_cache, cache: Kv8Cache, src_blocks, dst_blocks):
+    """What the moves between a bf16 and an 8-bit cache share: device, number of blocks, addresses, and the bf16 pool's blocks."""
+    bf16, _, _, _, i32, _ = _dtypes()
     dev = _device_of("k_cache", k_cache)
-    blocks, (hkv, d) = k_cache.shape[0], (cache.hkv, cache.d)
-    lists = [t for t in (src_blocks, dst_blocks) if t is not None]
-    n = len(lists[0]) if lists else min(pools)
-    if not lists and pools[0] != pools[1]:
-        raise ValueError(f"lists of blocks are needed between pools of {pools[0]} and {pools[1]} blocks")
-    at = [None if t is None else _expect(name, t, (n,), (torch.int32,), dev) for name, t in
-          (("src_blocks", src_blocks), ("dst_blocks", dst_blocks))]
-    return (dev, attn_cfg(hkv, hkv, d), n, at[0], at[1], _expect("k_cache", k_cache, (blocks, hkv, 16, d), bf16, dev),
-            _expect("v_cache", v_cache, (blocks, hkv, d, 16), bf16, dev), cache.of(hkv, d, dev))
+    pool, hkv, d = k_cache.shape[0], cache.hkv, cache.d
+    if src_blocks is not None:
+        n = len(src_blocks)
+    elif dst_blocks is not None:
+        n = len(dst_blocks)
+    elif pool == cache.num_blocks:
+        n = pool
+    else:
+        raise ValueError(f"lists of blocks are needed between pools of {pool} and {cache.num_blocks} blocks")
+    return (dev, n, None if src_blocks is None else _expect("src_blocks", src_blocks, (n,), i32, dev),
+            None if dst_blocks is None else _expect("dst_blocks", dst_blocks, (n,), i32, dev),
+            _expect("k_cache", k_cache, (pool, hkv, 16, d), bf16, dev),
+            _expect("v_cache", v_cache, (pool, hkv, d, 16), bf16, dev), pool)
 
 
 def epic_kv8_pack(k_cache, v_cache, cache: Kv8Cache, src_blocks=None, dst_blocks=None, stream=None):
     """Enqueue blocks src_blocks of a bf16 cache -> blocks dst_blocks of an 8-bit one (int32 lists in device
     memory; None: 0 .. n - 1)."""
-    dev, cfg, n, src, dst, k, v, c = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks,
-                                               (k_cache.shape[0], cache.num_blocks))
-    _check(_kv8_pack(C.byref(cfg), n, src, k, v, k_cache.shape[0], dst, c, _raw_stream(stream, dev)), "epic_kv8_pack")
+    dev, n, src, dst, k, v, pool = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks)
+    _check(_kv8_pack(C.byref(cache.cfg), n, src, k, v, pool, dst, cache.of(cache.hkv, cache.d, dev),
+                     _raw_stream(stream, dev)), "epic_kv8_pack")
 
 
 def epic_kv8_unpack(cache: Kv8Cache, k_cache, v_cache, src_blocks=None, dst_blocks=None, stream=None):
     """Enqueue blocks src_blocks of an 8-bit cache -> blocks dst_blocks of a bf16 one."""
-    dev, cfg, n, src, dst, k, v, c = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks,
-                                               (cache.num_blocks, k_cache.shape[0]))
-    _check(_kv8_unpack(C.byref(cfg), n, src, c, dst, k, v, k_cache.shape[0], _raw_stream(stream, dev)), "epic_kv8_unpack")
+    dev, n, src, dst, k, v, pool = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks)
+    _check(_kv8_unpack(C.byref(cache.cfg), n, src, cache.of(cache.hkv, cache.d, dev), dst, k, v, pool,
+                       _raw_stream(stream, dev)), "epic_kv8_unpack")
 
 
 def epic_link_kv8_workspace_bytes(cfg: epic_attn_cfg, sizes: epic_plan_sizes) -> int:
@@ -721,11 +734,11 @@ def epic_link_attention_kv8(cfg: epic_attn_cfg, dplan: DevicePlan, q_s, k_s, v_s
     bf16, f32 = _dtypes()[:2]
     dev, n = _current_device(), dplan.sizes.n_s
     hq, hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
-    at = [None] * 5
+    at = (None,) * 5
     if n:
-        at = [_expect("q_s", q_s, (n, hq, d), bf16, dev), _expect("k_s", k_s, (n, hkv, d), bf16, dev),
+        at = (_expect("q_s", q_s, (n, hq, d), bf16, dev), _expect("k_s", k_s, (n, hkv, d), bf16, dev),
               _expect("v_s", v_s, (n, hkv, d), bf16, dev), _expect("out", out, (n, hq, d), bf16, dev),
-              None if lse is None else _expect("lse", lse, (n, hq), f32, dev)]
+              None if lse is None else _expect("lse", lse, (n, hq), f32, dev))
     if dplan.dev.get_device() != dev:
         raise ValueError(f"plan: expected on device {dev}, got {dplan.dev.device}")
     ws, ws_bytes = _scratch(workspace, dev)
