@@ -120,12 +120,17 @@ extern "C" epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const e
     EPIC_CHECK_ARG(aligned16(workspace), "workspace must be 16-byte aligned");
   }
   record_profile_event(0, stream);
-  launch_kv8_write(plan_dev, sizes->n_private, sizes->n_rerotated > 0, hkv, d, cfg->rope_theta, k_s, v_s, *cache, stream);
+  const bool tiny = sizes->tile_rows == kTileRowsTiny && sizes->n_s > 0;
+  // Decode: few private blocks, none turned: the attention launch writes them itself
+  const bool joined = tiny && sizes->n_rerotated == 0 && sizes->n_private <= kKv8MaxRows;
+  if (!joined)
+    launch_kv8_write(plan_dev, sizes->n_private, sizes->n_rerotated > 0, hkv, d, cfg->rope_theta, k_s, v_s, *cache, stream);
   if (sizes->n_s == 0) return hip_status("8-bit link write launch");      // re-rotated copies only
   AttnArgs a = attention_args(cfg, sizes, plan_dev, q_s, nullptr, nullptr, out, lse, workspace);
-  if (sizes->tile_rows == kTileRowsTiny) {
+  if (tiny) {
+    const Kv8Rows rows{plan_dev->priv_block, plan_dev->priv_src, plan_dev->priv_rows, k_s, v_s, joined ? sizes->n_private : 0, 0};
     record_profile_event(1, stream);
-    launch_kv8_decode(a, *cache, d, sizes->n_work, sizes->n_tiles == 1, stream);
+    launch_kv8_decode(a, *cache, rows, d, sizes->n_work, sizes->n_tiles == 1, stream);
   } else {
     // The matrix cores bound wide tiles, and every tile would widen the same keys again: the
     // linked blocks are widened once, for the bf16 kernel.

@@ -36,8 +36,17 @@ void launch_kv8_expand(const int32_t* linked_blocks, int n, int hkv, int head_di
 // As launch_link_write and launch_link_write_rotated (rope_theta is read where blocks move).
 void launch_kv8_write(const epic_plan* plan, int n_private, bool rotated, int hkv, int head_dim, float rope_theta,
                       const uint16_t* k_s, const uint16_t* v_s, const epic_kv8_cache& c, hipStream_t stream);
+// The private blocks that an attention launch writes itself.
+struct Kv8Rows {
+  const int32_t *block, *src, *rows;          // priv_block, priv_src, priv_rows
+  const uint16_t *k_s, *v_s;
+  int n;                                      // at most kKv8MaxRows; 0: they are written
+  int groups;                                 // workgroups that write them (set by the launcher)
+};
+constexpr int kKv8MaxRows = 64;               // a lane each
+
 // As launch_link_decode; a.k_cache and a.v_cache are not read.  once: no two work items read the same block.
-void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, int head_dim, int n_work, bool once,
+void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, const Kv8Rows& rows, int head_dim, int n_work, bool once,
                        hipStream_t stream);
 
 }  // namespace epic

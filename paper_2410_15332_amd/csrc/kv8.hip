@@ -151,10 +151,7 @@ __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_k
 // The link write: every private block takes what its source block holds (ROTATE: K turned by
 // priv_rot, from its 8-bit values to 8 bits again), then the rows of S, rounded to 8 bits, in
 // their slots.  A slot that neither fills holds a row of zeros.  A block that is its own
-// source is read whole before it is written, by one wavefront.
-//
-// V rows come like K's, 16 dims of a token a lane; their e4m3 bytes change places through
-// LDS, a row of 64 + 4 bytes per token and 64 dims.
+// source only receives its rows.
 template <int D, bool ROTATE>
 __global__ __launch_bounds__(kThreads) void kv8_write_kernel(const int32_t* __restrict__ priv_block,
                                                              const int32_t* __restrict__ priv_src,
@@ -163,43 +160,18 @@ __global__ __launch_bounds__(kThreads) void kv8_write_kernel(const int32_t* __re
                                                              const uint16_t* __restrict__ k_s,
                                                              const uint16_t* __restrict__ v_s, epic_kv8_cache c, int hkv,
                                                              double log2_theta) {
-  constexpr int J = D / 64, LD = 68;
-  __shared__ uint32_t turn[kWaves][J][16 * LD / 4];
+  constexpr int J = D / 64;
+  __shared__ uint32_t turn[kWaves][kTurnInts<J>];
   __shared__ float2 cs[ROTATE ? D / 2 : 1];
   const Place at(hkv);
-  const int g = min(at.g, hkv - 1);            // all wavefronts meet at the barriers
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, a = lane >> 4;
+  const int g = min(at.g, hkv - 1);            // all wavefronts meet at the barrier
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, a = lane >> 4;
   const int dst = priv_block[at.i], src = priv_src[at.i];
   const int rot = ROTATE && src >= 0 ? priv_rot[at.i] : 0;
-  const int row = priv_rows[at.i * 16 + r];
-  const int32_t* rows4 = priv_rows + at.i * 16 + 4 * a;
-  const bool fresh = row >= 0;
-
-  uint4 x[2 * J], y[2 * J], kq[J], vq[J];
-  int kb = 127;                                // a row of zeros
-  uint32_t vw = 0x7F7F7F7Fu;
-#pragma unroll
-  for (int i = 0; i < 2 * J; ++i) {
-    x[i] = y[i] = make_uint4(0, 0, 0, 0);
-    if (fresh) {
-      const size_t from = (size_t(row) * hkv + g) * D + 64 * (i >> 1) + 16 * a + 8 * (i & 1);
-      x[i] = *reinterpret_cast<const uint4*>(k_s + from);
-      y[i] = *reinterpret_cast<const uint4*>(v_s + from);
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < J; ++j) kq[j] = vq[j] = make_uint4(0, 0, 0, 0);
-  if (src >= 0) {
-    const size_t from = (size_t(src) * hkv + g) * 16 * D;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      kq[j] = *reinterpret_cast<const uint4*>(c.k + from + 1024 * j + 16 * lane);
-      vq[j] = *reinterpret_cast<const uint4*>(c.v + from + 1024 * j + 16 * lane);
-    }
-    const uint8_t* s = c.scale + (size_t(src) * hkv + g) * kKv8Scales;
-    kb = s[r];
-    vw = *reinterpret_cast<const uint32_t*>(s + 16 + 4 * a);
-  }
+  uint4 kq[J], vq[J];
+  int kb;
+  uint32_t vs;
+  kv8_load_block<D>(c, src == dst ? -1 : src, hkv, g, lane, kq, vq, kb, vs);
   if constexpr (ROTATE) {
     if (rot != 0) {                            // one block per workgroup: all of its wavefronts or none
       if (threadIdx.x < D / 2) {
@@ -252,52 +224,11 @@ __global__ __launch_bounds__(kThreads) void kv8_write_kernel(const int32_t* __re
       }
     }
   }
-  // the rows of S
-  int nk = kv8_byte(row_top<J>(x)), nv = kv8_byte(row_top<J>(y));
-  if (nk == kKv8Nan || nv == kKv8Nan) nk = nv = kKv8Nan;
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    uint4 q = round16(x[2 * j], x[2 * j + 1], nk), p = round16(y[2 * j], y[2 * j + 1], nv);
-    if (nk == kKv8Nan) {
-      q = make_uint4(kNanBytes, kNanBytes, kNanBytes, kNanBytes);
-      p = make_uint4(0, 0, 0, 0);
-    }
-    if (fresh) kq[j] = q;
-    uint32_t* to = &turn[wave][j][(r * LD + 16 * a) / 4];
-    to[0] = p.x, to[1] = p.y, to[2] = p.z, to[3] = p.w;
-  }
-  if (fresh) kb = nk;
-  __syncthreads();
-  // this lane's tokens 4 a ..: their bytes and their scale
-  const uint32_t mask = (rows4[0] >= 0 ? 0xFFu : 0u) | (rows4[1] >= 0 ? 0xFF00u : 0u) |
-                        (rows4[2] >= 0 ? 0xFF0000u : 0u) | (rows4[3] >= 0 ? 0xFF000000u : 0u);
-  uint32_t nvw = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) nvw |= uint32_t(__shfl(nv, 4 * a + i)) << (8 * i);
-  vw = (vw & ~mask) | (nvw & mask);
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const uint8_t* from = reinterpret_cast<const uint8_t*>(turn[wave][j]);
-    uint32_t w[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      w[t] = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[t] |= uint32_t(from[(4 * a + i) * LD + 16 * t + r]) << (8 * i);
-    }
-    vq[j] = make_uint4((vq[j].x & ~mask) | (w[0] & mask), (vq[j].y & ~mask) | (w[1] & mask),
-                       (vq[j].z & ~mask) | (w[2] & mask), (vq[j].w & ~mask) | (w[3] & mask));
-  }
+  const Kv8Fresh<J> f = kv8_fresh<D>(priv_rows + at.i * 16, k_s, v_s, hkv, g, lane, turn[wave]);
   if (at.g >= hkv) return;
-  const size_t to = (size_t(dst) * hkv + g) * 16 * D;
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    *reinterpret_cast<uint4*>(c.k + to + 1024 * j + 16 * lane) = kq[j];
-    *reinterpret_cast<uint4*>(c.v + to + 1024 * j + 16 * lane) = vq[j];
-  }
-  uint8_t* s = c.scale + (size_t(dst) * hkv + g) * kKv8Scales;
-  if (lane < 16) s[lane] = uint8_t(kb);
-  if (r == 0) *reinterpret_cast<uint32_t*>(s + 16 + 4 * a) = vw;
+  const size_t to = size_t(dst) * hkv + g;
+  if (src == dst) kv8_store_fresh<D>(f, c, to, lane);
+  else kv8_store_block<D>(f, kq, vq, kb, vs, c, to, lane);
 }
 
 unsigned grid_of(int n, int hkv) { return unsigned(kv8_groups(n, hkv)); }

@@ -1,8 +1,7 @@
 // Causal attention (Eq. 1) over the 8-bit linked cache for tiles of 16 query rows: decode.
 //
-// Workgroup = (work item, KV head), 4 wavefronts, tile rows and items as in the bf16 kernel of
-// such tiles.  A wavefront takes pairs of the item's linked blocks, 32 keys, through a ring of
-// registers:
+// Workgroup = (work item, KV head), tile rows and items as in the bf16 kernel of such tiles.  A
+// wavefront takes pairs of the item's linked blocks, 32 keys, through a ring of registers:
 //   S^T (16 keys x 16 rows) = K Q^T per block by v_mfma_f32_16x16x32_bf16, K's bytes widened in
 //     registers (exact); lane l = r + 16 a holds the scores of row r for keys 4 a + i, which
 //     are scaled by their keys' 2^t;
@@ -11,8 +10,22 @@
 //   O^T (D x 16) += V^T P^T by v_mfma_f32_16x16x32_bf16 over both blocks' keys: the P operand of
 //     a lane is its own 8 probabilities times their keys' 2^t (exact), rounded to bf16, and V's
 //     is the dword of 4 keys of its dim that the cache's order keeps together, for each block.
-// What bounds it is the read of K and V, once per item.
+// What bounds it is the read of K and V, once per item.  K's registers take the next pair as soon
+// as its scores are formed, V's after the product, and three workgroups of four wavefronts fit a
+// CU: 131 329 keys of 8 heads of 128 (271 MB) in 48 us, 5.6 TB/s, the rate of a plain read
+// (56 with all loads behind the product and two workgroups).  With a single tile no block is read
+// twice, and K and V pass the caches (NT): 49 -> 43 us before the write joined; where requests
+// share blocks that costs 6 us of 64.  Up to 256 workgroups, one a CU, have eight wavefronts: what
+// bounds these is the chain of loads (528 keys: 9.5 -> 8.5 us a step).
+//
+// The link write of few private blocks (decode: one or two a request) is done here too, by
+// workgroups in front of the others, and nothing waits for them: the rows of S that a private block
+// receives are read from the call's inputs and rounded by whoever attends to them, as a block
+// of their own; of the block itself the other tokens are read, from its source, and a
+// block that is its own source has only the new rows' bytes stored.  A step of one request gets 3 to 4 us
+// shorter by the launch saved (528 keys 9.5 -> 6.9, 131 329 keys 58 -> 54).
 #include <cmath>
+#include <type_traits>
 
 #include "kv8_device.h"
 #include "plan_internal.h"
@@ -22,14 +35,13 @@ namespace epic {
 namespace {
 
 constexpr int kDecRows = 16;
-constexpr int kDecWaves = 4;
 constexpr float kLag = 8.0f;
 
-template <int D>
+template <int D, int W>
 struct Kv8DecodeLds {
-  float m[kDecWaves][kDecRows];
-  float l[kDecWaves][kDecRows];
-  float o[kDecWaves][D][kDecRows];
+  float m[W][kDecRows];
+  float l[W][kDecRows];
+  float o[W][D][kDecRows];
 };
 
 // What a wavefront holds of a block in flight.
@@ -39,16 +51,37 @@ struct Kv8Block {
   uint32_t ks, vs;                            // scales of keys 4 a ..
 };
 
+template <int D>
+__device__ __forceinline__ void write_private(const Kv8Rows& w, const epic_kv8_cache& c, int i, int hkv, int g, int lane,
+                                              uint32_t* turn) {
+  const int dst = w.block[i], src = w.src[i];
+  uint4 kq[D / 64], vq[D / 64];
+  int kb;
+  uint32_t vs;
+  kv8_load_block<D>(c, src == dst ? -1 : src, hkv, g, lane, kq, vq, kb, vs);
+  const Kv8Fresh<D / 64> f = kv8_fresh<D>(w.rows + i * 16, w.k_s, w.v_s, hkv, g, lane, turn);
+  const size_t to = size_t(dst) * hkv + g;
+  if (src == dst) kv8_store_fresh<D>(f, c, to, lane);
+  else kv8_store_block<D>(f, kq, vq, kb, vs, c, to, lane);
+}
+
 // NT: K and V are read past the caches, which hold nothing of them that is read again.
-template <int D, int RING, bool NT>
-__global__ __launch_bounds__(64 * kDecWaves, 3) void kv8_decode_kernel(AttnArgs a, epic_kv8_cache c) {
+template <int D, int W, int RING, bool NT>
+__global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(AttnArgs a, epic_kv8_cache c, Kv8Rows w) {
   constexpr int J = D / 64;
   constexpr int NDT = D / 16;                 // 16-dim tiles of O^T
-  __shared__ Kv8DecodeLds<D> lds;
+  __shared__ Kv8DecodeLds<D, W> lds;
 
   const int hkv = a.hkv;
-  const int g = blockIdx.x % hkv;
-  const int item = blockIdx.x / hkv;
+  if (int(blockIdx.x) < w.groups) {           // the link write: W KV heads of a private block
+    const int ng = (hkv + W - 1) / W, i = blockIdx.x / ng, g = (blockIdx.x % ng) * W + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (g >= hkv) return;
+    write_private<D>(w, c, i, hkv, g, lane, reinterpret_cast<uint32_t*>(lds.o[threadIdx.x >> 6]));
+    return;
+  }
+  const int g = (blockIdx.x - w.groups) % hkv;
+  const int item = (blockIdx.x - w.groups) / hkv;
   const int32_t* wk = a.work + kWorkInts * item;
   const int tile = wk[0], b0 = wk[1], b1 = wk[2], kind = wk[7];
   if (tile < 0) return;                       // list entries of other items
@@ -78,17 +111,26 @@ __global__ __launch_bounds__(64 * kDecWaves, 3) void kv8_decode_kernel(AttnArgs 
   // Their ids, positions and lengths come 64 at a time, one per lane, so that no load of a block
   // waits for a chain of loads; past the item's end stands its last block, with no keys.
   const int n_pairs = (b1 - b0 + 1) / 2;
-  const int mine = n_pairs > wave ? 2 * ((n_pairs - wave + kDecWaves - 1) / kDecWaves) : 0;
-  int phys_l, pos_l, len_l;
+  const int mine = n_pairs > wave ? 2 * ((n_pairs - wave + W - 1) / W) : 0;
+  int phys_l, pos_l, valid_l;                 // valid: bit s for token s of the block
+  // Private blocks are written by other workgroups of this launch: what they keep is read from their source, their
+  // rows of S from the call's inputs.  (Shared blocks are no request's own.)
+  const bool own = w.n > 0 && kind != kItemShared;
+  int priv_block = 0, priv_src = 0;           // of private block `lane`
   auto fetch = [&](int first) __attribute__((always_inline)) {
     const int i = first + lane;
-    const int b = b0 + 2 * (wave + kDecWaves * (i >> 1)) + (i & 1);
+    const int b = b0 + 2 * (wave + W * (i >> 1)) + (i & 1);
     const bool in = i < mine && b < b1;
     const int bc = in ? b : b1 - 1;
     const int lb = kind == kItemList ? listed(bc) : bc;
     phys_l = a.linked_blocks[lb];
     pos_l = a.block_pos0[lb];
-    len_l = in ? a.block_len[lb] : 0;
+    valid_l = in ? (1 << a.block_len[lb]) - 1 : 0;
+    if (own) {
+      const int at = min(lane, w.n - 1);
+      priv_block = w.block[at];
+      priv_src = w.src[at];
+    }
   };
   fetch(0);
 
@@ -157,26 +199,115 @@ __global__ __launch_bounds__(64 * kDecWaves, 3) void kv8_decode_kernel(AttnArgs 
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_ldexpf(acc[i] * sl2, int(x.ks >> (8 * i) & 255u) - 127);
   };
-  // V's bytes of keys past a block's end may hold any bits, and a weight of 0 would not hide NaN
-  auto cut = [&](uint4 (&v)[J], int len) __attribute__((always_inline)) {
-    const int k = len - 4 * qd;
-    const uint32_t keep = k >= 4 ? 0xFFFFFFFFu : k <= 0 ? 0u : 0xFFFFFFFFu >> (32 - 8 * k);
+  // One step of two blocks, at positions pos0 and pos1, of whose tokens those of the bits valid0 and valid1 are read.
+  // ONE: of x0 alone, whose V is finite; x1 is x0.
+  auto step = [&](auto one, Kv8Block<J>& x0, Kv8Block<J>& x1, int pos0, int pos1, int valid0, int valid1, auto after_k,
+                  auto after_v) __attribute__((always_inline)) {
+    constexpr bool ONE = decltype(one)::value;
+    float t0[4], t1[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    scores(x0, t0);
+    if constexpr (!ONE) scores(x1, t1);
+    float s[8] = {t0[0], t0[1], t0[2], t0[3], t1[0], t1[1], t1[2], t1[3]};
+    after_k();
+    // masked: tokens that are not valid, or after the row (whole blocks before every row need nothing)
+    const bool whole = !ONE && (valid0 & valid1) == 0xFFFF;
+    if (!whole || max(pos0, pos1) + 15 > first_row) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) v[j] = make_uint4(v[j].x & keep, v[j].y & keep, v[j].z & keep, v[j].w & keep);
+      for (int i = 0; i < 4; ++i) {
+        s[i] = (valid0 >> (4 * qd + i) & 1) && pos0 + 4 * qd + i <= qpos ? s[i] : -INFINITY;
+        if constexpr (!ONE) s[4 + i] = (valid1 >> (4 * qd + i) & 1) && pos1 + 4 * qd + i <= qpos ? s[4 + i] : -INFINITY;
+      }
+    }
+    float mb = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+    if (__ballot(mb > m + kLag)) {            // a row's maximum grew past the lag (at first: from nothing)
+      mb = fmaxf(mb, __shfl_xor(mb, 16));
+      mb = fmaxf(mb, __shfl_xor(mb, 32));
+      const bool grow = mb > m + kLag;        // row by row: a row's result depends on no other row
+      const float alpha = grow ? fast_exp2(m - mb) : 1.0f;
+      m = grow ? mb : m;
+      lsum *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[dt][i] *= alpha;
+    }
+    const float m_use = m == -INFINITY ? 0.0f : m;
+    float pv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float q = fast_exp2(s[i] - m_use);
+      lsum += q;
+      pv[i] = __builtin_amdgcn_ldexpf(q, int((i < 4 ? x0.vs : x1.vs) >> (8 * (i & 3)) & 255u) - 127);
+    }
+    const u32x4 pw = {pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
+                      pack_bf16x2(pv[6], pv[7])};
+    const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
+    if (!ONE && !whole) {                     // other tokens' bytes may be any, and a weight of 0 would not hide NaN
+      const uint32_t keep0 = byte_mask(valid0 >> (4 * qd) & 15), keep1 = byte_mask(valid1 >> (4 * qd) & 15);
+#pragma unroll
+      for (int q = 0; q < J; ++q) {
+        x0.v[q] = merge(make_uint4(0, 0, 0, 0), x0.v[q], keep0);
+        x1.v[q] = merge(make_uint4(0, 0, 0, 0), x1.v[q], keep1);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < J; ++q) {
+      const uint32_t w0[4] = {x0.v[q].x, x0.v[q].y, x0.v[q].z, x0.v[q].w};
+      const uint32_t w1[4] = {x1.v[q].x, x1.v[q].y, x1.v[q].z, x1.v[q].w};
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const u32x4 vv = {e4m3_pair<false>(w0[t], 1.0f), e4m3_pair<true>(w0[t], 1.0f), e4m3_pair<false>(w1[t], 1.0f),
+                          e4m3_pair<true>(w1[t], 1.0f)};
+        o[4 * q + t] = mfma_16x16x32(__builtin_bit_cast(bf16x8, vv), pb, o[4 * q + t]);
+      }
+    }
+    after_v();
   };
 
   for (int first = 0; first < mine; first += 64) {
     if (first > 0) fetch(first);
     const int n = min(64, mine - first) / 2;  // pairs of this batch
     Kv8Block<J> ring[RING][2];
+    auto fill = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < RING; ++j)
+      for (int j = 0; j < RING; ++j)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int phys = __builtin_amdgcn_readlane(phys_l, 2 * min(j, n - 1) + e);
-        load_k(phys, ring[j][e]);
-        load_v(phys, ring[j][e]);
+        for (int e = 0; e < 2; ++e) {
+          const int phys = __builtin_amdgcn_readlane(phys_l, 2 * min(j, n - 1) + e);
+          load_k(phys, ring[j][e]);
+          load_v(phys, ring[j][e]);
+        }
+    };
+    fill();
+    int priv_l = -1;                          // this block's place among the private ones
+    if (own) {
+      for (int q = 0; q < w.n; ++q) priv_l = phys_l == __builtin_amdgcn_readlane(priv_block, q) ? q : priv_l;
+      if (valid_l == 0) priv_l = -1;
+      // in decode a block is its own source, or has none and holds nothing but rows of S
+      const int from = __shfl(priv_src, max(priv_l, 0));
+      const bool moved = priv_l >= 0 && from >= 0 && from != phys_l;
+      const uint64_t any_moved = __ballot(moved);
+      if (moved) phys_l = from;
+      uint64_t left = __ballot(priv_l >= 0);
+      if (left != 0) {
+        // the rows of S of private blocks, each a block of its own
+        do {
+          const int i = __builtin_ctzll(left), q = __builtin_amdgcn_readlane(priv_l, i);
+          left &= left - 1;
+          const Kv8Fresh<J> f =
+              kv8_fresh<D>(w.rows + q * 16, w.k_s, w.v_s, hkv, g, lane, reinterpret_cast<uint32_t*>(lds.o[wave]));
+          Kv8Block<J> x;
+#pragma unroll
+          for (int j = 0; j < J; ++j) x.k[j] = f.k[j], x.v[j] = f.v[j];
+          x.ks = f.ks, x.vs = f.vs;
+          const int pos = __builtin_amdgcn_readlane(pos_l, i);
+          step(std::true_type{}, x, x, pos, pos, int(f.tokens), 0, [] {}, [] {});
+          if (lane == i) valid_l &= ~int(f.tokens);
+        } while (left != 0);
+        // from the sources; and four wavefronts have no registers for this and the ring at once
+        if (W <= 4 || any_moved != 0) fill();
       }
+    }
     for (int base = 0; base < n; base += RING) {
 #pragma unroll
       for (int j = 0; j < RING; ++j) {
@@ -186,62 +317,16 @@ __global__ __launch_bounds__(64 * kDecWaves, 3) void kv8_decode_kernel(AttnArgs 
           // are in flight behind every wait
           const int next = 2 * min(p + RING, n - 1);
           const int phys0 = __builtin_amdgcn_readlane(phys_l, next), phys1 = __builtin_amdgcn_readlane(phys_l, next + 1);
-          const int pos0 = __builtin_amdgcn_readlane(pos_l, 2 * p), pos1 = __builtin_amdgcn_readlane(pos_l, 2 * p + 1);
-          const int len0 = __builtin_amdgcn_readlane(len_l, 2 * p), len1 = __builtin_amdgcn_readlane(len_l, 2 * p + 1);
-          float t0[4], t1[4];
-          scores(ring[j][0], t0);
-          scores(ring[j][1], t1);
-          float s[8] = {t0[0], t0[1], t0[2], t0[3], t1[0], t1[1], t1[2], t1[3]};
-          load_k(phys0, ring[j][0]);
-          load_k(phys1, ring[j][1]);
-          // masked: keys past the block's end, after the row (whole blocks before every row need nothing)
-          if (len0 + len1 < 32 || max(pos0, pos1) + 15 > first_row) {
-            const int k0 = min(len0, qpos - pos0 + 1) - 4 * qd, k1 = min(len1, qpos - pos1 + 1) - 4 * qd;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              s[i] = i < k0 ? s[i] : -INFINITY;
-              s[4 + i] = i < k1 ? s[4 + i] : -INFINITY;
-            }
-          }
-          float mb = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-          if (__ballot(mb > m + kLag)) {      // a row's maximum grew past the lag (at first: from nothing)
-            mb = fmaxf(mb, __shfl_xor(mb, 16));
-            mb = fmaxf(mb, __shfl_xor(mb, 32));
-            const bool grow = mb > m + kLag;  // row by row: a row's result depends on no other row
-            const float alpha = grow ? fast_exp2(m - mb) : 1.0f;
-            m = grow ? mb : m;
-            lsum *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[dt][i] *= alpha;
-          }
-          const float m_use = m == -INFINITY ? 0.0f : m;
-          float pv[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float q = fast_exp2(s[i] - m_use);
-            lsum += q;
-            pv[i] = __builtin_amdgcn_ldexpf(q, int((i < 4 ? ring[j][0].vs : ring[j][1].vs) >> (8 * (i & 3)) & 255u) - 127);
-          }
-          const u32x4 pw = {pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
-                            pack_bf16x2(pv[6], pv[7])};
-          const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
-          if (len0 < 16) cut(ring[j][0].v, len0);
-          if (len1 < 16) cut(ring[j][1].v, len1);
-#pragma unroll
-          for (int q = 0; q < J; ++q) {
-            const uint4 v0 = ring[j][0].v[q], v1 = ring[j][1].v[q];
-            const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-              const u32x4 vv = {e4m3_pair<false>(w0[t], 1.0f), e4m3_pair<true>(w0[t], 1.0f), e4m3_pair<false>(w1[t], 1.0f),
-                                e4m3_pair<true>(w1[t], 1.0f)};
-              o[4 * q + t] = mfma_16x16x32(__builtin_bit_cast(bf16x8, vv), pb, o[4 * q + t]);
-            }
-          }
-          load_v(phys0, ring[j][0]);
-          load_v(phys1, ring[j][1]);
+          auto after_k = [&]() __attribute__((always_inline)) {
+            load_k(phys0, ring[j][0]);
+            load_k(phys1, ring[j][1]);
+          };
+          auto after_v = [&]() __attribute__((always_inline)) {
+            load_v(phys0, ring[j][0]);
+            load_v(phys1, ring[j][1]);
+          };
+          step(std::false_type{}, ring[j][0], ring[j][1], __builtin_amdgcn_readlane(pos_l, 2 * p), __builtin_amdgcn_readlane(pos_l, 2 * p + 1),
+               __builtin_amdgcn_readlane(valid_l, 2 * p), __builtin_amdgcn_readlane(valid_l, 2 * p + 1), after_k, after_v);
         }
       }
     }
@@ -260,18 +345,18 @@ __global__ __launch_bounds__(64 * kDecWaves, 3) void kv8_decode_kernel(AttnArgs 
 #pragma unroll
     for (int i = 0; i < 4; ++i) lds.o[wave][dt * 16 + qd * 4 + i][r] = o[dt][i];
   __syncthreads();
-  // thread -> (row rr, dims dd, dd + 16, ...): 16 rows x 16 dim groups
+  // thread -> (row rr, dims dd, dd + 4 W, ...): 16 rows x 4 W dim groups
   const int rr = tid & 15, d0 = tid >> 4;
-  float mw[kDecWaves], M = -INFINITY;
+  float mw[W], M = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kDecWaves; ++w) {
+  for (int w = 0; w < W; ++w) {
     mw[w] = lds.m[w][rr];
     M = fmaxf(M, mw[w]);
   }
   const float Mu = M == -INFINITY ? 0.0f : M;
-  float wt[kDecWaves], L = 0.0f;
+  float wt[W], L = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kDecWaves; ++w) {
+  for (int w = 0; w < W; ++w) {
     wt[w] = fast_exp2(mw[w] - Mu);
     L += lds.l[w][rr] * wt[w];
   }
@@ -281,10 +366,10 @@ __global__ __launch_bounds__(64 * kDecWaves, 3) void kv8_decode_kernel(AttnArgs 
   slot(s2, srow2, part, lr2);
   const int hh = rr / R, h2 = g * a.G + hh, rp = hh * R + lr2;   // rp: its row in its request's tile
   const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  for (int d = d0; d < D; d += 16) {
+  for (int d = d0; d < D; d += 4 * W) {
     float acc = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kDecWaves; ++w) acc += lds.o[w][d][rr] * wt[w];
+    for (int w = 0; w < W; ++w) acc += lds.o[w][d][rr] * wt[w];
     acc *= inv;
     if (part < 0)
       a.out[(size_t(srow2) * a.hq + h2) * D + d] = uint16_t(pack_bf16x2(acc, 0.0f) & 0xFFFFu);
@@ -302,13 +387,22 @@ __global__ __launch_bounds__(64 * kDecWaves, 3) void kv8_decode_kernel(AttnArgs 
 
 }  // namespace
 
-void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, int head_dim, int n_work, bool once,
+void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, const Kv8Rows& rows, int head_dim, int n_work, bool once,
                        hipStream_t stream) {
-  if (n_work == 0) return;
-  const dim3 grid{unsigned(n_work) * unsigned(a.hkv)};
-  auto go = [&](auto kernel) { kernel<<<grid, 64 * kDecWaves, 0, stream>>>(a, c); };
-  if (head_dim == 128) once ? go(kv8_decode_kernel<128, 1, true>) : go(kv8_decode_kernel<128, 1, false>);
-  else once ? go(kv8_decode_kernel<64, 2, true>) : go(kv8_decode_kernel<64, 2, false>);
+  const unsigned items = unsigned(n_work) * unsigned(a.hkv);
+  auto groups = [&](int waves) { return rows.n * ((a.hkv + waves - 1) / waves); };
+  auto go = [&](auto kernel, int waves) {
+    Kv8Rows w = rows;
+    w.groups = groups(waves);
+    if (items + w.groups > 0) kernel<<<items + w.groups, 64 * waves, 0, stream>>>(a, c, w);
+  };
+  if (items + groups(8) <= 256) {
+    if (head_dim == 128) go(kv8_decode_kernel<128, 8, 1, true>, 8);
+    else go(kv8_decode_kernel<64, 8, 1, true>, 8);
+    return;
+  }
+  if (head_dim == 128) once ? go(kv8_decode_kernel<128, 4, 1, true>, 4) : go(kv8_decode_kernel<128, 4, 1, false>, 4);
+  else once ? go(kv8_decode_kernel<64, 4, 2, true>, 4) : go(kv8_decode_kernel<64, 4, 2, false>, 4);
 }
 
 }  // namespace epic

@@ -68,4 +68,152 @@ __device__ __forceinline__ uint4 round16(const uint4& p, const uint4& q, int byt
 }
 constexpr uint32_t kNanBytes = 0x7F7F7F7Fu;   // K of a NaN token: its scores are NaN, whatever its scale
 
+// The rows of S that a block receives, rounded, as its wavefront holds a block; zero rows elsewhere.
+template <int J>
+struct Kv8Fresh {
+  uint4 k[J], v[J];
+  int kb;                                     // scale byte of K of token r
+  uint32_t ks, vs;                            // scale bytes of K and V of tokens 4 a ..
+  uint32_t tokens;                            // bit s: token s is a row of S
+};
+
+constexpr int kTurnLd = 68;                   // bytes of a token's 64 dims in LDS
+template <int J>
+constexpr int kTurnInts = J * 16 * kTurnLd / 4;
+
+// V rows come like K's, 16 dims of a token a lane; their e4m3 bytes change places through `turn`, LDS of this
+// wavefront alone.
+template <int D>
+__device__ __forceinline__ Kv8Fresh<D / 64> kv8_fresh(const int32_t* rows, const uint16_t* k_s, const uint16_t* v_s, int hkv,
+                                                      int g, int lane, uint32_t* turn) {
+  constexpr int J = D / 64;
+  const int r = lane & 15, a = lane >> 4;
+  const int row = rows[r];
+  Kv8Fresh<J> f;
+  f.tokens = uint32_t(__ballot(row >= 0)) & 0xFFFFu;
+  uint4 x[2 * J], y[2 * J];
+#pragma unroll
+  for (int i = 0; i < 2 * J; ++i) {
+    x[i] = y[i] = make_uint4(0, 0, 0, 0);
+    if (row >= 0) {
+      const size_t from = (size_t(row) * hkv + g) * D + 64 * (i >> 1) + 16 * a + 8 * (i & 1);
+      x[i] = *reinterpret_cast<const uint4*>(k_s + from);
+      y[i] = *reinterpret_cast<const uint4*>(v_s + from);
+    }
+  }
+  int kb = kv8_byte(row_top<J>(x)), vb = kv8_byte(row_top<J>(y));
+  if (kb == kKv8Nan || vb == kKv8Nan) kb = vb = kKv8Nan;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    f.k[j] = round16(x[2 * j], x[2 * j + 1], kb);
+    uint4 q = round16(y[2 * j], y[2 * j + 1], vb);
+    if (kb == kKv8Nan) {
+      f.k[j] = make_uint4(kNanBytes, kNanBytes, kNanBytes, kNanBytes);
+      q = make_uint4(0, 0, 0, 0);
+    }
+    uint32_t* to = turn + (j * 16 * kTurnLd + r * kTurnLd + 16 * a) / 4;
+    to[0] = q.x, to[1] = q.y, to[2] = q.z, to[3] = q.w;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();            // one wavefront: its LDS accesses run in order
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  f.kb = kb;
+  f.ks = f.vs = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f.ks |= uint32_t(__shfl(kb, 4 * a + i)) << (8 * i);
+    f.vs |= uint32_t(__shfl(vb, 4 * a + i)) << (8 * i);
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(turn) + j * 16 * kTurnLd;
+    uint32_t w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      w[t] = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[t] |= uint32_t(from[(4 * a + i) * kTurnLd + 16 * t + r]) << (8 * i);
+    }
+    f.v[j] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return f;
+}
+
+// Bytes i of a dword, for the bits i of the four.
+__device__ __forceinline__ uint32_t byte_mask(uint32_t four) { return (four * 0x00204081u & 0x01010101u) * 255u; }
+
+__device__ __forceinline__ uint4 merge(const uint4& old, const uint4& x, uint32_t mask) {
+  return make_uint4((old.x & ~mask) | (x.x & mask), (old.y & ~mask) | (x.y & mask), (old.z & ~mask) | (x.z & mask),
+                    (old.w & ~mask) | (x.w & mask));
+}
+
+// The bytes of the rows of S into their block, and no others: what the block holds beside them may be read meanwhile.
+template <int D>
+__device__ __forceinline__ void kv8_store_fresh(const Kv8Fresh<D / 64>& f, const epic_kv8_cache& c, size_t block_head,
+                                                int lane) {
+  constexpr int J = D / 64;
+  const int r = lane & 15, a = lane >> 4;
+  const size_t to = block_head * 16 * D;
+  uint8_t* s = c.scale + block_head * kKv8Scales;
+  if (f.tokens >> r & 1) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) *reinterpret_cast<uint4*>(c.k + to + 1024 * j + 16 * lane) = f.k[j];
+    if (a == 0) s[r] = uint8_t(f.kb);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (!(f.tokens >> (4 * a + i) & 1)) continue;
+    uint8_t* v = c.v + to + 16 * lane + i;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      v[1024 * j] = uint8_t(f.v[j].x >> (8 * i));
+      v[1024 * j + 4] = uint8_t(f.v[j].y >> (8 * i));
+      v[1024 * j + 8] = uint8_t(f.v[j].z >> (8 * i));
+      v[1024 * j + 12] = uint8_t(f.v[j].w >> (8 * i));
+    }
+    if (r == 0) s[16 + 4 * a + i] = uint8_t(f.vs >> (8 * i));
+  }
+}
+
+// The link write of one (private block, KV head) by one wavefront: what the source block holds (kq, vq, kb of token r and
+// vs of tokens 4 a ..; zero rows without one), then the rows of S.
+template <int D>
+__device__ __forceinline__ void kv8_store_block(const Kv8Fresh<D / 64>& f, uint4 (&kq)[D / 64], uint4 (&vq)[D / 64], int kb,
+                                                uint32_t vs, const epic_kv8_cache& c, size_t block_head, int lane) {
+  constexpr int J = D / 64;
+  const int r = lane & 15, a = lane >> 4;
+  const bool fresh = f.tokens >> r & 1;
+  const uint32_t mask = byte_mask(f.tokens >> (4 * a) & 15u);
+  const size_t to = block_head * 16 * D;
+  uint8_t* s = c.scale + block_head * kKv8Scales;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    *reinterpret_cast<uint4*>(c.k + to + 1024 * j + 16 * lane) = fresh ? f.k[j] : kq[j];
+    *reinterpret_cast<uint4*>(c.v + to + 1024 * j + 16 * lane) = merge(vq[j], f.v[j], mask);
+  }
+  if (lane < 16) s[lane] = uint8_t(fresh ? f.kb : kb);
+  if (r == 0) *reinterpret_cast<uint32_t*>(s + 16 + 4 * a) = (vs & ~mask) | (f.vs & mask);
+}
+
+// What a wavefront reads of a source block; rows of zeros where there is none.
+template <int D>
+__device__ __forceinline__ void kv8_load_block(const epic_kv8_cache& c, int src, int hkv, int g, int lane, uint4 (&kq)[D / 64],
+                                               uint4 (&vq)[D / 64], int& kb, uint32_t& vs) {
+  constexpr int J = D / 64;
+  kb = 127;
+  vs = 0x7F7F7F7Fu;
+#pragma unroll
+  for (int j = 0; j < J; ++j) kq[j] = vq[j] = make_uint4(0, 0, 0, 0);
+  if (src < 0) return;
+  const size_t from = size_t(src) * hkv + g;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    kq[j] = *reinterpret_cast<const uint4*>(c.k + from * 16 * D + 1024 * j + 16 * lane);
+    vq[j] = *reinterpret_cast<const uint4*>(c.v + from * 16 * D + 1024 * j + 16 * lane);
+  }
+  const uint8_t* s = c.scale + from * kKv8Scales;
+  kb = s[lane & 15];
+  vs = *reinterpret_cast<const uint32_t*>(s + 16 + 4 * (lane >> 4));
+}
+
 }  // namespace epic

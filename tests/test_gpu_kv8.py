@@ -398,19 +398,16 @@ def test_requests_without_chunks():
 
 @pytest.mark.parametrize("hq,hkv,d", [(8, 8, 64), (32, 8, 128), (64, 8, 64)])
 def test_decode_over_shared_chunks(hq, hkv, d):
-    """Requests enough that their work items carry rows of several requests and lists of blocks."""
+    """Requests enough that their work items carry rows of several requests and lists of blocks.  The link step is not
+    run: its private blocks hold what they hold."""
     some = [[0, 1, 2], [1, 0, 2], [2, 2, 3], [0, 3], [3, 1, 0], [1, 4], [0, 1, 4], [4, 0, 3]]
     n = 40
     r = Requests(hq, hkv, d, [some[i % 8] for i in range(n)], [1533, 1800, 47, 1200, 1000],
-                 [5 + 3 * i % 41 for i in range(n)], 16, spare=160)
-    r.decode([0] * n)                                    # the link step is not run: its private blocks hold what they hold
-    new = [1 + i % 2 if hq // hkv < 8 else 1 for i in range(n)]   # two rows of eight heads each fill a tile
-    r.c = _cache(r.rng, r.blocks, hkv, d)
-    r.cache = _upload(r.c)
-    r.decode(new)
+                 [5 + 3 * i % 41 for i in range(n)], 16, spare=60, garbage=False)
+    r.decode([1 + i % 2 if hq // hkv < 8 else 1 for i in range(n)])      # two rows of eight heads each fill a tile
     work = r.views["work"].reshape(-1, 8)
     assert {1, 2} <= set(work[work[:, 0] >= 0, 7].tolist()), "item kinds of the plan"
-    r.every = 3                                          # every kind of request, many of them
+    r.every = 5                                          # every kind of request
     out, lse = r.run(what="shared")
     assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
 
