@@ -105,9 +105,11 @@ extern "C" epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const e
   st = check_cache(cache);
   if (st != EPIC_OK) return st;
   const int hkv = cfg->num_kv_heads, d = cfg->head_dim;
-  if (kv8_groups(sizes->n_private, hkv) > kKv8MaxGroups || kv8_groups(sizes->n_linked_blocks, hkv) > kKv8MaxGroups)
-    return fail(EPIC_ERR_UNSUPPORTED, "%d linked and %d private blocks of %d KV heads are too many", sizes->n_linked_blocks,
-                sizes->n_private, hkv);
+  // a launch has fewer than 2^32 threads: 256 per four KV heads of a block, up to 512 per KV head of a work item
+  if (kv8_groups(int64_t(sizes->n_private) + sizes->n_linked_blocks, hkv) > kKv8MaxGroups ||
+      2 * (int64_t(sizes->n_work) + sizes->n_private) * hkv > kKv8MaxGroups)
+    return fail(EPIC_ERR_UNSUPPORTED, "%d linked and %d private blocks, %d work items of %d KV heads are too many",
+                sizes->n_linked_blocks, sizes->n_private, sizes->n_work, hkv);
   hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
   if (sizes->n_s > 0) {
     EPIC_CHECK_ARG(q_s && k_s && v_s && out, "NULL tensor argument");
@@ -120,26 +122,33 @@ extern "C" epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const e
     EPIC_CHECK_ARG(aligned16(workspace), "workspace must be 16-byte aligned");
   }
   record_profile_event(0, stream);
-  const bool tiny = sizes->tile_rows == kTileRowsTiny && sizes->n_s > 0;
-  // Decode: few private blocks, none turned: the attention launch writes them itself
-  const bool joined = tiny && sizes->n_rerotated == 0 && sizes->n_private <= kKv8MaxRows;
-  if (!joined)
-    launch_kv8_write(plan_dev, sizes->n_private, sizes->n_rerotated > 0, hkv, d, cfg->rope_theta, k_s, v_s, *cache, stream);
+  const bool tiny = sizes->tile_rows == kTileRowsTiny;
+  Kv8Rows rows{plan_dev->priv_block, plan_dev->priv_src, plan_dev->priv_rows, k_s, v_s, sizes->n_private, 0};
+  // Decode: few private blocks, none turned, are written by the launch that reads them
+  const bool joined = tiny && sizes->n_s > 0 && sizes->n_rerotated == 0 && sizes->n_private <= kKv8JoinedRows;
+  if (!joined) {
+    launch_kv8_write(rows, sizes->n_rerotated > 0 ? plan_dev->priv_rot : nullptr, hkv, d, cfg->rope_theta, *cache, stream);
+    rows.n = 0;
+  }
   if (sizes->n_s == 0) return hip_status("8-bit link write launch");      // re-rotated copies only
   AttnArgs a = attention_args(cfg, sizes, plan_dev, q_s, nullptr, nullptr, out, lse, workspace);
   if (tiny) {
-    const Kv8Rows rows{plan_dev->priv_block, plan_dev->priv_src, plan_dev->priv_rows, k_s, v_s, joined ? sizes->n_private : 0, 0};
     record_profile_event(1, stream);
     launch_kv8_decode(a, *cache, rows, d, sizes->n_work, sizes->n_tiles == 1, stream);
   } else {
-    // The matrix cores bound wide tiles, and every tile would widen the same keys again: the
-    // linked blocks are widened once, for the bf16 kernel.
+    // The matrix cores bound wide tiles, and every tile would widen the same keys again: they are widened once, for
+    // the bf16 kernel.  Requests that share blocks link more of them than there are: the pool then, block by block.
     char* ws = static_cast<char*>(workspace);
     uint16_t* k = reinterpret_cast<uint16_t*>(ws + w.k);
     uint16_t* v = reinterpret_cast<uint16_t*>(ws + w.v);
     int32_t* table = reinterpret_cast<int32_t*>(ws + w.table);
-    launch_kv8_expand(plan_dev->linked_blocks, sizes->n_linked_blocks, hkv, d, *cache, k, v, table, stream);
-    a.k_cache = k, a.v_cache = v, a.linked_blocks = table;
+    a.k_cache = k, a.v_cache = v;
+    if (cache->num_blocks < sizes->n_linked_blocks) {
+      launch_kv8_expand(nullptr, cache->num_blocks, hkv, d, *cache, k, v, nullptr, stream);
+    } else {
+      launch_kv8_expand(plan_dev->linked_blocks, sizes->n_linked_blocks, hkv, d, *cache, k, v, table, stream);
+      a.linked_blocks = table;
+    }
     record_profile_event(1, stream);
     launch_link_attention(a, d, sizes->n_work, stream);
   }

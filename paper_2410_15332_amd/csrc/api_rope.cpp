@@ -75,8 +75,8 @@ extern "C" epic_status epic_qk_norm_rope(const epic_attn_cfg* cfg, const epic_ro
   EPIC_CHECK_ARG(ld >= cols && ld * elem % 16 == 0, "row stride %lld: at least %lld, and a multiple of 16 bytes", (long long)ld,
                  (long long)cols);
   if (q_norm || k_norm) EPIC_CHECK_ARG(eps > 0.0f, "eps must be > 0");
-  // 31-bit (row of a workgroup, head) counts and grids
-  if (rows > kQkMaxRows || cols > (int64_t(1) << 26) || ld > (int64_t(1) << 40))
+  // grids, and byte counts below 2^63
+  if (rows > kQkMaxRows || cols > (int64_t(1) << 26) || ld > (int64_t(1) << 36))
     return fail(EPIC_ERR_UNSUPPORTED, "%d rows of %lld values are too many", rows, (long long)cols);
   if (rows == 0) return EPIC_OK;
   EPIC_CHECK_ARG(qkv && pos && q && k && v, "NULL tensor argument");

@@ -29,24 +29,26 @@ void launch_kv8_pack(const Kv8Move& mv, int head_dim, const uint16_t* k, const u
                      hipStream_t stream);
 void launch_kv8_unpack(const Kv8Move& mv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
                        hipStream_t stream);
-// The linked blocks of a plan as a bf16 cache of their own, [n_linked_blocks], for the attention kernel of
-// wide tiles, and the table 0 .. n_linked_blocks - 1 that it reads them by.  Tokens that are NaN get K = NaN, V = 0.
-void launch_kv8_expand(const int32_t* linked_blocks, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k,
-                       uint16_t* v, int32_t* table, hipStream_t stream);
-// As launch_link_write and launch_link_write_rotated (rope_theta is read where blocks move).
-void launch_kv8_write(const epic_plan* plan, int n_private, bool rotated, int hkv, int head_dim, float rope_theta,
-                      const uint16_t* k_s, const uint16_t* v_s, const epic_kv8_cache& c, hipStream_t stream);
-// The private blocks that an attention launch writes itself.
+// Private blocks, their sources and the rows of S that they receive.
 struct Kv8Rows {
   const int32_t *block, *src, *rows;          // priv_block, priv_src, priv_rows
   const uint16_t *k_s, *v_s;
-  int n;                                      // at most kKv8MaxRows; 0: they are written
-  int groups;                                 // workgroups that write them (set by the launcher)
+  int n;                                      // private blocks; 0 in launches that find them written
+  int groups;                                 // workgroups of the launch that write them (set by the launcher)
 };
-constexpr int kKv8MaxRows = 64;               // a lane each
+// Most that the decode launch writes itself: each of its wavefronts looks through them, a lane each.
+constexpr int kKv8JoinedRows = 64;
 
-// As launch_link_decode; a.k_cache and a.v_cache are not read.  once: no two work items read the same block.
-void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, const Kv8Rows& rows, int head_dim, int n_work, bool once,
+// As launch_link_write and (priv_rot not null) launch_link_write_rotated.
+void launch_kv8_write(const Kv8Rows& w, const int32_t* priv_rot, int hkv, int head_dim, float rope_theta,
+                      const epic_kv8_cache& c, hipStream_t stream);
+// Listed blocks (null: blocks 0 .. n - 1) as a bf16 cache of n blocks, for the attention kernel of wide tiles, and the
+// table 0 .. n - 1 where not null.
+void launch_kv8_expand(const int32_t* list, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
+                       int32_t* table, hipStream_t stream);
+// As launch_link_decode; a.k_cache and a.v_cache are not read.  Writes the private blocks of w.  once: no two work
+// items read the same block.
+void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, const Kv8Rows& w, int head_dim, int n_work, bool once,
                        hipStream_t stream);
 
 }  // namespace epic

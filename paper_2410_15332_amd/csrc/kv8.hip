@@ -25,10 +25,10 @@ constexpr int kThreads = 64 * kWaves;
 // The (list entry, KV head) of this wavefront.
 struct Place {
   int i, g;
-  __device__ __forceinline__ explicit Place(int hkv) {
+  __device__ __forceinline__ Place(int hkv, int group) {
     const int ng = (hkv + kWaves - 1) / kWaves;
-    i = int(blockIdx.x) / ng;
-    g = (int(blockIdx.x) % ng) * kWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    i = group / ng;
+    g = (group % ng) * kWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   }
 };
 
@@ -45,7 +45,7 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const uint16_t* __restrict__ k,
                                                             const uint16_t* __restrict__ v, epic_kv8_cache c) {
   constexpr int J = D / 64;
-  const Place at(mv.hkv);
+  const Place at(mv.hkv, blockIdx.x);
   if (at.g >= mv.hkv) return;
   const int src = mv.src ? mv.src[at.i] : at.i, dst = mv.dst ? mv.dst[at.i] : at.i;
   if (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks)) return;
@@ -96,46 +96,33 @@ __global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const ui
   if (r == 0) *reinterpret_cast<uint32_t*>(s + 16 + 4 * a) = vb[0] | vb[1] << 8 | vb[2] << 16 | uint32_t(vb[3]) << 24;
 }
 
-// The values of 8-bit blocks in bf16, as a cache of the other kind.  Exact, but for results
-// outside bf16's range.  EXPAND: for the attention kernel, block i of the list into block i;
-// K = NaN, V = 0 for NaN tokens (that kernel multiplies masked V by 0).  Else NaN in both.
-template <int D, bool EXPAND>
-__global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_kv8_cache c, uint16_t* __restrict__ k,
-                                                              uint16_t* __restrict__ v, int32_t* __restrict__ table) {
-  constexpr int J = D / 64;
-  const Place at(mv.hkv);
-  if (at.g >= mv.hkv) return;
-  const int src = mv.src ? mv.src[at.i] : at.i, dst = EXPAND || !mv.dst ? at.i : mv.dst[at.i];
-  if (!EXPAND && (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks))) return;
-  const int lane = threadIdx.x & 63, r = lane & 15, a = lane >> 4;
-  const size_t from = (size_t(src) * mv.hkv + at.g) * 16 * D, to = (size_t(dst) * mv.hkv + at.g) * 16 * D;
-  uint4 x[J], y[J];
-  const uint8_t* s = c.scale + (size_t(src) * mv.hkv + at.g) * kKv8Scales;
-  const int kb = s[r];
-  const uint32_t vw = *reinterpret_cast<const uint32_t*>(s + 16 + 4 * a);
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    x[j] = *reinterpret_cast<const uint4*>(c.k + from + 1024 * j + 16 * lane);
-    y[j] = *reinterpret_cast<const uint4*>(c.v + from + 1024 * j + 16 * lane);
-  }
-  // over the scale and then times it, in fp32: both exact, and no scale of 2^-127 as a float
-  auto wide = [&](uint32_t w, int b0, int b1, int b2, int b3) {
-    auto one = [&](float f, int b) {
-      const float z = __builtin_amdgcn_ldexpf(f, b - 127);
-      return b == kKv8Nan ? (EXPAND ? 0.0f : __uint_as_float(0x7FC00000u)) : z;
-    };
-    return make_uint2(pack_bf16x2(one(__builtin_amdgcn_cvt_f32_fp8(int(w), 0), b0), one(__builtin_amdgcn_cvt_f32_fp8(int(w), 1), b1)),
-                      pack_bf16x2(one(__builtin_amdgcn_cvt_f32_fp8(int(w), 2), b2), one(__builtin_amdgcn_cvt_f32_fp8(int(w), 3), b3)));
+// Four e4m3 of a dword times their 2^(byte - 127), as bf16: exact, but for results outside bf16's
+// range.  (In fp32: 2^-127 is no float to multiply by in bf16.)  Byte 255: `nan`.
+__device__ __forceinline__ uint2 wide4(uint32_t w, int b0, int b1, int b2, int b3, float nan) {
+  auto one = [&](float f, int b) {
+    const float z = __builtin_amdgcn_ldexpf(f, b - 127);
+    return b == kKv8Nan ? nan : z;
   };
+  return make_uint2(pack_bf16x2(one(__builtin_amdgcn_cvt_f32_fp8(int(w), 0), b0), one(__builtin_amdgcn_cvt_f32_fp8(int(w), 1), b1)),
+                    pack_bf16x2(one(__builtin_amdgcn_cvt_f32_fp8(int(w), 2), b2), one(__builtin_amdgcn_cvt_f32_fp8(int(w), 3), b3)));
+}
+
+// A block's K and V, as a wavefront holds them, into block `block_head` of a bf16 cache; V of NaN tokens: nan_v.
+template <int D>
+__device__ __forceinline__ void store_wide(const uint4 (&x)[D / 64], const uint4 (&y)[D / 64], int kb, uint32_t vs, float nan_v,
+                                           uint16_t* k, uint16_t* v, size_t block_head, int lane) {
+  const int r = lane & 15, a = lane >> 4;
+  const size_t to = block_head * 16 * D;
+  const float scale = __uint_as_float(uint32_t(kb) << 23);
   constexpr uint32_t kNanPair = 0x7FC07FC0u;
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
+  for (int j = 0; j < D / 64; ++j) {
     const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w}, u[4] = {y[j].x, y[j].y, y[j].z, y[j].w};
     uint2 q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      q[i] = wide(w[i], kb, kb, kb, kb);
-      if (EXPAND && kb == kKv8Nan) q[i] = make_uint2(kNanPair, kNanPair);
+      q[i] = make_uint2(e4m3_pair<false>(w[i], scale), e4m3_pair<true>(w[i], scale));
+      if (kb == kKv8Nan) q[i] = make_uint2(kNanPair, kNanPair);
     }
     uint4* kp = reinterpret_cast<uint4*>(k + to + r * D + 64 * j + 16 * a);
     kp[0] = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
@@ -143,92 +130,127 @@ __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_k
 #pragma unroll
     for (int t = 0; t < 4; ++t)
       *reinterpret_cast<uint2*>(v + to + (64 * j + 16 * t + r) * 16 + 4 * a) =
-          wide(u[t], vw & 255, vw >> 8 & 255, vw >> 16 & 255, vw >> 24);
+          wide4(u[t], vs & 255, vs >> 8 & 255, vs >> 16 & 255, vs >> 24, nan_v);
   }
-  if (EXPAND && at.g == 0 && lane == 0) table[at.i] = at.i;
 }
 
-// The link write: every private block takes what its source block holds (ROTATE: K turned by
-// priv_rot, from its 8-bit values to 8 bits again), then the rows of S, rounded to 8 bits, in
-// their slots.  A slot that neither fills holds a row of zeros.  A block that is its own
-// source only receives its rows.
-template <int D, bool ROTATE>
-__global__ __launch_bounds__(kThreads) void kv8_write_kernel(const int32_t* __restrict__ priv_block,
-                                                             const int32_t* __restrict__ priv_src,
-                                                             const int32_t* __restrict__ priv_rows,
-                                                             const int32_t* __restrict__ priv_rot,
-                                                             const uint16_t* __restrict__ k_s,
-                                                             const uint16_t* __restrict__ v_s, epic_kv8_cache c, int hkv,
-                                                             double log2_theta) {
+// 8192 blocks of 8 heads of 128 (806 MB): 165 us, 4.9 TB/s, the rate of a large copy.
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_kv8_cache c, uint16_t* __restrict__ k,
+                                                              uint16_t* __restrict__ v) {
+  const Place at(mv.hkv, blockIdx.x);
+  if (at.g >= mv.hkv) return;
+  const int src = mv.src ? mv.src[at.i] : at.i, dst = mv.dst ? mv.dst[at.i] : at.i;
+  if (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks)) return;
+  const int lane = threadIdx.x & 63;
+  uint4 x[D / 64], y[D / 64];
+  int kb;
+  uint32_t vs;
+  kv8_load_block<D>(c, size_t(src) * mv.hkv + at.g, lane, x, y, kb, vs);
+  store_wide<D>(x, y, kb, vs, __uint_as_float(0x7FC00000u), k, v, size_t(dst) * mv.hkv + at.g, lane);
+}
+
+// The attention kernel of wide tiles reads a bf16 cache: block i of the list (null: block i of the pool) into block i of
+// one, with K = NaN, V = 0 for NaN tokens (that kernel multiplies masked V by 0).  8208 blocks of 8 heads of 128 (809 MB):
+// 137 us, 5.9 TB/s.  (Forming private blocks here too, as decode does, saves the write's launch, 4 us, and costs
+// as much of 324 blocks and 20 us of 8208.)
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv8_expand_kernel(const int32_t* __restrict__ list, epic_kv8_cache c, int hkv,
+                                                              uint16_t* __restrict__ k, uint16_t* __restrict__ v,
+                                                              int32_t* __restrict__ table) {
+  const Place at(hkv, blockIdx.x);
+  if (at.g >= hkv) return;
+  const int lane = threadIdx.x & 63, phys = list ? list[at.i] : at.i;
+  uint4 x[D / 64], y[D / 64];
+  int kb;
+  uint32_t vs;
+  kv8_load_block<D>(c, size_t(phys) * hkv + at.g, lane, x, y, kb, vs);
+  store_wide<D>(x, y, kb, vs, 0.0f, k, v, size_t(at.i) * hkv + at.g, lane);
+  if (table != nullptr && at.g == 0 && lane == 0) table[at.i] = at.i;
+}
+
+// The link write: every private block takes what its source block holds, then the rows of S,
+// rounded to 8 bits, in their slots.  A slot that neither fills holds a row of zeros.
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv8_write_kernel(Kv8Rows w, epic_kv8_cache c, int hkv) {
+  __shared__ uint32_t turn[kWaves][kTurnInts<D / 64>];
+  const Place at(hkv, blockIdx.x);
+  if (at.g < hkv) kv8_write_private<D>(w, c, at.i, hkv, at.g, threadIdx.x & 63, turn[threadIdx.x >> 6]);
+}
+
+// The same for plans whose cached keys move: K of a block with priv_rot = off != 0 is turned by off
+// (R(off) R(t) = R(off + t)): pairs (i, i + D / 2), angle off * theta^(-2 i / D) in float64, from its
+// 8-bit values in fp32 to 8 bits again, with a scale of its own.
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv8_write_rotate_kernel(Kv8Rows w, const int32_t* __restrict__ priv_rot,
+                                                                    epic_kv8_cache c, int hkv, double log2_theta) {
   constexpr int J = D / 64;
   __shared__ uint32_t turn[kWaves][kTurnInts<J>];
-  __shared__ float2 cs[ROTATE ? D / 2 : 1];
-  const Place at(hkv);
+  __shared__ float2 cs[D / 2];
+  const Place at(hkv, blockIdx.x);
   const int g = min(at.g, hkv - 1);            // all wavefronts meet at the barrier
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, a = lane >> 4;
-  const int dst = priv_block[at.i], src = priv_src[at.i];
-  const int rot = ROTATE && src >= 0 ? priv_rot[at.i] : 0;
+  const int lane = threadIdx.x & 63, a = lane >> 4;
+  const int dst = w.block[at.i], src = w.src[at.i];
+  const int rot = src >= 0 ? priv_rot[at.i] : 0;
   uint4 kq[J], vq[J];
   int kb;
   uint32_t vs;
-  kv8_load_block<D>(c, src == dst ? -1 : src, hkv, g, lane, kq, vq, kb, vs);
-  if constexpr (ROTATE) {
-    if (rot != 0) {                            // one block per workgroup: all of its wavefronts or none
-      if (threadIdx.x < D / 2) {
-        double sn, cn;
-        sincos(double(rot) * exp2(-double(2 * int(threadIdx.x)) / double(D) * log2_theta), &sn, &cn);
-        cs[threadIdx.x] = make_float2(float(cn), float(sn));
-      }
-      __syncthreads();
-      float f[16 * J];
+  const int row = w.rows[at.i * 16 + (lane & 15)];
+  kv8_load_block<D>(c, size_t(max(src, 0)) * hkv + g, lane, kq, vq, kb, vs);
+  if (rot != 0) {                            // one block per workgroup: all of its wavefronts or none
+    if (threadIdx.x < D / 2) {
+      double sn, cn;
+      sincos(double(rot) * exp2(-double(2 * int(threadIdx.x)) / double(D) * log2_theta), &sn, &cn);
+      cs[threadIdx.x] = make_float2(float(cn), float(sn));
+    }
+    __syncthreads();
+    float f[16 * J];
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const uint32_t w[4] = {kq[j].x, kq[j].y, kq[j].z, kq[j].w};
+    for (int j = 0; j < J; ++j) {
+      const uint32_t w[4] = {kq[j].x, kq[j].y, kq[j].z, kq[j].w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          f[16 * j + 4 * i] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 0);
-          f[16 * j + 4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 1);
-          f[16 * j + 4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 2);
-          f[16 * j + 4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 3);
-        }
-      }
-      // the values over their scale: turning commutes with it, and nothing overflows
-      uint32_t top = 0;
-      float z[16 * J];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        if constexpr (J == 2) {                // dims 16 a + e and 64 more
-          const float2 t = cs[16 * a + e];
-          z[e] = f[e] * t.x - f[16 + e] * t.y;
-          z[16 + e] = f[16 + e] * t.x + f[e] * t.y;
-          top = max(top, max(finite_abs(z[e]), finite_abs(z[16 + e])));
-        } else {                               // the partner is 32 dims, 32 lanes away
-          const float2 t = cs[16 * (a & 1) + e];
-          const float o = __shfl_xor(f[e], 32);
-          z[e] = a < 2 ? f[e] * t.x - o * t.y : f[e] * t.x + o * t.y;
-          top = max(top, finite_abs(z[e]));
-        }
-      }
-      top = max(top, uint32_t(__shfl_xor(int(top), 16)));
-      top = max(top, uint32_t(__shfl_xor(int(top), 32)));
-      if (kb != kKv8Nan) {
-        // z is over 2^(kb - 127), and so is its scale; rows of bf16 leave bytes far below 254
-        const int byte = top == 0 ? 127 : min(max(scale_byte(top) + kb - 127, 0), kKv8Nan - 1), t = byte - kb + 127;
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-          kq[j] = make_uint4(pack_e4m3x4(z[16 * j], z[16 * j + 1], z[16 * j + 2], z[16 * j + 3], t),
-                             pack_e4m3x4(z[16 * j + 4], z[16 * j + 5], z[16 * j + 6], z[16 * j + 7], t),
-                             pack_e4m3x4(z[16 * j + 8], z[16 * j + 9], z[16 * j + 10], z[16 * j + 11], t),
-                             pack_e4m3x4(z[16 * j + 12], z[16 * j + 13], z[16 * j + 14], z[16 * j + 15], t));
-        kb = byte;
+      for (int i = 0; i < 4; ++i) {
+        f[16 * j + 4 * i] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 0);
+        f[16 * j + 4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 1);
+        f[16 * j + 4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 2);
+        f[16 * j + 4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8(int(w[i]), 3);
       }
     }
+    // the values over their scale: turning commutes with it, and nothing overflows
+    uint32_t top = 0;
+    float z[16 * J];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      if constexpr (J == 2) {                // dims 16 a + e and 64 more
+        const float2 t = cs[16 * a + e];
+        z[e] = f[e] * t.x - f[16 + e] * t.y;
+        z[16 + e] = f[16 + e] * t.x + f[e] * t.y;
+        top = max(top, max(finite_abs(z[e]), finite_abs(z[16 + e])));
+      } else {                               // the partner is 32 dims, 32 lanes away
+        const float2 t = cs[16 * (a & 1) + e];
+        const float o = __shfl_xor(f[e], 32);
+        z[e] = a < 2 ? f[e] * t.x - o * t.y : f[e] * t.x + o * t.y;
+        top = max(top, finite_abs(z[e]));
+      }
+    }
+    top = max(top, uint32_t(__shfl_xor(int(top), 16)));
+    top = max(top, uint32_t(__shfl_xor(int(top), 32)));
+    if (kb != kKv8Nan) {
+      // z is over 2^(kb - 127), and so is its scale; rows of bf16 leave bytes far below 254
+      const int byte = top == 0 ? 127 : min(max(scale_byte(top) + kb - 127, 0), kKv8Nan - 1), t = byte - kb + 127;
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        kq[j] = make_uint4(pack_e4m3x4(z[16 * j], z[16 * j + 1], z[16 * j + 2], z[16 * j + 3], t),
+                           pack_e4m3x4(z[16 * j + 4], z[16 * j + 5], z[16 * j + 6], z[16 * j + 7], t),
+                           pack_e4m3x4(z[16 * j + 8], z[16 * j + 9], z[16 * j + 10], z[16 * j + 11], t),
+                           pack_e4m3x4(z[16 * j + 12], z[16 * j + 13], z[16 * j + 14], z[16 * j + 15], t));
+      kb = byte;
+    }
   }
-  const Kv8Fresh<J> f = kv8_fresh<D>(priv_rows + at.i * 16, k_s, v_s, hkv, g, lane, turn[wave]);
-  if (at.g >= hkv) return;
-  const size_t to = size_t(dst) * hkv + g;
-  if (src == dst) kv8_store_fresh<D>(f, c, to, lane);
-  else kv8_store_block<D>(f, kq, vq, kb, vs, c, to, lane);
+  const Kv8Fresh<J> f = kv8_fresh<D>(row, w.k_s, w.v_s, hkv, g, lane, turn[threadIdx.x >> 6]);
+  if (src < 0) kv8_no_block<D>(kq, vq, kb, vs);
+  kv8_merge<D>(f, kq, vq, kb, vs, lane);
+  if (at.g < hkv) kv8_store_block<D>(kq, vq, kb, vs, c, size_t(dst) * hkv + g, lane);
 }
 
 unsigned grid_of(int n, int hkv) { return unsigned(kv8_groups(n, hkv)); }
@@ -244,30 +266,30 @@ void launch_kv8_pack(const Kv8Move& mv, int head_dim, const uint16_t* k, const u
 
 void launch_kv8_unpack(const Kv8Move& mv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
                        hipStream_t stream) {
-  auto go = [&](auto kernel) { kernel<<<grid_of(mv.n, mv.hkv), kThreads, 0, stream>>>(mv, c, k, v, nullptr); };
-  if (head_dim == 128) go(kv8_unpack_kernel<128, false>);
-  else go(kv8_unpack_kernel<64, false>);
+  auto go = [&](auto kernel) { kernel<<<grid_of(mv.n, mv.hkv), kThreads, 0, stream>>>(mv, c, k, v); };
+  if (head_dim == 128) go(kv8_unpack_kernel<128>);
+  else go(kv8_unpack_kernel<64>);
 }
 
-void launch_kv8_expand(const int32_t* linked_blocks, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k,
-                       uint16_t* v, int32_t* table, hipStream_t stream) {
-  Kv8Move mv{};
-  mv.src = linked_blocks, mv.n = n, mv.hkv = hkv;
-  auto go = [&](auto kernel) { kernel<<<grid_of(n, hkv), kThreads, 0, stream>>>(mv, c, k, v, table); };
-  if (head_dim == 128) go(kv8_unpack_kernel<128, true>);
-  else go(kv8_unpack_kernel<64, true>);
+void launch_kv8_expand(const int32_t* list, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
+                       int32_t* table, hipStream_t stream) {
+  auto go = [&](auto kernel) { kernel<<<grid_of(n, hkv), kThreads, 0, stream>>>(list, c, hkv, k, v, table); };
+  if (head_dim == 128) go(kv8_expand_kernel<128>);
+  else go(kv8_expand_kernel<64>);
 }
 
-void launch_kv8_write(const epic_plan* plan, int n_private, bool rotated, int hkv, int head_dim, float rope_theta,
-                      const uint16_t* k_s, const uint16_t* v_s, const epic_kv8_cache& c, hipStream_t stream) {
-  if (n_private == 0) return;
-  const double l2t = rotated ? std::log2(double(rope_theta)) : 0.0;
-  auto go = [&](auto kernel) {
-    kernel<<<grid_of(n_private, hkv), kThreads, 0, stream>>>(plan->priv_block, plan->priv_src, plan->priv_rows, plan->priv_rot,
-                                                             k_s, v_s, c, hkv, l2t);
-  };
-  if (rotated) head_dim == 128 ? go(kv8_write_kernel<128, true>) : go(kv8_write_kernel<64, true>);
-  else head_dim == 128 ? go(kv8_write_kernel<128, false>) : go(kv8_write_kernel<64, false>);
+void launch_kv8_write(const Kv8Rows& w, const int32_t* priv_rot, int hkv, int head_dim, float rope_theta,
+                      const epic_kv8_cache& c, hipStream_t stream) {
+  if (w.n == 0) return;
+  const dim3 grid(grid_of(w.n, hkv));
+  if (priv_rot != nullptr) {
+    const double l2t = std::log2(double(rope_theta));
+    if (head_dim == 128) kv8_write_rotate_kernel<128><<<grid, kThreads, 0, stream>>>(w, priv_rot, c, hkv, l2t);
+    else kv8_write_rotate_kernel<64><<<grid, kThreads, 0, stream>>>(w, priv_rot, c, hkv, l2t);
+  } else {
+    if (head_dim == 128) kv8_write_kernel<128><<<grid, kThreads, 0, stream>>>(w, c, hkv);
+    else kv8_write_kernel<64><<<grid, kThreads, 0, stream>>>(w, c, hkv);
+  }
 }
 
 }  // namespace epic

@@ -51,20 +51,6 @@ struct Kv8Block {
   uint32_t ks, vs;                            // scales of keys 4 a ..
 };
 
-template <int D>
-__device__ __forceinline__ void write_private(const Kv8Rows& w, const epic_kv8_cache& c, int i, int hkv, int g, int lane,
-                                              uint32_t* turn) {
-  const int dst = w.block[i], src = w.src[i];
-  uint4 kq[D / 64], vq[D / 64];
-  int kb;
-  uint32_t vs;
-  kv8_load_block<D>(c, src == dst ? -1 : src, hkv, g, lane, kq, vq, kb, vs);
-  const Kv8Fresh<D / 64> f = kv8_fresh<D>(w.rows + i * 16, w.k_s, w.v_s, hkv, g, lane, turn);
-  const size_t to = size_t(dst) * hkv + g;
-  if (src == dst) kv8_store_fresh<D>(f, c, to, lane);
-  else kv8_store_block<D>(f, kq, vq, kb, vs, c, to, lane);
-}
-
 // NT: K and V are read past the caches, which hold nothing of them that is read again.
 template <int D, int W, int RING, bool NT>
 __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(AttnArgs a, epic_kv8_cache c, Kv8Rows w) {
@@ -77,7 +63,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(Attn
     const int ng = (hkv + W - 1) / W, i = blockIdx.x / ng, g = (blockIdx.x % ng) * W + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (g >= hkv) return;
-    write_private<D>(w, c, i, hkv, g, lane, reinterpret_cast<uint32_t*>(lds.o[threadIdx.x >> 6]));
+    kv8_write_private<D>(w, c, i, hkv, g, lane, reinterpret_cast<uint32_t*>(lds.o[threadIdx.x >> 6]));
     return;
   }
   const int g = (blockIdx.x - w.groups) % hkv;
@@ -295,7 +281,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(Attn
           const int i = __builtin_ctzll(left), q = __builtin_amdgcn_readlane(priv_l, i);
           left &= left - 1;
           const Kv8Fresh<J> f =
-              kv8_fresh<D>(w.rows + q * 16, w.k_s, w.v_s, hkv, g, lane, reinterpret_cast<uint32_t*>(lds.o[wave]));
+              kv8_fresh<D>(w.rows[q * 16 + r], w.k_s, w.v_s, hkv, g, lane, reinterpret_cast<uint32_t*>(lds.o[wave]));
           Kv8Block<J> x;
 #pragma unroll
           for (int j = 0; j < J; ++j) x.k[j] = f.k[j], x.v[j] = f.v[j];

@@ -46,10 +46,12 @@ __device__ __forceinline__ int kv8_byte(uint32_t top16) {
   return top16 >= 0x7F80u ? kKv8Nan : scale_byte(top16 << 16);
 }
 
-// Two bf16 pairs over 2^(byte - 127) as four e4m3, for finite values.
+// Two bf16 pairs over 2^(byte - 127) as four e4m3, for finite values: the conversion divides by a power of two itself.
 __device__ __forceinline__ uint32_t round4(uint32_t lo, uint32_t hi, int byte) {
-  return pack_e4m3x4(__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u), __uint_as_float(hi << 16),
-                     __uint_as_float(hi & 0xFFFF0000u), byte);
+  typedef short i16x2 __attribute__((ext_vector_type(2)));
+  const float s = __uint_as_float(uint32_t(byte) << 23);
+  const i16x2 r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(i16x2{0, 0}, __builtin_bit_cast(bf16x2r, lo), s, false);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2r, hi), s, true));
 }
 
 // Rows in the K arrangement: x[2 j], x[2 j + 1] are the 16 bf16 of dims 64 j + 16 a .. of token r.
@@ -81,24 +83,30 @@ constexpr int kTurnLd = 68;                   // bytes of a token's 64 dims in L
 template <int J>
 constexpr int kTurnInts = J * 16 * kTurnLd / 4;
 
-// V rows come like K's, 16 dims of a token a lane; their e4m3 bytes change places through `turn`, LDS of this
+// row: of token r, or -1.  V rows come like K's, 16 dims of a token a lane; their e4m3 bytes change places through `turn`, LDS of this
 // wavefront alone.
 template <int D>
-__device__ __forceinline__ Kv8Fresh<D / 64> kv8_fresh(const int32_t* rows, const uint16_t* k_s, const uint16_t* v_s, int hkv,
-                                                      int g, int lane, uint32_t* turn) {
+__device__ __forceinline__ Kv8Fresh<D / 64> kv8_fresh(int row, const uint16_t* k_s, const uint16_t* v_s, int hkv, int g,
+                                                      int lane, uint32_t* turn) {
   constexpr int J = D / 64;
   const int r = lane & 15, a = lane >> 4;
-  const int row = rows[r];
   Kv8Fresh<J> f;
   f.tokens = uint32_t(__ballot(row >= 0)) & 0xFFFFu;
   uint4 x[2 * J], y[2 * J];
 #pragma unroll
-  for (int i = 0; i < 2 * J; ++i) {
-    x[i] = y[i] = make_uint4(0, 0, 0, 0);
-    if (row >= 0) {
-      const size_t from = (size_t(row) * hkv + g) * D + 64 * (i >> 1) + 16 * a + 8 * (i & 1);
-      x[i] = *reinterpret_cast<const uint4*>(k_s + from);
-      y[i] = *reinterpret_cast<const uint4*>(v_s + from);
+  for (int i = 0; i < 2 * J; ++i) x[i] = y[i] = make_uint4(0, 0, 0, 0);
+  if (f.tokens != 0) {
+    const size_t from = (size_t(max(row, 0)) * hkv + g) * D + 16 * a;
+#pragma unroll
+    for (int i = 0; i < 2 * J; ++i) {
+      x[i] = *reinterpret_cast<const uint4*>(k_s + from + 64 * (i >> 1) + 8 * (i & 1));
+      y[i] = *reinterpret_cast<const uint4*>(v_s + from + 64 * (i >> 1) + 8 * (i & 1));
+    }
+    const uint32_t keep = row >= 0 ? 0xFFFFFFFFu : 0u;
+#pragma unroll
+    for (int i = 0; i < 2 * J; ++i) {
+      x[i] = make_uint4(x[i].x & keep, x[i].y & keep, x[i].z & keep, x[i].w & keep);
+      y[i] = make_uint4(y[i].x & keep, y[i].y & keep, y[i].z & keep, y[i].w & keep);
     }
   }
   int kb = kv8_byte(row_top<J>(x)), vb = kv8_byte(row_top<J>(y));
@@ -175,45 +183,78 @@ __device__ __forceinline__ void kv8_store_fresh(const Kv8Fresh<D / 64>& f, const
   }
 }
 
-// The link write of one (private block, KV head) by one wavefront: what the source block holds (kq, vq, kb of token r and
-// vs of tokens 4 a ..; zero rows without one), then the rows of S.
+// The rows of S over what their block's source holds (kb: of token r, vs: of tokens 4 a ..).
 template <int D>
-__device__ __forceinline__ void kv8_store_block(const Kv8Fresh<D / 64>& f, uint4 (&kq)[D / 64], uint4 (&vq)[D / 64], int kb,
-                                                uint32_t vs, const epic_kv8_cache& c, size_t block_head, int lane) {
-  constexpr int J = D / 64;
-  const int r = lane & 15, a = lane >> 4;
-  const bool fresh = f.tokens >> r & 1;
-  const uint32_t mask = byte_mask(f.tokens >> (4 * a) & 15u);
+__device__ __forceinline__ void kv8_merge(const Kv8Fresh<D / 64>& f, uint4 (&kq)[D / 64], uint4 (&vq)[D / 64], int& kb,
+                                          uint32_t& vs, int lane) {
+  const bool fresh = f.tokens >> (lane & 15) & 1;
+  const uint32_t mask = byte_mask(f.tokens >> (4 * (lane >> 4)) & 15u);
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    kq[j] = fresh ? f.k[j] : kq[j];
+    vq[j] = merge(vq[j], f.v[j], mask);
+  }
+  kb = fresh ? f.kb : kb;
+  vs = (vs & ~mask) | (f.vs & mask);
+}
+
+// A whole block.
+template <int D>
+__device__ __forceinline__ void kv8_store_block(const uint4 (&kq)[D / 64], const uint4 (&vq)[D / 64], int kb, uint32_t vs,
+                                                const epic_kv8_cache& c, size_t block_head, int lane) {
   const size_t to = block_head * 16 * D;
   uint8_t* s = c.scale + block_head * kKv8Scales;
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    *reinterpret_cast<uint4*>(c.k + to + 1024 * j + 16 * lane) = fresh ? f.k[j] : kq[j];
-    *reinterpret_cast<uint4*>(c.v + to + 1024 * j + 16 * lane) = merge(vq[j], f.v[j], mask);
+  for (int j = 0; j < D / 64; ++j) {
+    *reinterpret_cast<uint4*>(c.k + to + 1024 * j + 16 * lane) = kq[j];
+    *reinterpret_cast<uint4*>(c.v + to + 1024 * j + 16 * lane) = vq[j];
   }
-  if (lane < 16) s[lane] = uint8_t(fresh ? f.kb : kb);
-  if (r == 0) *reinterpret_cast<uint32_t*>(s + 16 + 4 * a) = (vs & ~mask) | (f.vs & mask);
+  if (lane < 16) s[lane] = uint8_t(kb);
+  if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(s + 16 + 4 * (lane >> 4)) = vs;
 }
 
-// What a wavefront reads of a source block; rows of zeros where there is none.
+// What a wavefront reads of a block.
 template <int D>
-__device__ __forceinline__ void kv8_load_block(const epic_kv8_cache& c, int src, int hkv, int g, int lane, uint4 (&kq)[D / 64],
+__device__ __forceinline__ void kv8_load_block(const epic_kv8_cache& c, size_t block_head, int lane, uint4 (&kq)[D / 64],
                                                uint4 (&vq)[D / 64], int& kb, uint32_t& vs) {
-  constexpr int J = D / 64;
+  const uint8_t* s = c.scale + block_head * kKv8Scales;
+  kb = s[lane & 15];
+  vs = *reinterpret_cast<const uint32_t*>(s + 16 + 4 * (lane >> 4));
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    kq[j] = *reinterpret_cast<const uint4*>(c.k + block_head * 16 * D + 1024 * j + 16 * lane);
+    vq[j] = *reinterpret_cast<const uint4*>(c.v + block_head * 16 * D + 1024 * j + 16 * lane);
+  }
+}
+
+// Rows of zeros.
+template <int D>
+__device__ __forceinline__ void kv8_no_block(uint4 (&kq)[D / 64], uint4 (&vq)[D / 64], int& kb, uint32_t& vs) {
   kb = 127;
   vs = 0x7F7F7F7Fu;
 #pragma unroll
-  for (int j = 0; j < J; ++j) kq[j] = vq[j] = make_uint4(0, 0, 0, 0);
-  if (src < 0) return;
-  const size_t from = size_t(src) * hkv + g;
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    kq[j] = *reinterpret_cast<const uint4*>(c.k + from * 16 * D + 1024 * j + 16 * lane);
-    vq[j] = *reinterpret_cast<const uint4*>(c.v + from * 16 * D + 1024 * j + 16 * lane);
+  for (int j = 0; j < D / 64; ++j) kq[j] = vq[j] = make_uint4(0, 0, 0, 0);
+}
+
+// The link write of one (private block i, KV head) by one wavefront: what its source block holds, zero rows without
+// one, then its rows of S.  A block that is its own source only receives its rows.
+template <int D>
+__device__ __forceinline__ void kv8_write_private(const Kv8Rows& w, const epic_kv8_cache& c, int i, int hkv, int g, int lane,
+                                                  uint32_t* turn) {
+  const int dst = w.block[i], src = w.src[i], row = w.rows[i * 16 + (lane & 15)];
+  uint4 kq[D / 64], vq[D / 64];
+  int kb;
+  uint32_t vs;
+  kv8_load_block<D>(c, size_t(max(src, 0)) * hkv + g, lane, kq, vq, kb, vs);
+  const Kv8Fresh<D / 64> f = kv8_fresh<D>(row, w.k_s, w.v_s, hkv, g, lane, turn);
+  if (src < 0) kv8_no_block<D>(kq, vq, kb, vs);            // (here: before, it would wait for the loads)
+  const size_t to = size_t(dst) * hkv + g;
+  if (src == dst) {
+    kv8_store_fresh<D>(f, c, to, lane);
+  } else {
+    kv8_merge<D>(f, kq, vq, kb, vs, lane);
+    kv8_store_block<D>(kq, vq, kb, vs, c, to, lane);
   }
-  const uint8_t* s = c.scale + from * kKv8Scales;
-  kb = s[lane & 15];
-  vs = *reinterpret_cast<const uint32_t*>(s + 16 + 4 * (lane >> 4));
 }
 
 }  // namespace epic

@@ -222,7 +222,8 @@ class Requests:
         self.rng = np.random.default_rng([hq, hkv, d, seed, len(picks)])
         self.heads, self.cfg = (hq, hkv, d), el.attn_cfg(hq, hkv, d, scale, split, tile_rows, THETA)
         nb = [-(-n // 16) for n in lens]
-        private = sum(sum(nb[c] for c in r) + -(-s // 16) for r, s in zip(picks, suffix))
+        private = sum(sum(nb[c] if rerotate or k < 0 else min(nb[c], -(-k // 16)) for c in r) + -(-s // 16)
+                      for r, s in zip(picks, suffix))
         self.blocks = sum(nb) + private + spare
         perm = self.rng.permutation(self.blocks)
         first = np.cumsum([0] + nb)
@@ -388,6 +389,49 @@ def test_decode_lengths(length, d):
     assert r.sizes.n_s == 0
     r.decode([1]).run(what=f"length {length}")
     r.decode([1]).run(what=f"length {length} + 1")
+
+
+@pytest.mark.parametrize("k", [17, -1])
+def test_decode_into_a_chunks_last_block(k):
+    """Without a suffix the first new token goes to the copy of a chunk's last block."""
+    r = Requests(8, 2, 64, [[0, 1], [1, 0]], [40, 20], [0, 0], k)
+    r.run(what=f"k {k}")
+    for new in ([1, 2], [0, 1], [20, 1]):
+        r.decode(new).run(what=f"decode {new}")
+
+
+@pytest.mark.parametrize("rerotate", [False, True])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (16, 2, 128)])
+def test_many_private_blocks_in_small_tiles(hq, hkv, d, rerotate):
+    """More private blocks than the attention launch writes itself, and turned ones, in 16-row tiles."""
+    n = 37
+    r = Requests(hq, hkv, d, [[i % 3, (i + 1) % 3] for i in range(n)], [50, 33, 70], [1 + i % 19 for i in range(n)], 5,
+                 rerotate=rerotate, tile_rows=16, spare=2 * n)
+    assert r.sizes.n_private > 64
+    r.run(what="link")
+    r.rerotate = False
+    r.decode([1] * n).run(what="decode")
+
+
+def test_many_requests_decode():
+    """70 requests: more private blocks than one wavefront looks through; then 64 of them."""
+    n = 70
+    r = Requests(8, 2, 64, [[i % 4] for i in range(n)], [20, 33, 17, 64], [1 + i % 17 for i in range(n)], 0, spare=3 * n)
+    r.run(what="link")
+    for new in ([1] * n, [1] * 64 + [0] * 6, [0] * 69 + [1]):
+        r.decode(new)
+        print(f"[gpu-test] private {r.sizes.n_private}", flush=True)
+        r.run(what="decode")
+
+
+@pytest.mark.parametrize("tile_rows", [128, 256])
+def test_wide_tiles_over_shared_chunks(tile_rows):
+    """Requests that link more blocks than the pool has: the pool is widened, not the list."""
+    n = 9
+    r = Requests(8, 2, 128, [[0, 1, 2], [2, 1, 0], [1, 2, 0]] * 3, [200, 133, 170], [3] * n, 2, tile_rows=tile_rows, spare=4)
+    assert r.sizes.n_linked_blocks > r.blocks
+    spoil = [4, int(r.views["s_off"][2]) + 1]
+    r.run(r.draw(spoil), what="shared")
 
 
 def test_requests_without_chunks():
