@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "attention_call.h"
 #include "decode_attention.h"
 #include "kernels.h"
 #include "link_write.h"

@@ -4,6 +4,7 @@
 
 #include <cstdint>
 
+#include "attention_call.h"
 #include "kv8.h"
 #include "plan_internal.h"
 #include "status.h"

@@ -299,10 +299,12 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(Attn
       for (int j = 0; j < RING; ++j) {
         const int p = base + j;
         if (p < n) {
-          // what this slot holds next; past the batch's end its last pair again, so that the same loads
-          // are in flight behind every wait
+          // what this slot holds next; past the batch's end block 0 of the pool, which every wavefront reads there and
+          // the caches keep, so that the same loads are in flight behind every wait (the last pair again: 7% more bytes)
           const int next = 2 * min(p + RING, n - 1);
-          const int phys0 = __builtin_amdgcn_readlane(phys_l, next), phys1 = __builtin_amdgcn_readlane(phys_l, next + 1);
+          const bool more = p + RING < n;
+          const int phys0 = more ? __builtin_amdgcn_readlane(phys_l, next) : 0;
+          const int phys1 = more ? __builtin_amdgcn_readlane(phys_l, next + 1) : 0;
           auto after_k = [&]() __attribute__((always_inline)) {
             load_k(phys0, ring[j][0]);
             load_k(phys1, ring[j][1]);

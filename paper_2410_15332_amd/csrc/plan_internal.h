@@ -1,10 +1,7 @@
 // Constants and helpers shared by the host sources (planner and entry points).
 #pragma once
 
-#include <hip/hip_runtime.h>
-
 #include "epic_link.h"
-#include "kernels.h"
 
 namespace epic {
 
@@ -31,12 +28,5 @@ epic_status run_link_attention(const epic_attn_cfg* cfg, const epic_plan_sizes* 
                                const uint16_t* q_s, const uint16_t* k_s, const uint16_t* v_s,
                                uint16_t* k_cache, uint16_t* v_cache, uint16_t* out, float* lse,
                                void* workspace, void* stream);
-
-// What the attention entry points ask of their config and plan, and the kernels' arguments for them.
-epic_status check_attention(const epic_attn_cfg* cfg, const epic_plan_sizes* sizes, const epic_plan* plan_dev);
-AttnArgs attention_args(const epic_attn_cfg* cfg, const epic_plan_sizes* s, const epic_plan* p, const uint16_t* q_s,
-                        const uint16_t* k_cache, const uint16_t* v_cache, uint16_t* out, float* lse, void* workspace);
-// The calling thread's profiling event i, if it has one, on `stream`.
-void record_profile_event(int i, hipStream_t stream);
 
 }  // namespace epic

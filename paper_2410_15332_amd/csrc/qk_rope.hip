@@ -10,8 +10,10 @@
 //
 // What bounds it is reading and writing the rows once.  A head is D / 16 lanes of 16 values,
 // two pieces of 8 each: both pieces of a lane's pairs, so a rotation stays in the lane.  A workgroup
-// takes a row in passes of 256 threads, the next pass's loads ahead of this one's work; the row's
-// angles (one per thread) are computed once, into LDS, while the first loads are in flight.
+// takes a row, or several short ones (MANY), in passes of 256 threads, the next pass's loads ahead of this one's
+// work; the angles are computed once, into LDS, while the first loads are in flight.
+#include <type_traits>
+
 #include "device_common.h"
 #include "qk_rope.h"
 
@@ -20,7 +22,7 @@ namespace epic {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxPairs = 64;
+constexpr int kMaxPairs = 64, kMaxRows = 8;
 
 // (cos, sin) of pos * f.
 __device__ __forceinline__ float2 turn_of(int pos, double f) {
@@ -73,25 +75,29 @@ struct Piece<true> {
   }
 };
 
-template <int D, bool F32, bool INTER>
-__global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p) {
+template <int D, bool F32, bool INTER, bool MANY>
+__global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p, int rows_per_group) {
   constexpr int L = D / 16;                   // lanes per head
-  __shared__ float2 cs[kMaxPairs];
-  const int heads = p.hq + 2 * p.hkv, row = blockIdx.x, step = kThreads / L * gridDim.y;
+  __shared__ float2 cs[MANY ? kMaxRows : 1][kMaxPairs];
+  const int heads = p.hq + 2 * p.hkv, half = p.rot / 2, step = kThreads / L * gridDim.y;
+  const int row0 = blockIdx.x * (MANY ? rows_per_group : 1), rows = MANY ? min(rows_per_group, p.rows - row0) : 1;
+  const int total = rows * heads;
   const int l = threadIdx.x % L;
   // this lane's two pieces of 8 dims: the two sides of its pairs (half layout), or neighbours
   const int R = p.rot / 8;                    // rotated pieces, an even number
   const bool turned = l < R / 2;
   const int c0 = INTER || !turned ? 2 * l : l, c1 = INTER || !turned ? 2 * l + 1 : l + R / 2;
 
-  int head = blockIdx.y * (kThreads / L) + threadIdx.x / L;
+  int at = blockIdx.y * (kThreads / L) + threadIdx.x / L;       // (row of the group, head), and the next one's values
   Piece<F32> x[2];
-  auto fetch = [&](int at) __attribute__((always_inline)) {
-    const size_t from = size_t(row) * p.ld + size_t(min(at, heads - 1)) * D;
+  auto fetch = [&](int i) __attribute__((always_inline)) {
+    i = min(i, total - 1);
+    const int row = MANY ? i / heads : 0;
+    const size_t from = size_t(row0 + row) * p.ld + size_t(i - row * heads) * D;
     x[0].load(p.qkv, from + 8 * c0);
     x[1].load(p.qkv, from + 8 * c1);
   };
-  fetch(head);
+  fetch(at);
   uint4 wq[2] = {}, wk[2] = {};
   if (p.q_norm) {
     wq[0] = *reinterpret_cast<const uint4*>(p.q_norm + 8 * c0);
@@ -101,14 +107,16 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p) {
     wk[0] = *reinterpret_cast<const uint4*>(p.k_norm + 8 * c0);
     wk[1] = *reinterpret_cast<const uint4*>(p.k_norm + 8 * c1);
   }
-  if (int(threadIdx.x) < p.rot / 2) {
-    const float2 t = turn_of(p.pos[row], p.freqs[threadIdx.x]);
-    cs[threadIdx.x] = make_float2(p.amplitude * t.x, p.amplitude * t.y);
+  for (int i = threadIdx.x; i < rows * half; i += kThreads) {
+    const int row = MANY ? i / half : 0;
+    const float2 t = turn_of(p.pos[row0 + row], p.freqs[i - row * half]);
+    cs[row][i - row * half] = make_float2(p.amplitude * t.x, p.amplitude * t.y);
   }
   __syncthreads();
-  for (;; head += step) {
+  for (;; at += step) {
     const Piece<F32> y0 = x[0], y1 = x[1];
-    if (head + step < heads) fetch(head + step);
+    if (at + step < total) fetch(at + step);
+    const int row = MANY ? at / heads : 0, head = at - row * heads;
     const bool is_q = head < p.hq, is_v = head >= p.hq + p.hkv;
     float u[8], v[8];
     y0.get(u);
@@ -118,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p) {
     for (int i = 0; i < 8; ++i) ss += u[i] * u[i] + v[i] * v[i];
 #pragma unroll
     for (int off = L / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
-    if (head >= heads) break;                 // after the exchange: all lanes of a head together
+    if (at >= total) break;                   // after the exchange: all lanes of a head together
     uint4 r0 = y0.bf16(), r1 = y1.bf16();
     if (!is_v) {
       if ((is_q ? p.q_norm : p.k_norm) != nullptr) {
@@ -137,12 +145,12 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p) {
         for (int i = 0; i < 8; ++i) {
           if constexpr (INTER) {              // pairs 8 l + i: u holds four of them, then v
             float* e = i < 4 ? u + 2 * i : v + 2 * (i - 4);
-            const float2 k = cs[8 * l + i];
+            const float2 k = cs[row][8 * l + i];
             const float a = e[0], b = e[1];
             e[0] = a * k.x - b * k.y;
             e[1] = b * k.x + a * k.y;
           } else {
-            const float2 k = cs[8 * l + i];
+            const float2 k = cs[row][8 * l + i];
             const float a = u[i], b = v[i];
             u[i] = a * k.x - b * k.y;
             v[i] = b * k.x + a * k.y;
@@ -152,9 +160,9 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p) {
       r0 = pack8(u);
       r1 = pack8(v);
     }
-    const size_t at = row;
-    uint16_t* to = is_q ? p.q + (at * p.hq + head) * D
-                        : is_v ? p.v + (at * p.hkv + (head - p.hq - p.hkv)) * D : p.k + (at * p.hkv + (head - p.hq)) * D;
+    const size_t r = row0 + row;
+    uint16_t* to = is_q ? p.q + (r * p.hq + head) * D
+                        : is_v ? p.v + (r * p.hkv + (head - p.hq - p.hkv)) * D : p.k + (r * p.hkv + (head - p.hq)) * D;
     *reinterpret_cast<uint4*>(to + 8 * c0) = r0;
     *reinterpret_cast<uint4*>(to + 8 * c1) = r1;
   }
@@ -163,19 +171,28 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkRopeArgs p) {
 }  // namespace
 
 void launch_qk_rope(const QkRopeArgs& p, int head_dim, bool fp32, bool interleaved, hipStream_t stream) {
-  // Passes of 32 heads (64 of 64 dims) over a row; each a workgroup of its own where rows are fewer
-  // than CUs.  32 + 8 + 8 heads of 128: 1 row 2.8 us (3.5 undivided), 736 rows of fp32 7.5 (8.4 divided), 20 560 rows
-  // 85 (505 MB, 5.9 TB/s; 96 to 99 divided, with 4 rows a workgroup, or in one pass of 384 threads).
-  const int per_pass = kThreads / (head_dim / 16);
-  const int passes = p.rows < 256 ? (p.hq + 2 * p.hkv + per_pass - 1) / per_pass : 1;
-  auto go = [&](auto kernel) { kernel<<<dim3(p.rows, passes), kThreads, 0, stream>>>(p); };
-  if (head_dim == 128) {
-    if (fp32) interleaved ? go(qk_rope_kernel<128, true, true>) : go(qk_rope_kernel<128, true, false>);
-    else interleaved ? go(qk_rope_kernel<128, false, true>) : go(qk_rope_kernel<128, false, false>);
-  } else {
-    if (fp32) interleaved ? go(qk_rope_kernel<64, true, true>) : go(qk_rope_kernel<64, true, false>);
-    else interleaved ? go(qk_rope_kernel<64, false, true>) : go(qk_rope_kernel<64, false, false>);
-  }
+  // A pass takes 32 heads (64 of 64 dims).  Rows fewer than CUs: a workgroup for each pass over a row (1 row of 32 + 8 + 8
+  // heads of 128: 2.8 us, 3.5 undivided).  Else a row a workgroup: 736 rows of fp32 7.3 us, 20 560 rows 87 (505 MB, 5.8
+  // TB/s; 92 to 99 with more rows, divided, or in one pass of more threads).  Rows that are less than a pass go
+  // several to a workgroup, to two passes, where these are as many as CUs: 16 + 1 + 1 heads of 64, 900 rows 3.8 us (4.2 if
+  // they did), 2000 rows 5.0 (5.4 by rows), 20 560 rows 20 (33 by rows, 22 to one pass).
+  const int heads = p.hq + 2 * p.hkv, per_pass = kThreads / (head_dim / 16);
+  const bool few = p.rows < 256;
+  const int most = heads >= per_pass ? 1 : min(kMaxRows, 2 * per_pass / heads), rows = p.rows >= 256 * most ? most : 1;
+  const dim3 grid((p.rows + rows - 1) / rows, few ? (heads + per_pass - 1) / per_pass : 1);
+  auto go = [&](auto one, auto many) {
+    if (rows == 1) one<<<grid, kThreads, 0, stream>>>(p, 1);
+    else many<<<grid, kThreads, 0, stream>>>(p, rows);
+  };
+  auto pairs = [&](auto d, auto f32) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool F32 = decltype(f32)::value;
+    if (interleaved) go(qk_rope_kernel<D, F32, true, false>, qk_rope_kernel<D, F32, true, true>);
+    else go(qk_rope_kernel<D, F32, false, false>, qk_rope_kernel<D, F32, false, true>);
+  };
+  auto type = [&](auto d) { fp32 ? pairs(d, std::true_type{}) : pairs(d, std::false_type{}); };
+  if (head_dim == 128) type(std::integral_constant<int, 128>{});
+  else type(std::integral_constant<int, 64>{});
 }
 
 }  // namespace epic

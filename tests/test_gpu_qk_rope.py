@@ -96,6 +96,13 @@ def test_heads_and_rows(n, hq, hkv, d):
     _case(n, hq, hkv, d, d, torch.bfloat16)
 
 
+@pytest.mark.parametrize("hq,hkv,d,rot", [(8, 8, 64, 64), (16, 1, 64, 48), (8, 1, 128, 128), (1, 1, 64, 16), (6, 3, 128, 96)])
+@pytest.mark.parametrize("dtype,interleaved", [(torch.bfloat16, False), (torch.float32, True)])
+def test_short_rows(hq, hkv, d, rot, dtype, interleaved):
+    """Rows of few heads, several to a workgroup, the last workgroup with fewer."""
+    _case(2051, hq, hkv, d, rot, dtype, interleaved)
+
+
 @pytest.mark.parametrize("norms", ["", "q", "k", "qk"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_norms_of_either(norms, dtype):
