@@ -14,7 +14,7 @@ namespace epic {
 constexpr int kKv8Scales = 32;
 constexpr int kKv8Nan = 255;                  // scale byte of a token whose K or V is not finite
 
-// Launches stay below 2^31 workgroups of 4 (block, KV head) pairs.
+// Workgroups of four KV heads of a block each.
 inline int64_t kv8_groups(int64_t n, int hkv) { return n * ((hkv + 3) / 4); }
 constexpr int64_t kKv8MaxGroups = (int64_t(1) << 24) - 1;        // x 256 threads < 2^32
 

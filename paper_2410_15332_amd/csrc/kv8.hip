@@ -19,16 +19,18 @@ namespace epic {
 
 namespace {
 
-constexpr int kWaves = 4;                     // KV heads per workgroup
+constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 
-// The (list entry, KV head) of this wavefront.
+// The (list entry, KV head) of this wavefront: pairs in order, so few heads fill workgroups too.
 struct Place {
   int i, g;
-  __device__ __forceinline__ Place(int hkv, int group) {
-    const int ng = (hkv + kWaves - 1) / kWaves;
-    i = group / ng;
-    g = (group % ng) * kWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  bool in;
+  __device__ __forceinline__ Place(int n, int hkv) {
+    const int pair = int(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    i = pair / hkv;
+    g = pair - i * hkv;
+    in = i < n;
   }
 };
 
@@ -45,8 +47,8 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const uint16_t* __restrict__ k,
                                                             const uint16_t* __restrict__ v, epic_kv8_cache c) {
   constexpr int J = D / 64;
-  const Place at(mv.hkv, blockIdx.x);
-  if (at.g >= mv.hkv) return;
+  const Place at(mv.n, mv.hkv);
+  if (!at.in) return;
   const int src = mv.src ? mv.src[at.i] : at.i, dst = mv.dst ? mv.dst[at.i] : at.i;
   if (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks)) return;
   const int lane = threadIdx.x & 63, r = lane & 15, a = lane >> 4;
@@ -138,8 +140,8 @@ __device__ __forceinline__ void store_wide(const uint4 (&x)[D / 64], const uint4
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_kv8_cache c, uint16_t* __restrict__ k,
                                                               uint16_t* __restrict__ v) {
-  const Place at(mv.hkv, blockIdx.x);
-  if (at.g >= mv.hkv) return;
+  const Place at(mv.n, mv.hkv);
+  if (!at.in) return;
   const int src = mv.src ? mv.src[at.i] : at.i, dst = mv.dst ? mv.dst[at.i] : at.i;
   if (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks)) return;
   const int lane = threadIdx.x & 63;
@@ -155,11 +157,11 @@ __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_k
 // 137 us, 5.9 TB/s.  (Forming private blocks here too, as decode does, saves the write's launch, 4 us, and costs
 // as much of 324 blocks and 20 us of 8208.)
 template <int D>
-__global__ __launch_bounds__(kThreads) void kv8_expand_kernel(const int32_t* __restrict__ list, epic_kv8_cache c, int hkv,
-                                                              uint16_t* __restrict__ k, uint16_t* __restrict__ v,
+__global__ __launch_bounds__(kThreads) void kv8_expand_kernel(const int32_t* __restrict__ list, int n, epic_kv8_cache c,
+                                                              int hkv, uint16_t* __restrict__ k, uint16_t* __restrict__ v,
                                                               int32_t* __restrict__ table) {
-  const Place at(hkv, blockIdx.x);
-  if (at.g >= hkv) return;
+  const Place at(n, hkv);
+  if (!at.in) return;
   const int lane = threadIdx.x & 63, phys = list ? list[at.i] : at.i;
   uint4 x[D / 64], y[D / 64];
   int kb;
@@ -174,8 +176,8 @@ __global__ __launch_bounds__(kThreads) void kv8_expand_kernel(const int32_t* __r
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_write_kernel(Kv8Rows w, epic_kv8_cache c, int hkv) {
   __shared__ uint32_t turn[kWaves][kTurnInts<D / 64>];
-  const Place at(hkv, blockIdx.x);
-  if (at.g < hkv) kv8_write_private<D>(w, c, at.i, hkv, at.g, threadIdx.x & 63, turn[threadIdx.x >> 6]);
+  const Place at(w.n, hkv);
+  if (at.in) kv8_write_private<D>(w, c, at.i, hkv, at.g, threadIdx.x & 63, turn[threadIdx.x >> 6]);
 }
 
 // The same for plans whose cached keys move: K of a block with priv_rot = off != 0 is turned by off
@@ -187,15 +189,17 @@ __global__ __launch_bounds__(kThreads) void kv8_write_rotate_kernel(Kv8Rows w, c
   constexpr int J = D / 64;
   __shared__ uint32_t turn[kWaves][kTurnInts<J>];
   __shared__ float2 cs[D / 2];
-  const Place at(hkv, blockIdx.x);
-  const int g = min(at.g, hkv - 1);            // all wavefronts meet at the barrier
+  // a block's heads four by four: its wavefronts share the angles, and all meet at the barrier
+  const int groups = (hkv + kWaves - 1) / kWaves, i = int(blockIdx.x) / groups;
+  const int head = (int(blockIdx.x) % groups) * kWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int g = min(head, hkv - 1);
   const int lane = threadIdx.x & 63, a = lane >> 4;
-  const int dst = w.block[at.i], src = w.src[at.i];
-  const int rot = src >= 0 ? priv_rot[at.i] : 0;
+  const int dst = w.block[i], src = w.src[i];
+  const int rot = src >= 0 ? priv_rot[i] : 0;
   uint4 kq[J], vq[J];
   int kb;
   uint32_t vs;
-  const int row = w.rows[at.i * 16 + (lane & 15)];
+  const int row = w.rows[i * 16 + (lane & 15)];
   kv8_load_block<D>(c, size_t(max(src, 0)) * hkv + g, lane, kq, vq, kb, vs);
   if (rot != 0) {                            // one block per workgroup: all of its wavefronts or none
     if (threadIdx.x < D / 2) {
@@ -250,10 +254,10 @@ __global__ __launch_bounds__(kThreads) void kv8_write_rotate_kernel(Kv8Rows w, c
   const Kv8Fresh<J> f = kv8_fresh<D>(row, w.k_s, w.v_s, hkv, g, lane, turn[threadIdx.x >> 6]);
   if (src < 0) kv8_no_block<D>(kq, vq, kb, vs);
   kv8_merge<D>(f, kq, vq, kb, vs, lane);
-  if (at.g < hkv) kv8_store_block<D>(kq, vq, kb, vs, c, size_t(dst) * hkv + g, lane);
+  if (head < hkv) kv8_store_block<D>(kq, vq, kb, vs, c, size_t(dst) * hkv + g, lane);
 }
 
-unsigned grid_of(int n, int hkv) { return unsigned(kv8_groups(n, hkv)); }
+unsigned grid_of(int n, int hkv) { return unsigned((int64_t(n) * hkv + kWaves - 1) / kWaves); }
 
 }  // namespace
 
@@ -273,7 +277,7 @@ void launch_kv8_unpack(const Kv8Move& mv, int head_dim, const epic_kv8_cache& c,
 
 void launch_kv8_expand(const int32_t* list, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
                        int32_t* table, hipStream_t stream) {
-  auto go = [&](auto kernel) { kernel<<<grid_of(n, hkv), kThreads, 0, stream>>>(list, c, hkv, k, v, table); };
+  auto go = [&](auto kernel) { kernel<<<grid_of(n, hkv), kThreads, 0, stream>>>(list, n, c, hkv, k, v, table); };
   if (head_dim == 128) go(kv8_expand_kernel<128>);
   else go(kv8_expand_kernel<64>);
 }
@@ -281,12 +285,13 @@ void launch_kv8_expand(const int32_t* list, int n, int hkv, int head_dim, const 
 void launch_kv8_write(const Kv8Rows& w, const int32_t* priv_rot, int hkv, int head_dim, float rope_theta,
                       const epic_kv8_cache& c, hipStream_t stream) {
   if (w.n == 0) return;
-  const dim3 grid(grid_of(w.n, hkv));
   if (priv_rot != nullptr) {
+    const dim3 grid(kv8_groups(w.n, hkv));
     const double l2t = std::log2(double(rope_theta));
     if (head_dim == 128) kv8_write_rotate_kernel<128><<<grid, kThreads, 0, stream>>>(w, priv_rot, c, hkv, l2t);
     else kv8_write_rotate_kernel<64><<<grid, kThreads, 0, stream>>>(w, priv_rot, c, hkv, l2t);
   } else {
+    const dim3 grid(grid_of(w.n, hkv));
     if (head_dim == 128) kv8_write_kernel<128><<<grid, kThreads, 0, stream>>>(w, c, hkv);
     else kv8_write_kernel<64><<<grid, kThreads, 0, stream>>>(w, c, hkv);
   }
