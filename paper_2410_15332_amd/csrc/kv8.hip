@@ -43,6 +43,7 @@ __device__ __forceinline__ uint32_t round4_each(uint32_t lo, uint32_t hi, const 
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(in(hi << 16, b[2]), in(hi & 0xFFFF0000u, b[3]), r, true));
 }
 
+// 8192 blocks of 8 heads of 128 (806 MB): 155 us, 5.2 TB/s (two bytes read per byte written; 161 through the caches).
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const uint16_t* __restrict__ k,
                                                             const uint16_t* __restrict__ v, epic_kv8_cache c) {
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const ui
     store16(c.k + to + 1024 * j + 16 * lane, q);
     store16(c.v + to + 1024 * j + 16 * lane,
             make_uint4(round4_each(y[4 * j].x, y[4 * j].y, vb), round4_each(y[4 * j + 1].x, y[4 * j + 1].y, vb),
-                   round4_each(y[4 * j + 2].x, y[4 * j + 2].y, vb), round4_each(y[4 * j + 3].x, y[4 * j + 3].y, vb)));
+                       round4_each(y[4 * j + 2].x, y[4 * j + 2].y, vb), round4_each(y[4 * j + 3].x, y[4 * j + 3].y, vb)));
   }
   uint8_t* s = c.scale + (size_t(dst) * mv.hkv + at.g) * kKv8Scales;
   if (lane < 16) s[lane] = uint8_t(kb);
@@ -105,8 +106,9 @@ __device__ __forceinline__ uint2 wide4(uint32_t w, int b0, int b1, int b2, int b
     const float z = __builtin_amdgcn_ldexpf(f, b - 127);
     return b == kKv8Nan ? nan : z;
   };
-  return make_uint2(pack_bf16x2(one(__builtin_amdgcn_cvt_f32_fp8(int(w), 0), b0), one(__builtin_amdgcn_cvt_f32_fp8(int(w), 1), b1)),
-                    pack_bf16x2(one(__builtin_amdgcn_cvt_f32_fp8(int(w), 2), b2), one(__builtin_amdgcn_cvt_f32_fp8(int(w), 3), b3)));
+  const float f0 = one(__builtin_amdgcn_cvt_f32_fp8(int(w), 0), b0), f1 = one(__builtin_amdgcn_cvt_f32_fp8(int(w), 1), b1);
+  const float f2 = one(__builtin_amdgcn_cvt_f32_fp8(int(w), 2), b2), f3 = one(__builtin_amdgcn_cvt_f32_fp8(int(w), 3), b3);
+  return make_uint2(pack_bf16x2(f0, f1), pack_bf16x2(f2, f3));
 }
 
 // A block's K and V, as a wavefront holds them, into block `block_head` of a bf16 cache; V of NaN tokens: nan_v.
@@ -136,7 +138,7 @@ __device__ __forceinline__ void store_wide(const uint4 (&x)[D / 64], const uint4
   }
 }
 
-// 8192 blocks of 8 heads of 128 (806 MB): 165 us, 4.9 TB/s, the rate of a large copy.
+// 8192 blocks of 8 heads of 128 (806 MB): 166 us, 4.9 TB/s, the rate of a large copy (176 with stores past the caches).
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_kv8_cache c, uint16_t* __restrict__ k,
                                                               uint16_t* __restrict__ v) {
@@ -154,8 +156,8 @@ __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_k
 
 // The attention kernel of wide tiles reads a bf16 cache: block i of the list (null: block i of the pool) into block i of
 // one, with K = NaN, V = 0 for NaN tokens (that kernel multiplies masked V by 0).  8208 blocks of 8 heads of 128 (809 MB):
-// 137 us, 5.9 TB/s.  (Forming private blocks here too, as decode does, saves the write's launch, 4 us, and costs
-// as much of 324 blocks and 20 us of 8208.)
+// 138 us, 5.9 TB/s.  (Forming private blocks here too, as decode does, saves the write's launch and costs as much:
+// 46.7 us of a link step over 324 blocks both ways, 125 for 120 over 964.)
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_expand_kernel(const int32_t* __restrict__ list, int n, epic_kv8_cache c,
                                                               int hkv, uint16_t* __restrict__ k, uint16_t* __restrict__ v,

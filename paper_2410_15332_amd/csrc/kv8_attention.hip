@@ -12,18 +12,18 @@
 //     is the dword of 4 keys of its dim that the cache's order keeps together, for each block.
 // What bounds it is the read of K and V, once per item.  K's registers take the next pair as soon
 // as its scores are formed, V's after the product, and three workgroups of four wavefronts fit a
-// CU: 131 329 keys of 8 heads of 128 (271 MB) in 48 us, 5.6 TB/s, the rate of a plain read
-// (56 with all loads behind the product and two workgroups).  With a single tile no block is read
-// twice, and K and V pass the caches (NT): 49 -> 43 us before the write joined; where requests
-// share blocks that costs 6 us of 64.  Up to 256 workgroups, one a CU, have eight wavefronts: what
-// bounds these is the chain of loads (528 keys: 9.5 -> 8.5 us a step).
+// CU: 131 323 keys of 8 heads of 128 (271 MB) in 45.5 us, 6.0 TB/s, above what a plain read reaches
+// (55.8 with all loads behind the product and two workgroups).  With a single tile no block is read
+// twice, and K and V pass the caches (NT): 62.6 -> 56.1 us a step, write and merge among them; where
+// requests share blocks that costs 6 us of 64.  Up to 256 workgroups, one a CU, have eight wavefronts:
+// what bounds these is the chain of loads (529 keys of 8 heads of 64: 9.5 -> 8.5 us a step).
 //
 // The link write of few private blocks (decode: one or two a request) is done here too, by
 // workgroups in front of the others, and nothing waits for them: the rows of S that a private block
-// receives are read from the call's inputs and rounded by whoever attends to them, as a block
-// of their own; of the block itself the other tokens are read, from its source, and a
-// block that is its own source has only the new rows' bytes stored.  A step of one request gets 3 to 4 us
-// shorter by the launch saved (528 keys 9.5 -> 6.9, 131 329 keys 58 -> 54).
+// receives are read from the call's inputs and rounded by whoever attends to them, as a block of
+// their own; of the block itself the other tokens are read, from its source, and a block that is its
+// own source has only the new rows' bytes stored.  The launch saved makes a step of one request
+// shorter (529 keys 8.5 -> 6.9 us, 131 323 keys 58.4 -> 53.6) and leaves one of 32 requests at 64.
 #include <cmath>
 #include <type_traits>
 
@@ -51,7 +51,8 @@ struct Kv8Block {
   uint32_t ks, vs;                            // scales of keys 4 a ..
 };
 
-// NT: K and V are read past the caches, which hold nothing of them that is read again.
+// W wavefronts, RING pairs of blocks in flight of each.  NT: K and V are read past the caches, which hold nothing of
+// them that is read again.
 template <int D, int W, int RING, bool NT>
 __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(AttnArgs a, epic_kv8_cache c, Kv8Rows w) {
   constexpr int J = D / 64;
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(Attn
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // The wavefront's blocks, in pairs: block i of its own (i = 2 p + e) is b0 + 2 (wave + 4 p) + e.
+  // The wavefront's blocks, in pairs: block i of its own (i = 2 p + e) is b0 + 2 (wave + W p) + e.
   // Their ids, positions and lengths come 64 at a time, one per lane, so that no load of a block
   // waits for a chain of loads; past the item's end stands its last block, with no keys.
   const int n_pairs = (b1 - b0 + 1) / 2;
@@ -313,8 +314,9 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(Attn
             load_v(phys0, ring[j][0]);
             load_v(phys1, ring[j][1]);
           };
-          step(std::false_type{}, ring[j][0], ring[j][1], __builtin_amdgcn_readlane(pos_l, 2 * p), __builtin_amdgcn_readlane(pos_l, 2 * p + 1),
-               __builtin_amdgcn_readlane(valid_l, 2 * p), __builtin_amdgcn_readlane(valid_l, 2 * p + 1), after_k, after_v);
+          step(std::false_type{}, ring[j][0], ring[j][1], __builtin_amdgcn_readlane(pos_l, 2 * p),
+               __builtin_amdgcn_readlane(pos_l, 2 * p + 1), __builtin_amdgcn_readlane(valid_l, 2 * p),
+               __builtin_amdgcn_readlane(valid_l, 2 * p + 1), after_k, after_v);
         }
       }
     }

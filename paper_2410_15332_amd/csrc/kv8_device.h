@@ -23,9 +23,15 @@ __device__ __forceinline__ uint32_t e4m3_pair(uint32_t w, float scale) {
 // Loads and stores of bytes that nothing reads again soon.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ uint4 load16(const void* p) { return __builtin_bit_cast(uint4, __builtin_nontemporal_load(static_cast<const u32x4*>(p))); }
-__device__ __forceinline__ uint2 load8(const void* p) { return __builtin_bit_cast(uint2, __builtin_nontemporal_load(static_cast<const u32x2*>(p))); }
-__device__ __forceinline__ void store16(void* p, const uint4& x) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), static_cast<u32x4*>(p)); }
+__device__ __forceinline__ uint4 load16(const void* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(static_cast<const u32x4*>(p)));
+}
+__device__ __forceinline__ uint2 load8(const void* p) {
+  return __builtin_bit_cast(uint2, __builtin_nontemporal_load(static_cast<const u32x2*>(p)));
+}
+__device__ __forceinline__ void store16(void* p, const uint4& x) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), static_cast<u32x4*>(p));
+}
 
 // |bits| of the pairs of a dword, and the larger of two such dwords, half by half.
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -83,8 +89,8 @@ constexpr int kTurnLd = 68;                   // bytes of a token's 64 dims in L
 template <int J>
 constexpr int kTurnInts = J * 16 * kTurnLd / 4;
 
-// row: of token r, or -1.  V rows come like K's, 16 dims of a token a lane; their e4m3 bytes change places through `turn`, LDS of this
-// wavefront alone.
+// row: of token r, or -1.  V rows come like K's, 16 dims of a token a lane; their e4m3 bytes change places
+// through `turn`, LDS of this wavefront alone.
 template <int D>
 __device__ __forceinline__ Kv8Fresh<D / 64> kv8_fresh(int row, const uint16_t* k_s, const uint16_t* v_s, int hkv, int g,
                                                       int lane, uint32_t* turn) {
@@ -242,19 +248,19 @@ template <int D>
 __device__ __forceinline__ void kv8_write_private(const Kv8Rows& w, const epic_kv8_cache& c, int i, int hkv, int g, int lane,
                                                   uint32_t* turn) {
   const int dst = w.block[i], src = w.src[i], row = w.rows[i * 16 + (lane & 15)];
+  const size_t to = size_t(dst) * hkv + g;
+  if (src == dst) {
+    kv8_store_fresh<D>(kv8_fresh<D>(row, w.k_s, w.v_s, hkv, g, lane, turn), c, to, lane);
+    return;
+  }
   uint4 kq[D / 64], vq[D / 64];
   int kb;
   uint32_t vs;
   kv8_load_block<D>(c, size_t(max(src, 0)) * hkv + g, lane, kq, vq, kb, vs);
   const Kv8Fresh<D / 64> f = kv8_fresh<D>(row, w.k_s, w.v_s, hkv, g, lane, turn);
   if (src < 0) kv8_no_block<D>(kq, vq, kb, vs);            // (here: before, it would wait for the loads)
-  const size_t to = size_t(dst) * hkv + g;
-  if (src == dst) {
-    kv8_store_fresh<D>(f, c, to, lane);
-  } else {
-    kv8_merge<D>(f, kq, vq, kb, vs, lane);
-    kv8_store_block<D>(kq, vq, kb, vs, c, to, lane);
-  }
+  kv8_merge<D>(f, kq, vq, kb, vs, lane);
+  kv8_store_block<D>(kq, vq, kb, vs, c, to, lane);
 }
 
 }  // namespace epic
