@@ -125,8 +125,10 @@ extern "C" epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const e
   record_profile_event(0, stream);
   const bool tiny = sizes->tile_rows == kTileRowsTiny;
   Kv8Rows rows{plan_dev->priv_block, plan_dev->priv_src, plan_dev->priv_rows, k_s, v_s, sizes->n_private, 0};
-  // Decode: few private blocks, none turned, are written by the launch that reads them
-  const bool joined = tiny && sizes->n_s > 0 && sizes->n_rerotated == 0 && sizes->n_private <= kKv8JoinedRows;
+  // Few private blocks, none turned, are written by the launch that reads them; for wide tiles where a launch counts
+  // beside what is widened
+  const bool joined = sizes->n_s > 0 && sizes->n_rerotated == 0 && sizes->n_private <= kKv8JoinedRows &&
+                      (tiny || int64_t(sizes->n_linked_blocks) * hkv <= kKv8JoinedPairs);
   if (!joined) {
     launch_kv8_write(rows, sizes->n_rerotated > 0 ? plan_dev->priv_rot : nullptr, hkv, d, cfg->rope_theta, *cache, stream);
     rows.n = 0;
@@ -135,6 +137,7 @@ extern "C" epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const e
   AttnArgs a = attention_args(cfg, sizes, plan_dev, q_s, nullptr, nullptr, out, lse, workspace);
   if (tiny) {
     record_profile_event(1, stream);
+    // a single tile: no two work items read the same block
     launch_kv8_decode(a, *cache, rows, d, sizes->n_work, sizes->n_tiles == 1, stream);
   } else {
     // The matrix cores bound wide tiles, and every tile would widen the same keys again: they are widened once, for
@@ -145,9 +148,9 @@ extern "C" epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const e
     int32_t* table = reinterpret_cast<int32_t*>(ws + w.table);
     a.k_cache = k, a.v_cache = v;
     if (cache->num_blocks < sizes->n_linked_blocks) {
-      launch_kv8_expand(nullptr, cache->num_blocks, hkv, d, *cache, k, v, nullptr, stream);
+      launch_kv8_expand(nullptr, cache->num_blocks, hkv, d, *cache, rows, k, v, nullptr, stream);
     } else {
-      launch_kv8_expand(plan_dev->linked_blocks, sizes->n_linked_blocks, hkv, d, *cache, k, v, table, stream);
+      launch_kv8_expand(plan_dev->linked_blocks, sizes->n_linked_blocks, hkv, d, *cache, rows, k, v, table, stream);
       a.linked_blocks = table;
     }
     record_profile_event(1, stream);

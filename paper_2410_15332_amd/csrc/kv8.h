@@ -36,16 +36,17 @@ struct Kv8Rows {
   int n;                                      // private blocks; 0 in launches that find them written
   int groups;                                 // workgroups of the launch that write them (set by the launcher)
 };
-// Most that the decode launch writes itself: each of its wavefronts looks through them, a lane each.
+// Most that the launch that reads them writes itself: each of its wavefronts looks through them, a lane each.
 constexpr int kKv8JoinedRows = 64;
+constexpr int kKv8JoinedPairs = 1024;         // (linked block, KV head) of wide tiles
 
 // As launch_link_write and (priv_rot not null) launch_link_write_rotated.
 void launch_kv8_write(const Kv8Rows& w, const int32_t* priv_rot, int hkv, int head_dim, float rope_theta,
                       const epic_kv8_cache& c, hipStream_t stream);
 // Listed blocks (null: blocks 0 .. n - 1) as a bf16 cache of n blocks, for the attention kernel of wide tiles, and the
-// table 0 .. n - 1 where not null.
-void launch_kv8_expand(const int32_t* list, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
-                       int32_t* table, hipStream_t stream);
+// table 0 .. n - 1 where not null; writes the private blocks of w.
+void launch_kv8_expand(const int32_t* list, int n, int hkv, int head_dim, const epic_kv8_cache& c, const Kv8Rows& w,
+                       uint16_t* k, uint16_t* v, int32_t* table, hipStream_t stream);
 // As launch_link_decode; a.k_cache and a.v_cache are not read.  Writes the private blocks of w.  once: no two work
 // items read the same block.
 void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, const Kv8Rows& w, int head_dim, int n_work, bool once,

@@ -26,8 +26,8 @@ constexpr int kThreads = 64 * kWaves;
 struct Place {
   int i, g;
   bool in;
-  __device__ __forceinline__ Place(int n, int hkv) {
-    const int pair = int(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  __device__ __forceinline__ Place(int n, int hkv, int group) {
+    const int pair = group * kWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     i = pair / hkv;
     g = pair - i * hkv;
     in = i < n;
@@ -48,7 +48,7 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_pack_kernel(Kv8Move mv, const uint16_t* __restrict__ k,
                                                             const uint16_t* __restrict__ v, epic_kv8_cache c) {
   constexpr int J = D / 64;
-  const Place at(mv.n, mv.hkv);
+  const Place at(mv.n, mv.hkv, blockIdx.x);
   if (!at.in) return;
   const int src = mv.src ? mv.src[at.i] : at.i, dst = mv.dst ? mv.dst[at.i] : at.i;
   if (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks)) return;
@@ -142,7 +142,7 @@ __device__ __forceinline__ void store_wide(const uint4 (&x)[D / 64], const uint4
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_kv8_cache c, uint16_t* __restrict__ k,
                                                               uint16_t* __restrict__ v) {
-  const Place at(mv.n, mv.hkv);
+  const Place at(mv.n, mv.hkv, blockIdx.x);
   if (!at.in) return;
   const int src = mv.src ? mv.src[at.i] : at.i, dst = mv.dst ? mv.dst[at.i] : at.i;
   if (unsigned(src) >= unsigned(mv.src_blocks) || unsigned(dst) >= unsigned(mv.dst_blocks)) return;
@@ -156,19 +156,43 @@ __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_k
 
 // The attention kernel of wide tiles reads a bf16 cache: block i of the list (null: block i of the pool) into block i of
 // one, with K = NaN, V = 0 for NaN tokens (that kernel multiplies masked V by 0).  8208 blocks of 8 heads of 128 (809 MB):
-// 138 us, 5.9 TB/s.  (Forming private blocks here too, as decode does, saves the write's launch and costs as much:
-// 46.7 us of a link step over 324 blocks both ways, 125 for 120 over 964.)
-template <int D>
+// 137 us, 5.9 TB/s.
+// JOINED: few private blocks (w) are written by the workgroups in front, and nothing waits for these: a private block is
+// formed again here, from its source and its rows of S.  That saves a launch: a link step over 16 blocks of
+// 8 heads 20.7 us (23.0 with two), over 324 46.8 (46.1), over 380 43.5 (42.2), over 964 125 (120).
+template <int D, bool JOINED>
 __global__ __launch_bounds__(kThreads) void kv8_expand_kernel(const int32_t* __restrict__ list, int n, epic_kv8_cache c,
-                                                              int hkv, uint16_t* __restrict__ k, uint16_t* __restrict__ v,
-                                                              int32_t* __restrict__ table) {
-  const Place at(n, hkv);
+                                                              Kv8Rows w, int hkv, uint16_t* __restrict__ k,
+                                                              uint16_t* __restrict__ v, int32_t* __restrict__ table) {
+  __shared__ uint32_t turn[JOINED ? kWaves : 1][JOINED ? kTurnInts<D / 64> : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (JOINED && int(blockIdx.x) < w.groups) {
+    const Place at(w.n, hkv, blockIdx.x);
+    if (at.in) kv8_write_private<D>(w, c, at.i, hkv, at.g, lane, turn[wave]);
+    return;
+  }
+  const Place at(n, hkv, blockIdx.x - (JOINED ? w.groups : 0));
   if (!at.in) return;
-  const int lane = threadIdx.x & 63, phys = list ? list[at.i] : at.i;
+  const int phys = list ? list[at.i] : at.i;
   uint4 x[D / 64], y[D / 64];
-  int kb;
+  int kb, block = -1, block_src = 0;
   uint32_t vs;
+  if constexpr (JOINED) {
+    block = w.block[min(lane, w.n - 1)];
+    block_src = w.src[min(lane, w.n - 1)];
+  }
   kv8_load_block<D>(c, size_t(phys) * hkv + at.g, lane, x, y, kb, vs);
+  if constexpr (JOINED) {
+    const uint64_t mine = __ballot(lane < w.n && block == phys);
+    if (mine != 0) {
+      const int p = __builtin_ctzll(mine), src = __builtin_amdgcn_readlane(block_src, p);
+      const int row = w.rows[p * 16 + (lane & 15)];
+      if (src >= 0 && src != phys) kv8_load_block<D>(c, size_t(src) * hkv + at.g, lane, x, y, kb, vs);
+      const Kv8Fresh<D / 64> f = kv8_fresh<D>(row, w.k_s, w.v_s, hkv, at.g, lane, turn[wave]);
+      if (src < 0) kv8_no_block<D>(x, y, kb, vs);
+      kv8_merge<D>(f, x, y, kb, vs, lane);
+    }
+  }
   store_wide<D>(x, y, kb, vs, 0.0f, k, v, size_t(at.i) * hkv + at.g, lane);
   if (table != nullptr && at.g == 0 && lane == 0) table[at.i] = at.i;
 }
@@ -178,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void kv8_expand_kernel(const int32_t* __r
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_write_kernel(Kv8Rows w, epic_kv8_cache c, int hkv) {
   __shared__ uint32_t turn[kWaves][kTurnInts<D / 64>];
-  const Place at(w.n, hkv);
+  const Place at(w.n, hkv, blockIdx.x);
   if (at.in) kv8_write_private<D>(w, c, at.i, hkv, at.g, threadIdx.x & 63, turn[threadIdx.x >> 6]);
 }
 
@@ -277,11 +301,13 @@ void launch_kv8_unpack(const Kv8Move& mv, int head_dim, const epic_kv8_cache& c,
   else go(kv8_unpack_kernel<64>);
 }
 
-void launch_kv8_expand(const int32_t* list, int n, int hkv, int head_dim, const epic_kv8_cache& c, uint16_t* k, uint16_t* v,
-                       int32_t* table, hipStream_t stream) {
-  auto go = [&](auto kernel) { kernel<<<grid_of(n, hkv), kThreads, 0, stream>>>(list, n, c, hkv, k, v, table); };
-  if (head_dim == 128) go(kv8_expand_kernel<128>);
-  else go(kv8_expand_kernel<64>);
+void launch_kv8_expand(const int32_t* list, int n, int hkv, int head_dim, const epic_kv8_cache& c, const Kv8Rows& rows,
+                       uint16_t* k, uint16_t* v, int32_t* table, hipStream_t stream) {
+  Kv8Rows w = rows;
+  w.groups = int(grid_of(w.n, hkv));
+  auto go = [&](auto kernel) { kernel<<<w.groups + grid_of(n, hkv), kThreads, 0, stream>>>(list, n, c, w, hkv, k, v, table); };
+  if (head_dim == 128) w.n > 0 ? go(kv8_expand_kernel<128, true>) : go(kv8_expand_kernel<128, false>);
+  else w.n > 0 ? go(kv8_expand_kernel<64, true>) : go(kv8_expand_kernel<64, false>);
 }
 
 void launch_kv8_write(const Kv8Rows& w, const int32_t* priv_rot, int hkv, int head_dim, float rope_theta,

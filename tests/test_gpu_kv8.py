@@ -425,10 +425,12 @@ def test_many_requests_decode():
 
 
 @pytest.mark.parametrize("tile_rows", [128, 256])
-def test_wide_tiles_over_shared_chunks(tile_rows):
-    """Requests that link more blocks than the pool has: the pool is widened, not the list."""
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (16, 8, 64)])
+def test_wide_tiles_over_shared_chunks(hq, hkv, d, tile_rows):
+    """Requests that link more blocks than the pool has: the pool is widened, not the list; the private blocks with
+    it, or before it."""
     n = 9
-    r = Requests(8, 2, 128, [[0, 1, 2], [2, 1, 0], [1, 2, 0]] * 3, [200, 133, 170], [3] * n, 2, tile_rows=tile_rows, spare=4)
+    r = Requests(hq, hkv, d, [[0, 1, 2], [2, 1, 0], [1, 2, 0]] * 3, [200, 133, 170], [3] * n, 2, tile_rows=tile_rows, spare=4)
     assert r.sizes.n_linked_blocks > r.blocks
     spoil = [4, int(r.views["s_off"][2]) + 1]
     r.run(r.draw(spoil), what="shared")
