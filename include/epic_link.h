@@ -287,8 +287,8 @@ epic_status epic_link_attention_noalloc(const epic_attn_cfg* cfg, const epic_pla
  * where their Q|K|V projection leaves partial sums and nothing is re-rotated, the
  * pass that adds them up writes the private blocks itself, before events[0], so
  * nothing runs between events[0] and events[1].
- * epic_link_attention_kv8 widens the cache for wide tiles before events[1]; in 16-row tiles its
- * attention kernel writes few private blocks itself.)
+ * epic_link_attention_kv8 widens the cache for wide tiles before events[1]; few private blocks
+ * are written by that launch, or in 16-row tiles by its attention kernel.)
  * Never fails. */
 epic_status epic_set_profile_events(void* const* events);
 
