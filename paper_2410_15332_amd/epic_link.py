@@ -660,20 +660,37 @@ def kv8_shapes(num_blocks: int, hkv: int, d: int):
 
 class Kv8Cache:
     """An 8-bit cache of one layer (see include/epic_link.h): three tensors of kv8_shapes(), uint8 or torch's
-    8-bit float types, which stay the caller's."""
+    8-bit float types, which stay the caller's.  A call works on the memory that they have by then: other tensors
+    may take their place, and they may be resized."""
 
     def __init__(self, k, v, scale):
+        self.k, self.v, self.scale = k, v, scale
+        self._checked()
+
+    def __setattr__(self, name, x):
+        if name in ("k", "v", "scale"):
+            self.__dict__["_at"] = None               # the next call looks at it
+        self.__dict__[name] = x
+
+    def _checked(self) -> "Kv8Cache":
+        """Itself.  Addresses and sizes other than those that were checked last are checked again (0.35 us where they are
+        the same; all of shapes, types, strides and device would be 1.1)."""
+        k, v, scale = self.k, self.v, self.scale
+        at = (k.data_ptr(), v.data_ptr(), scale.data_ptr(), k.numel(), v.numel(), scale.numel())
+        if at == self._at:
+            return self
         if k.dim() != 6 or k.shape[2] not in (1, 2):
             raise ValueError(f"k: [blocks, Hkv, D / 64, 4, 16, 16] expected, got {tuple(k.shape)}")
         _, _, e4m3, e8m0 = _dtypes()[:4]
-        self.num_blocks, self.hkv, self.d = k.shape[0], k.shape[1], 64 * k.shape[2]
-        self.device = k.get_device()
-        shapes = kv8_shapes(self.num_blocks, self.hkv, self.d)
-        at = [_expect(name, t, shape, dtypes, self.device) for name, t, shape, dtypes in
-              zip(("k", "v", "scale"), (k, v, scale), shapes, (e4m3, e4m3, e8m0))]
-        self.k, self.v, self.scale = k, v, scale
-        self.c = epic_kv8_cache(*at, self.num_blocks)
-        self.cfg = attn_cfg(self.hkv, self.hkv, self.d)   # what the moves need of an attention config
+        num_blocks, hkv, d, device = k.shape[0], k.shape[1], 64 * k.shape[2], k.get_device()
+        for name, t, shape, dtypes in zip(("k", "v", "scale"), (k, v, scale), kv8_shapes(num_blocks, hkv, d),
+                                          (e4m3, e4m3, e8m0)):
+            _expect(name, t, shape, dtypes, device)
+        self.num_blocks, self.hkv, self.d, self.device = num_blocks, hkv, d, device
+        self.c = epic_kv8_cache(*at[:3], num_blocks)
+        self.cfg = attn_cfg(hkv, hkv, d)              # what the moves need of an attention config
+        self._at = at
+        return self
 
     @classmethod
     def zeros(cls, num_blocks: int, hkv: int, d: int, device="cuda"):
@@ -683,18 +700,23 @@ class Kv8Cache:
 
     def of(self, hkv: int, d: int, device: int):
         """Its C form, for a call with these heads on this device."""
+        self._checked()
         if self.hkv != hkv or self.d != d:
             raise ValueError(f"8-bit cache: {hkv} KV heads of {d} expected, got {self.hkv} of {self.d}")
+        return self.on(device)
+
+    def on(self, device: int):
         if self.device != device:
             raise ValueError(f"8-bit cache: expected on device {device}, got one of {self.device}")
         return C.byref(self.c)
 
 
 def _kv8_move(k_cache, v_cache, cache: Kv8Cache, src_blocks, dst_blocks):
-    """What the moves between a bf16 and an 8-bit cache share: device, number of blocks, addresses, and the bf16 pool's blocks."""
+    """What the moves between a bf16 and an 8-bit cache share: device, number of blocks, addresses, the bf16 pool's blocks
+    and the 8-bit cache's C form."""
     bf16, _, _, _, i32, _ = _dtypes()
     dev = _device_of("k_cache", k_cache)
-    pool, hkv, d = k_cache.shape[0], cache.hkv, cache.d
+    pool, hkv, d = k_cache.shape[0], cache._checked().hkv, cache.d
     if src_blocks is not None:
         n = len(src_blocks)
     elif dst_blocks is not None:
@@ -706,22 +728,20 @@ def _kv8_move(k_cache, v_cache, cache: Kv8Cache, src_blocks, dst_blocks):
     return (dev, n, None if src_blocks is None else _expect("src_blocks", src_blocks, (n,), i32, dev),
             None if dst_blocks is None else _expect("dst_blocks", dst_blocks, (n,), i32, dev),
             _expect("k_cache", k_cache, (pool, hkv, 16, d), bf16, dev),
-            _expect("v_cache", v_cache, (pool, hkv, d, 16), bf16, dev), pool)
+            _expect("v_cache", v_cache, (pool, hkv, d, 16), bf16, dev), pool, cache.on(dev))
 
 
 def epic_kv8_pack(k_cache, v_cache, cache: Kv8Cache, src_blocks=None, dst_blocks=None, stream=None):
     """Enqueue blocks src_blocks of a bf16 cache -> blocks dst_blocks of an 8-bit one (int32 lists in device
     memory; None: 0 .. n - 1)."""
-    dev, n, src, dst, k, v, pool = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks)
-    _check(_kv8_pack(C.byref(cache.cfg), n, src, k, v, pool, dst, cache.of(cache.hkv, cache.d, dev),
-                     _raw_stream(stream, dev)), "epic_kv8_pack")
+    dev, n, src, dst, k, v, pool, c = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks)
+    _check(_kv8_pack(C.byref(cache.cfg), n, src, k, v, pool, dst, c, _raw_stream(stream, dev)), "epic_kv8_pack")
 
 
 def epic_kv8_unpack(cache: Kv8Cache, k_cache, v_cache, src_blocks=None, dst_blocks=None, stream=None):
     """Enqueue blocks src_blocks of an 8-bit cache -> blocks dst_blocks of a bf16 one."""
-    dev, n, src, dst, k, v, pool = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks)
-    _check(_kv8_unpack(C.byref(cache.cfg), n, src, cache.of(cache.hkv, cache.d, dev), dst, k, v, pool,
-                       _raw_stream(stream, dev)), "epic_kv8_unpack")
+    dev, n, src, dst, k, v, pool, c = _kv8_move(k_cache, v_cache, cache, src_blocks, dst_blocks)
+    _check(_kv8_unpack(C.byref(cache.cfg), n, src, c, dst, k, v, pool, _raw_stream(stream, dev)), "epic_kv8_unpack")
 
 
 def epic_link_kv8_workspace_bytes(cfg: epic_attn_cfg, sizes: epic_plan_sizes) -> int:

@@ -243,3 +243,48 @@ def test_cache_types_and_strides_are_checked():
     with pytest.raises(ValueError):
         el.Kv8Cache(k, v.transpose(3, 4), s)
     el.Kv8Cache(k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu))
+
+
+def _parts(cache, hkv=2, d=64):
+    c = cache.of(hkv, d, -1)._obj
+    return c.k, c.v, c.scale, c.num_blocks
+
+
+def _addresses(cache):
+    return cache.k.data_ptr(), cache.v.data_ptr(), cache.scale.data_ptr(), cache.k.shape[0]
+
+
+def test_cache_follows_its_tensors():
+    """A call takes the addresses that the tensors have by then: after other tensors took their place, and after they
+    were resized."""
+    cache = el.Kv8Cache.zeros(4, 2, 64, device="cpu")
+    assert _parts(cache) == _addresses(cache)
+    old = cache.k                                        # (kept, so that its address is no other's)
+    cache.k = torch.ones_like(old)
+    assert cache.k.data_ptr() != old.data_ptr() and _parts(cache) == _addresses(cache)
+    cache.k, cache.v, cache.scale = (torch.zeros(s, dtype=torch.uint8) for s in el.kv8_shapes(9, 2, 64))
+    assert _parts(cache) == _addresses(cache) and cache.num_blocks == 9
+    for n in (4096, 3):                                  # to other memory; within what it has
+        for t, s in zip((cache.k, cache.v, cache.scale), el.kv8_shapes(n, 2, 64)):
+            t.resize_(s)
+        assert _parts(cache) == _addresses(cache) and cache.num_blocks == n
+    cache.k, cache.v, cache.scale = (torch.zeros(s, dtype=torch.uint8) for s in el.kv8_shapes(4, 3, 128))
+    assert _parts(cache, 3, 128) == _addresses(cache) and (cache.hkv, cache.d) == (3, 128)
+    with pytest.raises(ValueError):
+        cache.of(2, 64, -1)
+
+
+@pytest.mark.parametrize("name", ["k", "v", "scale"])
+def test_cache_of_unlike_tensors_is_refused(name):
+    for change in (lambda t: t[:3], lambda t: torch.zeros((5, *t.shape[1:]), dtype=t.dtype), lambda t: t.to(torch.int16),
+                   lambda t: t.transpose(0, 1)):
+        cache = el.Kv8Cache.zeros(4, 4, 64, device="cpu")
+        setattr(cache, name, change(getattr(cache, name)))
+        for _ in range(2):
+            with pytest.raises(ValueError):
+                cache.of(4, 64, -1)
+    cache = el.Kv8Cache.zeros(4, 4, 64, device="cpu")
+    t = getattr(cache, name)
+    t.resize_((6, *t.shape[1:]))                         # one of the three
+    with pytest.raises(ValueError):
+        cache.of(4, 64, -1)
