@@ -458,6 +458,86 @@ def test_decode_over_shared_chunks(hq, hkv, d):
     assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
 
 
+def _workgroups(r, waves):
+    """Workgroups of a launch of 16-row tiles at `waves` wavefronts: up to 256 take eight, more four."""
+    hkv = r.heads[1]
+    return r.sizes.n_work * hkv + r.sizes.n_private * -(-hkv // waves)
+
+
+def _item_blocks(r):
+    work = r.views["work"].reshape(-1, 8)
+    work = work[work[:, 0] >= 0]
+    return work[:, 2] - work[:, 1]
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (16, 8, 64)])
+@pytest.mark.parametrize("split", [4, 20])
+def test_decode_of_one_long_request(hq, hkv, d, split):
+    """A single tile in more workgroups than CUs: its blocks are read past the caches, by four wavefronts each."""
+    r = Requests(hq, hkv, d, [[0, 1]], [16 * 18 * split - 5, 16 * 17 * split + 3], [0], 0, split=split)
+    for new in ([1], [1 if hq // hkv > 2 else 3], [1]):
+        r.decode(new)
+        assert r.sizes.tile_rows == 16 and r.sizes.n_tiles == 1 and _workgroups(r, 8) > 256 and r.sizes.n_private <= 64
+        r.run(what=f"one request, items of {split} blocks")
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(16, 8, 64), (8, 8, 128)])
+@pytest.mark.parametrize("length", [16 * 257, 16 * 300 - 7])
+def test_long_items_of_four_wavefronts(hq, hkv, d, length):
+    """Items of more blocks than four wavefronts take the ids of at once; the last blocks, a private one among them, are
+    of the second lot, and their number is odd."""
+    n = 40
+    r = Requests(hq, hkv, d, [[i % 2] for i in range(n)], [length, length + 32], [5 + i % 12 for i in range(n)], 0, split=4096,
+                 spare=2 * n, garbage=False)
+    for new in ([1] * n, [1 + i % 2 for i in range(n)]):
+        r.decode(new)
+        assert r.sizes.tile_rows == 16 and _workgroups(r, 8) > 256 and 0 < r.sizes.n_private <= 64
+        blocks = _item_blocks(r)
+        assert blocks.min() > 256 and (blocks % 2 == 1).any()
+        r.every = 13
+        r.run(what="long items")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("length", [16 * 513 - 3, 16 * 530])
+def test_long_items_of_eight_wavefronts(d, length):
+    r = Requests(4, 1, d, [[0]], [length], [7], 0, split=4096)
+    for new in ([1], [4], [3]):
+        r.decode(new)
+        assert r.sizes.tile_rows == 16 and _workgroups(r, 8) <= 256 and _item_blocks(r).min() > 512
+        r.run(what="long item")
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(16, 8, 64), (16, 8, 128)])
+def test_copied_blocks_in_many_small_tiles(hq, hkv, d):
+    """Private blocks that keep tokens of a shared block, written by the attention launch of more workgroups than CUs."""
+    n = 10
+    r = Requests(hq, hkv, d, [[i % 3, (i + 1) % 3] for i in range(n)], [90, 57, 131], [9 + i % 3 for i in range(n)], 20,
+                 tile_rows=16)
+    src = r.views["priv_src"]
+    assert _workgroups(r, 8) > 256 and r.sizes.n_private <= 64 and ((src >= 0) & (src != r.views["priv_block"])).any()
+    r.run(what="copied blocks")
+
+
+@pytest.mark.parametrize("tile_rows", [16, 128, 256])
+@pytest.mark.parametrize("d", [64, 128])
+def test_nan_in_a_chunk(d, tile_rows):
+    """A cached token that is NaN, of one KV head, with a thousand tokens before it and behind it: rows before it and rows of
+    requests that do not link its chunk stay finite, rows behind it are NaN in that head's."""
+    r = Requests(8, 4, d, [[0, 1], [1, 0], [0]], [1400, 2300], [20, 9, 3], 6, tile_rows=tile_rows)
+    b, s = r.ids[1][1111 // 16], 1111 % 16               # token 1111 of chunk 1
+    r.c["k"][b, 2, s], r.c["v"][b, 2, s], r.c["ks"][b, 2, s], r.c["vs"][b, 2, s] = 0x7F, 0, 255, 255
+    r.cache = _upload(r.c)
+    out, _ = r.run(what="NaN in a chunk")
+    bad = torch.isnan(out).any(-1).cpu().numpy()
+    off = r.views["s_off"]
+    want = np.zeros_like(bad)
+    for req, at in ((0, 1400 + 1111), (1, 1111)):
+        rows = slice(int(off[req]), int(off[req + 1]))
+        want[rows, 4:6] = (r.views["s_pos"][rows] >= at)[:, None]
+    assert np.array_equal(bad, want) and want.any() and not want[:, 4].all()
+
+
 @pytest.mark.parametrize("tile_rows", [16, 128, 256])
 @pytest.mark.parametrize("d", [64, 128])
 def test_nan_where_it_is_masked(d, tile_rows):
