@@ -92,7 +92,9 @@ typedef struct {
  * by its linked offset off_j (RoPE composes, so R(off_j) R(t) = R(off_j + t)): all
  * blocks of those chunks become private copies, written by the link write with K
  * rotated in fp32 from float64 angles and rounded to bf16, V copied unchanged.
- * Chunk 0 (offset 0) stays shared.  Ignored for k < 0 (every token recomputed). */
+ * Chunk 0 (offset 0) stays shared.  Ignored for k < 0 (every token recomputed).
+ * The rotation is that of epic_attn_cfg.rope_theta: keys that were rotated otherwise
+ * (epic_rope_cfg) must not be re-rotated. */
 typedef struct {
   int32_t num_chunks;
   const int32_t* chunk_len;        /* [num_chunks], each >= 1 */
@@ -478,7 +480,12 @@ epic_status epic_link_model_fp8(const epic_model_cfg* cfg, const epic_layer_weig
  * keep_j = 0 where original_context == 0 (every frequency divided by factor), else, with
  * turns_j = original_context * theta^(-2 j / rot_dim) / 2 pi the turns that pair j makes over the
  * context the model was trained on, 0 up to low_turns, 1 from high_turns, and linear between.
- * amplitude multiplies the rotated pairs.  factor == 0 and amplitude == 0 stand for 1. */
+ * amplitude multiplies the rotated pairs.  factor == 0 and amplitude == 0 stand for 1.
+ * Plans that re-rotate cached keys (epic_link_request.rerotate) turn the whole head, pairs
+ * (j, j + D / 2), by offset * rope_theta^(-2 j / D) of epic_attn_cfg, however the keys were made;
+ * nothing tells it from the keys.  Such plans are for keys of rot_dim == head_dim, interleaved == 0,
+ * factor 1 and theta == rope_theta, with any amplitude and norm; keys of other forms would come
+ * out wrong. */
 typedef struct {
   int32_t rot_dim;
   int32_t interleaved;
@@ -542,7 +549,7 @@ epic_status epic_kv8_unpack(const epic_attn_cfg* cfg, int32_t n, const int32_t* 
 
 /* epic_link_attention over an 8-bit cache, with any plan (link, decode, compile):
  *   1. every private block takes its source's bytes (K of re-rotated blocks: turned in fp32 and
- *      rounded to 8 bits again), then the S rows k_s / v_s, rounded; a slot with neither holds zeros;
+ *      rounded to 8 bits again; see epic_rope_cfg for the keys that these may hold), then the S rows k_s / v_s, rounded; a slot with neither holds zeros;
  *   2. attention as there, over the values that the cache now holds, with fp32 sums (V of 2^119 and
  *      more may overflow them), P rounded to bf16.  A row that attends to a NaN token has NaN in
  *      out, and its lse means nothing; NaN in tokens after a row, or in slots past a block's

@@ -611,6 +611,8 @@ def epic_link_model_fp8(cfg: epic_model_cfg, layers: Sequence[epic_layer_weights
 
 def rope_cfg(rot_dim: int, theta: float, interleaved: bool = False, factor: float = 1.0, original_context: int = 0,
              low_turns: float = 0.0, high_turns: float = 0.0, amplitude: float = 1.0) -> epic_rope_cfg:
+    """How epic_qk_norm_rope rotates.  Requests with rerotate take keys of the whole head, not interleaved, of factor 1 and
+    the plan's rope_theta alone (see include/epic_link.h)."""
     return epic_rope_cfg(rot_dim, int(interleaved), theta, factor, original_context, low_turns, high_turns, amplitude)
 
 

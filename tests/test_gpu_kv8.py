@@ -15,7 +15,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from oracle import fp8, kv8  # noqa: E402
-from oracle.link import masked_attention  # noqa: E402
+from oracle.link import masked_attention, rope as rope_at  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -536,6 +536,51 @@ def test_nan_in_a_chunk(d, tile_rows):
         rows = slice(int(off[req]), int(off[req + 1]))
         want[rows, 4:6] = (r.views["s_pos"][rows] >= at)[:, None]
     assert np.array_equal(bad, want) and want.any() and not want[:, 4].all()
+
+
+@pytest.mark.parametrize("amplitude", [1.0, 1.25])
+def test_turned_keys_after_the_rotation(amplitude):
+    """Keys of epic_qk_norm_rope in the form that re-rotating plans turn (the whole head, half pairs, the plan's base, no
+    scaled frequencies): compiled into 8-bit blocks at their chunks' positions, then linked with rerotate, they are the normed
+    keys turned at their linked positions.  Bars, with p = |(a, b)| of a value's pair, which no turn changes, and m the row's
+    largest |y| before the first turn: a turned row's largest is at most sqrt(2) m (1.1 of that after its rounding), its scale 2^t
+    at most 1 / 224 of it =: s.  Rounding to bf16 and to 8 bits leaves 2^-8 and 2^-4 of a value or half the smallest step, 2^-10
+    2^t; two such errors of a pair come out of a turn as at most e = (2^-8 + 2^-4) p + sqrt(2) 2^-10 s.  The second rounding
+    to 8 bits adds 2^-4 (|y| + e) + 2^-10 s; fp32 stays under 2^-12 p in all."""
+    el = _el()
+    hq, hkv, d = 8, 2, 128
+    lens, dev = [75, 130, 48], "cuda"
+    r = Requests(hq, hkv, d, [[0, 1, 2]], lens, [11], 4, rerotate=True, spare=60, garbage=False)
+    link = (r.sizes, r.host, r.views)
+    sizes, host, views = el.epic_plan_compile(lens, r.ids, 0, r.cfg, r.free, r.blocks)
+    n, rope = sizes.n_s, el.rope_cfg(d, THETA, amplitude=amplitude)
+    x = torch.from_numpy(_rows(r.rng, n, (hq + 2 * hkv) * d)).float().to(dev)
+    w = torch.from_numpy(1 + 0.2 * r.rng.normal(size=d)).to(torch.bfloat16).to(dev)
+    q, k, v = (torch.empty((n, h, d), dtype=torch.bfloat16, device=dev) for h in (hq, hkv, hkv))
+    el.epic_qk_norm_rope(r.cfg, rope, x, torch.from_numpy(views["s_pos"].copy()).to(dev),
+                         torch.from_numpy(el.epic_rope_freqs(rope)).to(dev), q, k, v, q_norm=w, k_norm=w)
+    ws = torch.empty(max(256, el.epic_link_kv8_workspace_bytes(r.cfg, sizes)), dtype=torch.uint8, device=dev)
+    el.epic_link_attention_kv8(r.cfg, el.DevicePlan(sizes, host), q, k, v, r.cache, torch.empty_like(q), None, ws)
+    torch.cuda.synchronize()
+    r.c = _download(r.cache)
+    r.sizes, r.host, r.views = link
+    r.run(what="link of turned keys")
+    y = x.double().cpu().numpy().reshape(n, -1, d)[:, hq:hq + hkv]
+    y = amplitude * y / np.sqrt((y * y).mean(-1, keepdims=True) + 1e-6) * w.double().cpu().numpy()
+    K, _ = kv8.linked(r.c, r.views, 0)
+    first = np.cumsum([0] + lens)
+    rows = set(r.views["s_pos"].tolist())                # of S, not cached
+    for c in range(3):
+        pos = np.array([p for p in range(first[c], first[c + 1]) if p not in rows])
+        part = y[pos]
+        want = rope_at(part, pos, THETA)
+        pair = np.hypot(part, np.roll(part, d // 2, -1))  # |(a, b)| of each dim's pair
+        top = np.abs(part).max(-1, keepdims=True)
+        step = 2.0 ** -10 * np.sqrt(2) * 1.1 * top / 224
+        e = (2.0 ** -8 + 2.0 ** -4) * pair + np.sqrt(2) * step
+        bar = e + 2.0 ** -4 * (np.abs(want) + e) + step + 2.0 ** -12 * pair
+        err = np.abs(K[pos] - want)
+        assert (err <= bar).all(), f"chunk {c}: {np.max(err / bar):.2f} bars"
 
 
 @pytest.mark.parametrize("tile_rows", [16, 128, 256])
