@@ -519,6 +519,18 @@ def test_copied_blocks_in_many_small_tiles(hq, hkv, d):
     r.run(what="copied blocks")
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(16, 4, 64), (32, 4, 128), (16, 1, 128)])
+def test_decode_of_many_tokens_in_small_tiles(hq, hkv, d):
+    """Several 16-row tiles of a request, each over the blocks that the others' rows go to: the last block's free slots, whole
+    new blocks and part of another."""
+    r = Requests(hq, hkv, d, [[0, 1], [1]], [350, 219], [7, 16], 5, tile_rows=16, spare=60)
+    r.run(what="link")
+    for new in ([21, 5], [33, 0], [1, 48]):
+        r.decode(new)
+        assert r.sizes.tile_rows == 16 and r.sizes.n_tiles >= sum(n * (hq // hkv) // 16 for n in new)
+        r.run(what=f"decode {new}")
+
+
 @pytest.mark.parametrize("tile_rows", [16, 128, 256])
 @pytest.mark.parametrize("d", [64, 128])
 def test_nan_in_a_chunk(d, tile_rows):
