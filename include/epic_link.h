@@ -557,7 +557,12 @@ epic_status epic_kv8_unpack(const epic_attn_cfg* cfg, int32_t n, const int32_t* 
  * q_s, k_s, v_s, out, lse as there.  workspace: epic_link_kv8_workspace_bytes() bytes (0 without
  * split-KV partials and wide tiles), 16-byte aligned; calls in flight at the same time need separate
  * ones.  Plans of wide tiles (128 or 256 rows) keep their linked blocks in it in bf16, 64 D Hkv
- * bytes each, for the time of the call.
+ * bytes for each entry of the linked table, for the time of the call.  That widening is a copy of the
+ * linked cache, so plans of few new rows over long caches are better made with tile_rows = 16 here: of one
+ * request over 131 072 cached keys of 8 heads of 128, 16 new rows of 32 heads take 88 us so, 290 by default (bf16
+ * cache: 135), 32 rows 149 and 294.
+ * The last bits of a row's result depend on the batch here too, by what its plan shares and splits and
+ * by how many private blocks it writes.
  * The plan's block ids are below cache->num_blocks. */
 size_t epic_link_kv8_workspace_bytes(const epic_attn_cfg* cfg, const epic_plan_sizes* sizes);
 epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const epic_plan_sizes* sizes, const epic_plan* plan_dev,

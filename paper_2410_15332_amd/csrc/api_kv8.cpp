@@ -141,7 +141,10 @@ extern "C" epic_status epic_link_attention_kv8(const epic_attn_cfg* cfg, const e
     launch_kv8_decode(a, *cache, rows, d, sizes->n_work, sizes->n_tiles == 1, stream);
   } else {
     // The matrix cores bound wide tiles, and every tile would widen the same keys again: they are widened once, for
-    // the bf16 kernel.  Requests that share blocks link more of them than there are: the pool then, block by block.
+    // the bf16 kernel.  Requests that share blocks link more of them than there are: the pool then, block by block.  A
+    // pool that holds more than the list, of other documents, is not: there a block is widened once for each request that
+    // links it (32 requests of 8 x 2000 tokens of 64 documents, 8505 distinct of 32 256 blocks: 2119 us over a pool of
+    // 8704, 2729 over one of 40 704).
     char* ws = static_cast<char*>(workspace);
     uint16_t* k = reinterpret_cast<uint16_t*>(ws + w.k);
     uint16_t* v = reinterpret_cast<uint16_t*>(ws + w.v);

@@ -14,7 +14,8 @@ namespace epic {
 constexpr int kKv8Scales = 32;
 constexpr int kKv8Nan = 255;                  // scale byte of a token whose K or V is not finite
 
-// Workgroups of four KV heads of a block each.
+// Workgroups of the re-rotating write: four KV heads of a block each.  The other launches fill theirs with (block, KV
+// head) pairs and take no more than that; their limit is held by this count too.
 inline int64_t kv8_groups(int64_t n, int hkv) { return n * ((hkv + 3) / 4); }
 constexpr int64_t kKv8MaxGroups = (int64_t(1) << 24) - 1;        // x 256 threads < 2^32
 
@@ -38,7 +39,7 @@ struct Kv8Rows {
 };
 // Most that the launch that reads them writes itself: each of its wavefronts looks through them, a lane each.
 constexpr int kKv8JoinedRows = 64;
-constexpr int kKv8JoinedPairs = 1024;         // (linked block, KV head) of wide tiles
+constexpr int kKv8JoinedPairs = 1024;         // (linked block, KV head) of wide tiles; measured at kv8_expand_kernel
 
 // As launch_link_write and (priv_rot not null) launch_link_write_rotated.
 void launch_kv8_write(const Kv8Rows& w, const int32_t* priv_rot, int hkv, int head_dim, float rope_theta,

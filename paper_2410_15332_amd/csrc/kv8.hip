@@ -9,8 +9,9 @@
 // from the score; whatever does not meets only the zeros, since a weight of 0 times a NaN in
 // V would be NaN.
 //
-// One wavefront per (block, KV head), the slab in registers (kv8_device.h); all four kernels
-// read and write their bytes once and are bound by that.
+// One wavefront per (block, KV head), the slab in registers (kv8_device.h).  The kernels are bound by
+// reading and writing these bytes; all do it once but the widening that also writes private blocks, which
+// forms a linked private block from its source and rows a second time.
 #include <cmath>
 
 #include "kv8_device.h"
@@ -158,8 +159,13 @@ __global__ __launch_bounds__(kThreads) void kv8_unpack_kernel(Kv8Move mv, epic_k
 // one, with K = NaN, V = 0 for NaN tokens (that kernel multiplies masked V by 0).  8208 blocks of 8 heads of 128 (809 MB):
 // 137 us, 5.9 TB/s.
 // JOINED: few private blocks (w) are written by the workgroups in front, and nothing waits for these: a private block is
-// formed again here, from its source and its rows of S.  That saves a launch: a link step over 16 blocks of
-// 8 heads 20.7 us (23.0 with two), over 324 46.8 (46.1), over 380 43.5 (42.2), over 964 125 (120).
+// formed again here, from its source and its rows of S.  That saves a launch: up to 1024 (block, KV head) pairs a link
+// step is 1 to 2 us shorter whether it writes 6 private blocks or 64; past them that is lost, the sooner the more private
+// blocks there are, as every wavefront looks through them.  One request of 32 / 8 heads of 128, us joined (two launches):
+//   pairs              128          512          768          1024         2048         3072           4128
+//   few private blocks 20.5 (22.5)  26.0 (28.1)  28.9 (30.9)  31.4 (32.9)  40.7 (41.6)  51.8 (52.8)
+//   32 private blocks               37.0 (38.5)  44.5 (44.9)  50.6 (51.6)  61.4 (61.5)  80.3 (79.3)    89.9 (88.2)
+//   64 private blocks                                                      81.0 (80.5)  105.7 (104.9)  135.0 (131.1)
 template <int D, bool JOINED>
 __global__ __launch_bounds__(kThreads) void kv8_expand_kernel(const int32_t* __restrict__ list, int n, epic_kv8_cache c,
                                                               Kv8Rows w, int hkv, uint16_t* __restrict__ k,

@@ -8,22 +8,31 @@
 //   online softmax per row in the scaled log2 domain; the running maximum lags by up to kLag,
 //     so that rows are merged over lanes and the output is rescaled only when one grows past it;
 //   O^T (D x 16) += V^T P^T by v_mfma_f32_16x16x32_bf16 over both blocks' keys: the P operand of
-//     a lane is its own 8 probabilities times their keys' 2^t (exact), rounded to bf16, and V's
-//     is the dword of 4 keys of its dim that the cache's order keeps together, for each block.
+//     a lane is its own 8 probabilities times their keys' 2^t (exact), rounded to bf16, the operands'
+//     type, and V's is the dword of 4 keys of its dim that the cache's order keeps together, for each
+//     block.  That rounding is 2^-8 of a probability at most, beside the 2^-4 that V's rounding to e4m3
+//     left; the sum of probabilities is taken before it.  Outputs are 0.0017 to 0.0024 of their norm
+//     from float64 over the same cache, where rounding them to bf16 alone is 0.0016 to 0.0017; what
+//     the probabilities lose would take a second product of as many instructions.
 // What bounds it is the read of K and V, once per item.  K's registers take the next pair as soon
 // as its scores are formed, V's after the product, and three workgroups of four wavefronts fit a
 // CU: 131 323 keys of 8 heads of 128 (271 MB) in 45.5 us, 6.0 TB/s, above what a plain read reaches
 // (55.8 with all loads behind the product and two workgroups).  With a single tile no block is read
-// twice, and K and V pass the caches (NT): 62.6 -> 56.1 us a step, write and merge among them; where
-// requests share blocks that costs 6 us of 64.  Up to 256 workgroups, one a CU, have eight wavefronts:
-// what bounds these is the chain of loads (529 keys of 8 heads of 64: 9.5 -> 8.5 us a step).
+// twice, and K and V pass the caches (NT): 51 us a step, merge among it, for 58 through them; 131 103 keys of 8
+// heads of 64: 31 for 34.  Requests that share blocks read them through the caches: 32 of them 63 us for 71, of
+// short documents 25 for 29 (of 64 dims 41.5 for 40.7).
+// Up to 256 workgroups, one a CU, have eight wavefronts: what bounds these is the chain of loads (529 keys
+// of 8 heads of 64 6.7 us a step, 8.1 by four; 4113 keys 9.5 and 9.9).  They read past the caches whether or not blocks
+// are shared, at most 256 / Hkv items then: four requests over the same 32 000 keys of a head of 128 14.8 us, 15.3 through
+// the caches, two of them 13.0 and 14.2, of 64 dims 12.3 and 13.2; 24 over the same 2000 keys 11.3 both; 24 over 300 keys
+// of 8 heads 8.7 and 8.5.
 //
 // The link write of few private blocks (decode: one or two a request) is done here too, by
 // workgroups in front of the others, and nothing waits for them: the rows of S that a private block
 // receives are read from the call's inputs and rounded by whoever attends to them, as a block of
 // their own; of the block itself the other tokens are read, from its source, and a block that is its
-// own source has only the new rows' bytes stored.  The launch saved makes a step of one request
-// shorter (529 keys 8.5 -> 6.9 us, 131 323 keys 58.4 -> 53.6) and leaves one of 32 requests at 64.
+// own source has only the new rows' bytes stored.  The launch saved makes every step shorter (529 keys
+// 6.7 us for 8.5, 131 323 keys 51 for 54, one of 32 requests 63 for 66).
 #include <cmath>
 #include <type_traits>
 
@@ -51,8 +60,7 @@ struct Kv8Block {
   uint32_t ks, vs;                            // scales of keys 4 a ..
 };
 
-// W wavefronts, RING pairs of blocks in flight of each.  NT: K and V are read past the caches, which hold nothing of
-// them that is read again.
+// W wavefronts, RING pairs of blocks in flight of each.  NT: K and V are read past the caches.
 template <int D, int W, int RING, bool NT>
 __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 1) void kv8_decode_kernel(AttnArgs a, epic_kv8_cache c, Kv8Rows w) {
   constexpr int J = D / 64;
@@ -386,7 +394,7 @@ void launch_kv8_decode(const AttnArgs& a, const epic_kv8_cache& c, const Kv8Rows
     w.groups = groups(waves);
     if (items + w.groups > 0) kernel<<<items + w.groups, 64 * waves, 0, stream>>>(a, c, w);
   };
-  if (items + groups(8) <= 256) {
+  if (items + groups(8) <= 256) {              // (NT whatever `once` says: figures above)
     if (head_dim == 128) go(kv8_decode_kernel<128, 8, 1, true>, 8);
     else go(kv8_decode_kernel<64, 8, 1, true>, 8);
     return;
