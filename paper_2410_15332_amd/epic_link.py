@@ -678,20 +678,21 @@ class Kv8Cache:
         """Itself.  Addresses and sizes other than those that were checked last are checked again (0.35 us where they are
         the same; all of shapes, types, strides and device would be 1.1)."""
         k, v, scale = self.k, self.v, self.scale
-        at = (k.data_ptr(), v.data_ptr(), scale.data_ptr(), k.numel(), v.numel(), scale.numel())
-        if at == self._at:
+        if self._at is not None and self._at == (k.data_ptr(), v.data_ptr(), scale.data_ptr(), k.numel(), v.numel(),
+                                                 scale.numel()):
             return self
+        if k is None:
+            raise ValueError("k is missing")
         if k.dim() != 6 or k.shape[2] not in (1, 2):
             raise ValueError(f"k: [blocks, Hkv, D / 64, 4, 16, 16] expected, got {tuple(k.shape)}")
         _, _, e4m3, e8m0 = _dtypes()[:4]
         num_blocks, hkv, d, device = k.shape[0], k.shape[1], 64 * k.shape[2], k.get_device()
-        for name, t, shape, dtypes in zip(("k", "v", "scale"), (k, v, scale), kv8_shapes(num_blocks, hkv, d),
-                                          (e4m3, e4m3, e8m0)):
-            _expect(name, t, shape, dtypes, device)
+        at = [_expect(name, t, shape, dtypes, device) for name, t, shape, dtypes in
+              zip(("k", "v", "scale"), (k, v, scale), kv8_shapes(num_blocks, hkv, d), (e4m3, e4m3, e8m0))]
         self.num_blocks, self.hkv, self.d, self.device = num_blocks, hkv, d, device
-        self.c = epic_kv8_cache(*at[:3], num_blocks)
+        self.c = epic_kv8_cache(*at, num_blocks)
         self.cfg = attn_cfg(hkv, hkv, d)              # what the moves need of an attention config
-        self._at = at
+        self._at = (*at, k.numel(), v.numel(), scale.numel())
         return self
 
     @classmethod

@@ -211,6 +211,35 @@ def test_moves_refuse():
     torch.cuda.synchronize()
 
 
+def test_moves_follow_the_caches_tensors():
+    """After its tensors were replaced by larger ones, and after those were resized, a cache is read and written where they
+    are, and the memory that they left stays as it is."""
+    el = _el()
+    rng = np.random.default_rng(8)
+    hkv, d = 2, 64
+    kt, k = _bf16(_rows(rng, 30, hkv, 16, d))
+    vt, v = _bf16(_rows(rng, 30, hkv, d, 16))
+    cache = el.Kv8Cache.zeros(5, hkv, d)
+    first = cache.k, cache.v, cache.scale
+    for n in (5, 9, 30, 7):
+        if n == 9:
+            cache.k, cache.v, cache.scale = (torch.zeros(s, dtype=torch.uint8, device="cuda") for s in el.kv8_shapes(n, hkv, d))
+            for t in first:
+                t.fill_(0x11)
+        elif n != 5:
+            for t, s in zip((cache.k, cache.v, cache.scale), el.kv8_shapes(n, hkv, d)):
+                t.resize_(s)
+        kn, vn = kt[30 - n:], vt[30 - n:]
+        el.epic_kv8_pack(kn, vn, cache)
+        kq, vq, ks, vs = kv8.quantise(k[30 - n:], v[30 - n:].swapaxes(-1, -2))
+        _equal(_download(cache), {"k": kq, "v": vq, "ks": ks, "vs": vs}, f"{n} blocks")
+        back_k, back_v = torch.empty_like(kn), torch.empty_like(vn)
+        el.epic_kv8_unpack(cache, back_k, back_v)
+        assert np.array_equal(back_k.double().cpu().numpy(), kv8.values(kq, ks))
+        assert np.array_equal(back_v.double().cpu().numpy(), kv8.values(vq, vs).swapaxes(-1, -2))
+    assert all(bool((t == 0x11).all()) for t in first)
+
+
 # ---------------------------------------------------------------- attention
 
 class Requests:

@@ -288,3 +288,12 @@ def test_cache_of_unlike_tensors_is_refused(name):
     t.resize_((6, *t.shape[1:]))                         # one of the three
     with pytest.raises(ValueError):
         cache.of(4, 64, -1)
+    cache = el.Kv8Cache.zeros(4, 4, 64, device="cpu")
+    parts = {"k": cache.k, "v": cache.v, "scale": cache.scale}
+    with pytest.raises(ValueError, match="missing"):
+        el.Kv8Cache(**{**parts, name: None})
+    setattr(cache, name, None)
+    with pytest.raises(ValueError, match="missing"):
+        cache.of(4, 64, -1)
+    setattr(cache, name, parts[name])
+    assert _parts(cache, 4) == _addresses(cache)
