@@ -389,6 +389,25 @@ def test_link_then_decode(hq, hkv, d, rerotate):
         r.decode(new).run(what=f"decode {new}")
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(32, 1, 64), (128, 1, 128), (16, 16, 64), (9, 9, 128)])
+def test_other_head_counts(hq, hkv, d):
+    """Groups too large for 16-row tiles, whose decode has wide ones; more KV heads than the wavefronts of a workgroup."""
+    r = Requests(hq, hkv, d, [[0, 1], [1]], [100, 37], [5, 1], 7)
+    r.run(what="link")
+    for new in ([1, 1], [0, 13], [1, 0]):
+        r.decode(new).run(what=f"decode {new}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_turned_blocks_without_rows(d):
+    """No row of S, but private blocks of turned keys: they are written, and nothing else is."""
+    r = Requests(8, 2, d, [[0, 1], [1, 0, 0]], [100, 37], [0, 0], 0, rerotate=True)
+    assert r.sizes.n_s == 0 and r.sizes.n_private > 0
+    r.run(what="turned blocks alone")
+    r.rerotate = False
+    r.decode([1, 2]).run(what="decode")
+
+
 @pytest.mark.parametrize("tile_rows", [16, 128, 256])
 @pytest.mark.parametrize("split", [0, 1, 3, 8])
 @pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (32, 8, 128)])
