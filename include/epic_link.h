@@ -551,7 +551,8 @@ epic_status epic_kv8_unpack(const epic_attn_cfg* cfg, int32_t n, const int32_t* 
  *   1. every private block takes its source's bytes (K of re-rotated blocks: turned in fp32 and
  *      rounded to 8 bits again; see epic_rope_cfg for the keys that these may hold), then the S rows k_s / v_s, rounded; a slot with neither holds zeros;
  *   2. attention as there, over the values that the cache now holds, with fp32 sums (V of 2^119 and
- *      more may overflow them), P rounded to bf16.  A row that attends to a NaN token has NaN in
+ *      more may overflow them), P rounded to bf16 (in 16-row tiles times the scale of V: probabilities of
+ *      tokens whose V stays below some 2^-102 lose bits there).  A row that attends to a NaN token has NaN in
  *      out, and its lse means nothing; NaN in tokens after a row, or in slots past a block's
  *      tokens, does not reach it.
  * q_s, k_s, v_s, out, lse as there.  workspace: epic_link_kv8_workspace_bytes() bytes (0 without
